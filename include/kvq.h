@@ -212,6 +212,39 @@ kvq_status_t kvq_append_decode_attention_batch(kvq_cache_t* const* caches, int32
                                                void* const* out_dev, int32_t out_is_fp32, float softmax_scale,
                                                void* hip_stream);
 
+/* Causal attention of whole prompts, or of chunks of them, over fp16 keys and values: packed sequences of different
+ * lengths, grouped heads.  Needs no cache; the keys and values are those that kvq_quantize_append takes next.
+ *   Sequence i has the query rows q_begin_host[i] .. q_begin_host[i + 1] - 1 and the key and value rows k_begin_host[i] ..
+ *   k_begin_host[i + 1] - 1 (host arrays of n_seqs + 1 non-decreasing row numbers, read during the call; k_begin_host ==
+ *   NULL: the same as the queries').  Its n_q queries are the last of its n_k keys: query i sees the keys 0 .. i + n_k - n_q,
+ *     out[i, h, :] = softmax_j( q[i, h, :] . k[j, h / g, :] * softmax_scale ) v[j, h / g, :],
+ *   so n_q = n_k is a whole prompt, n_q < n_k a chunk behind the keys of earlier ones, n_q = 1 a decode step.  A query that sees no
+ *   key (n_k < n_q) gets zeros and lse = -inf.  Keys that a query does not see do not reach it, whatever they hold.
+ *   q_dev, out_dev: row (t, h) at t * *_token_stride + h * *_head_stride elements, 128 consecutive ones; k_dev, v_dev the same
+ *   with KV heads.  Strides are multiples of 8 and not negative (a head stride of 0 in inputs: broadcast), addresses of
+ *   16 bytes; the token strides of k and v are 128 .. 2^22 - 1.  Output fp16, or
+ *   fp32 with out_is_fp32.
+ *   lse_dev: NULL, or fp32 [n_q_heads][q_begin_host[n_seqs]]: log of the sum of exponentials of every row's scaled scores.
+ *   softmax_scale 0 means 1 / sqrt(128).
+ *   workspace_dev: kvq_prompt_workspace_bytes() bytes, 16-byte aligned, for launches of few rows over many keys, which are cut into
+ *   ranges of keys; with less, or NULL, they are not cut, which is slower.  It may be reused by the next call on the stream.
+ * Enqueues kernels only and may be captured.  Sums run in a fixed order: equal calls give equal bits. */
+typedef struct {
+    int32_t n_q_heads;     /* query head h reads KV head h / (n_q_heads / n_kv_heads); at most 16 of them share one */
+    int32_t n_kv_heads;
+    int64_t q_token_stride, q_head_stride;
+    int64_t k_token_stride, k_head_stride;
+    int64_t v_token_stride, v_head_stride;
+    int64_t out_token_stride, out_head_stride;
+    int32_t out_is_fp32;
+    float softmax_scale;
+} kvq_prompt_t;
+uint64_t kvq_prompt_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, const int32_t* q_begin_host,
+                                    const int32_t* k_begin_host, int32_t n_seqs);
+kvq_status_t kvq_prompt_attention(const kvq_prompt_t* prompt, const void* q_dev, const void* k_dev, const void* v_dev,
+                                  void* out_dev, float* lse_dev, const int32_t* q_begin_host, const int32_t* k_begin_host,
+                                  int32_t n_seqs, void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
+
 /* Bookkeeping read-out (host only): maximal runs of pages with equal width, oldest first.
  *   segs_host[cap] receives min(cap, *n) entries; n, bytes_used, n_tokens, current_bits may each be NULL.
  *   bytes_used = sum over tokens of batch * n_kv_heads * kvq_bytes_per_token_head(bits of that token). */

@@ -31,6 +31,12 @@ class KvqConfig(C.Structure):
                          page_tokens, policy, count_metadata_in_budget)
 
 
+class _Prompt(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32)] + [
+        (x + "_" + d + "_stride", C.c_int64) for x in ("q", "k", "v", "out") for d in ("token", "head")] + [
+        ("out_is_fp32", C.c_int32), ("softmax_scale", C.c_float)]
+
+
 class _SegmentInfo(C.Structure):
     _fields_ = [("token_begin", C.c_int32), ("token_end", C.c_int32), ("bits", C.c_int32)]
 
@@ -80,6 +86,9 @@ _SIGNATURES = {
                                     C.POINTER(C.c_int32), C.POINTER(C.c_double), C.POINTER(C.c_uint64)]),
     "kvq_cache_sq_error": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(C.c_double), C.c_void_p]),
     "kvq_stream_read_probe": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_int32, C.c_void_p]),
+    "kvq_prompt_workspace_bytes": (C.c_uint64, [C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32]),
+    "kvq_prompt_attention": (C.c_int, [C.POINTER(_Prompt), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
     "kvq_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -169,6 +178,42 @@ def kvq_append_decode_attention_batch(caches, layer, ks, vs, qs, outs, cos_sins=
                                                           float(softmax_scale), _stream(stream))
     if st != KVQ_OK:
         raise KvqError(st, "kvq_append_decode_attention_batch")
+
+
+def _rows(begin):
+    """Host array of row numbers."""
+    return (C.c_int32 * len(begin))(*[int(x) for x in begin])
+
+
+def kvq_prompt_workspace_bytes(n_q_heads, n_kv_heads, q_begin, k_begin=None) -> int:
+    assert k_begin is None or len(k_begin) == len(q_begin)
+    return int(load_library().kvq_prompt_workspace_bytes(n_q_heads, n_kv_heads, _rows(q_begin),
+                                                         None if k_begin is None else _rows(k_begin), len(q_begin) - 1))
+
+
+def kvq_prompt_attention(q, k, v, out, q_begin, k_begin=None, softmax_scale=0.0, lse=None, workspace=None, stream=None):
+    """Causal attention of packed sequences.  q [rows, n_q_heads, 128], k, v [rows, n_kv_heads, 128]: fp16 device tensors of any
+    strides (transposed and sliced ones too) whose channels follow one another; out like q, fp16 or fp32.  q_begin, k_begin:
+    host sequences of n_seqs + 1 row numbers.  lse: fp32 device tensor [n_q_heads, q_begin[-1]] or None; workspace: uint8 device tensor or None."""
+    q_begin = [int(x) for x in q_begin]
+    k_begin = q_begin if k_begin is None else [int(x) for x in k_begin]
+    assert len(q_begin) == len(k_begin) >= 2
+    for t, rows, heads in ((q, q_begin[-1], q.shape[1]), (k, k_begin[-1], k.shape[1]), (v, k_begin[-1], k.shape[1]),
+                           (out, q_begin[-1], q.shape[1])):
+        assert t.dim() == 3 and t.shape[0] >= rows and t.shape[1] == heads and t.shape[2] == 128 and t.stride(2) == 1
+    assert all(t.dtype.itemsize == 2 for t in (q, k, v))
+    assert lse is None or (tuple(lse.shape) == (q.shape[1], q_begin[-1]) and lse.dtype.itemsize == 4)
+
+    def strides(t):  # a dimension of one element may carry any stride
+        return [128 if t.shape[d] == 1 else t.stride(d) for d in (0, 1)]
+
+    d = _Prompt(q.shape[1], k.shape[1], *strides(q), *strides(k), *strides(v), *strides(out),
+                1 if out.dtype.itemsize == 4 else 0, float(softmax_scale))
+    st = load_library().kvq_prompt_attention(
+        C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), _rows(q_begin), _rows(k_begin),
+        len(q_begin) - 1, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_prompt_attention")
 
 
 def kvq_bytes_per_token_head(bits, head_dim=128, group=32, count_metadata=1, int16_tier=0) -> int:

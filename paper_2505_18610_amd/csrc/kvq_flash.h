@@ -1,0 +1,248 @@
+// Device code shared by prompt attention and tree attention (gfx950): attention of many query rows over 32-token tiles of fp16
+// keys and values, one pass with a running maximum and sum.
+//
+// Both contractions are taken transposed, with v_mfma_f32_16x16x32_f16 and the rows in its N dimension:
+//   S^T[token, row] = K q^T,   O^T[channel, row] += V^T P^T.
+// lane = 16 j + n.  The K operand's rows are dealt so that lane quarter j receives the scores of tokens 8j .. 8j + 7 of row n, which
+// after exponentiation are the B operand of the second product as they stand: nothing crosses lanes between the products.  A
+// wavefront carries R groups of 16 rows, so an operand read from LDS serves R products.
+//
+// Statistics: the maximum is kept per row in log2 units, the sum in 32 bits from the unrounded probabilities.  Probabilities are
+// rounded to fp16 for the second product (relative to the running maximum: at most 2^-12 of the largest weight).  The accumulators are
+// rescaled only when some row's maximum moves.
+#ifndef KVQ_FLASH_H
+#define KVQ_FLASH_H
+
+#include <hip/hip_runtime.h>
+#include "kvq_layout.h"
+
+namespace kvq_flash {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+#define KVQ_FLASH_TILE_BYTES 8192  // one fp16 K or V tile in LDS
+
+__device__ inline float4v mfma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline uint32_t pack_rn(float a, float b) {
+    const half2v h = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, h);
+}
+struct Swapped { float lo, hi; };
+// over the four lane quarters, in every lane
+__device__ inline float quarters_max(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float quarters_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int R>
+struct State {
+    float4v o[R][8];  // o[r][nt][i]: channel 16 nt + 4 j + i of row n of group r
+    float m[R];       // running maximum (log2 units), equal in the four quarters
+    float l[R];       // this quarter's share of the sum
+    __device__ void clear() {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt) o[r][nt] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+
+// What is subtracted from a score: the maximum, or zero while nothing has been seen (exp2(-inf - -inf) would be NaN).
+__device__ inline float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// Probabilities of TT tiles for row group r from raw scores s (before the scale), masked ones at -inf; p in the order of the V
+// operand: natural, or (v, v + 4) pairs of a quarter's eight tokens.
+template <int R, int TT, bool PAIRED>
+__device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT][2], float scale_log2, uint32_t (&p)[TT][4]) {
+    float lmax = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, s[t][sub][i]);
+    lmax *= scale_log2;
+    if (__any(lmax > st.m[r])) {
+        const float m_new = fmaxf(st.m[r], quarters_max(lmax));
+        const float alpha = __builtin_amdgcn_exp2f(st.m[r] - reference_of(m_new));  // 0 for the first scores
+        st.l[r] *= alpha;
+#pragma unroll
+        for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= alpha;
+        st.m[r] = m_new;
+    }
+    const float ref = reference_of(st.m[r]);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        float e[2][4];
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[sub][i] = __builtin_amdgcn_exp2f(fmaf(s[t][sub][i], scale_log2, -ref));
+                st.l[r] += e[sub][i];
+            }
+        if constexpr (PAIRED) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) p[t][v] = pack_rn(e[0][v], e[1][v]);
+        } else {
+            p[t][0] = pack_rn(e[0][0], e[0][1]);
+            p[t][1] = pack_rn(e[0][2], e[0][3]);
+            p[t][2] = pack_rn(e[1][0], e[1][1]);
+            p[t][3] = pack_rn(e[1][2], e[1][3]);
+        }
+    }
+}
+
+__device__ inline half8 as_half8(const uint32_t (&w)[4]) {
+    const u32x4 v = {w[0], w[1], w[2], w[3]};
+    return __builtin_bit_cast(half8, v);
+}
+__device__ inline half8 as_half8(u32x4 v) { return __builtin_bit_cast(half8, v); }
+
+// A V tile in LDS, row-major in blocks that the transposing read takes whole: token 8 j + 4 h + k, channel 16 nt + c at byte
+// ((2 nt + h) 64 + 16 j + 4 k) 8 + 2 c.  A read covers 512 consecutive bytes; of 16 lanes, lane n receives channel n of four tokens.
+__device__ inline half8 read_v(const uint8_t* tile, int nt, int lane) {
+    typedef __attribute__((address_space(3))) short4v lds_short4;
+    const uint8_t* at = tile + (nt * 128 + lane) * 8;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at));
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + 512));
+    const auto both = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(half8, both);
+}
+// Where the 16 bytes of (token, chunk of 8 channels) go in such a tile, and in a K tile (operand order).
+__device__ inline int v_chunk_at(int token, int chunk) {
+    return ((chunk >> 1) * 128 + ((token >> 2) & 1) * 64 + (token >> 3) * 16 + (token & 3) * 4 + (chunk & 1) * 2) * 8;
+}
+__device__ inline int k_chunk_at(int token, int chunk) {
+    return ((((token >> 2) & 1) * 4 + (chunk >> 2)) * 64 + (chunk & 3) * 16 + (token >> 3) * 4 + (token & 3)) * 16;
+}
+
+// A lane's eight values of one V operand added to `seen` times zero: 0 stays 0 unless one of them is infinite or NaN.
+__device__ inline void watch_nonfinite(half8 v, uint32_t& seen) {
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    half2v acc = __builtin_bit_cast(half2v, seen);
+    const half2v zero = {(_Float16)0.f, (_Float16)0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t two = w[e];  // (a bit cast of a vector's element itself takes its first one)
+        acc += __builtin_bit_cast(half2v, two) * zero;
+    }
+    seen = __builtin_bit_cast(uint32_t, acc) & 0x7fff7fffu;
+}
+
+// The products of a V operand that holds infinities or NaNs: a key that a row does not see must not reach it, not even as zero times
+// infinity.  The finite values are taken as ever; three more products count the infinities of either sign and the NaNs among the
+// keys that the row sees (`seen`: 1 for these, 0 for the others, in the order of p), and what is counted decides.  Slow, and rare.
+__device__ inline float4v mfma_nonfinite(half8 v, half8 p, half8 seen, float4v o) {
+    half8 finite, kind[3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const _Float16 x = v[e];
+        const uint16_t w = __builtin_bit_cast(uint16_t, x), size = w & 0x7fffu;
+        finite[e] = size < 0x7c00u ? x : (_Float16)0.f;
+        kind[0][e] = w == 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+        kind[1][e] = w == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
+        kind[2][e] = size > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+    }
+    o = mfma(finite, p, o);
+    const float values[3] = {INFINITY, -INFINITY, __builtin_nanf("")};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const float4v count = mfma(kind[k], seen, float4v{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += count[i] > 0.f ? values[k] : 0.f;
+    }
+    return o;
+}
+
+// Joins the states of two wavefronts that saw different tokens of the same rows: x of the other one.
+template <int R>
+__device__ inline void join_row(State<R>& st, int r, float m_x, float l_x, float& w_mine, float& w_x) {
+    const float m_new = fmaxf(st.m[r], m_x), ref = reference_of(m_new);
+    w_mine = __builtin_amdgcn_exp2f(st.m[r] - ref);
+    w_x = __builtin_amdgcn_exp2f(m_x - ref);
+    st.l[r] = st.l[r] * w_mine + l_x * w_x;
+    st.m[r] = m_new;
+}
+
+// Bytes of LDS that join_waves needs for half of a workgroup's wavefronts.
+template <int R> constexpr int join_bytes() { return R * (8 * 64 * 16 + 2 * 64 * 4); }
+// The WT wavefronts wt = 0 .. WT - 1 that share rows (the same wm) hand their states to wt = 0, halving by halving.  lds: WM * WT / 2
+// times join_bytes<R>().  Every wavefront of the workgroup takes part.
+template <int R, int WM, int WT>
+__device__ inline void join_waves(State<R>& st, uint8_t* lds, int wm, int wt, int lane) {
+#pragma unroll
+    for (int half = WT / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        uint8_t* const at = lds + (wm * (WT / 2) + (wt % half)) * join_bytes<R>();
+        float4v* const o = reinterpret_cast<float4v*>(at);
+        float* const ml = reinterpret_cast<float*>(at + R * 8 * 64 * 16);
+        if (wt >= half && wt < 2 * half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) o[(r * 8 + nt) * 64 + lane] = st.o[r][nt];
+                ml[(r * 2) * 64 + lane] = st.m[r];
+                ml[(r * 2 + 1) * 64 + lane] = st.l[r];
+            }
+        }
+        __syncthreads();
+        if (wt < half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float a, b;
+                join_row<R>(st, r, ml[(r * 2) * 64 + lane], ml[(r * 2 + 1) * 64 + lane], a, b);
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] = st.o[r][nt] * a + o[(r * 8 + nt) * 64 + lane] * b;
+            }
+        }
+    }
+}
+
+// Partial results of one group of 16 rows and one split, 32 bits, as the lanes hold them: 8 KiB of un-normalised outputs
+// [nt][lane][4] and the pairs (maximum, sum) of the 16 rows.
+#define KVQ_PART_O_FLOATS (8 * 64 * 4)
+#define KVQ_PART_ML_FLOATS 32
+#define KVQ_PART_BYTES ((KVQ_PART_O_FLOATS + KVQ_PART_ML_FLOATS) * 4)
+
+template <int R>
+__device__ inline void store_partial(const State<R>& st, int r, float* part, int lane) {
+    float4v* const o = reinterpret_cast<float4v*>(part);
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) o[nt * 64 + lane] = st.o[r][nt];
+    const float l = quarters_sum(st.l[r]);
+    if (lane < 16) {
+        part[KVQ_PART_O_FLOATS + 2 * lane] = st.m[r];
+        part[KVQ_PART_O_FLOATS + 2 * lane + 1] = l;
+    }
+}
+
+// Four channels of an output row.
+__device__ inline void store_out4(void* row, int fp32, int channel, float4v x) {
+    if (fp32) {
+        *reinterpret_cast<float4v*>(static_cast<float*>(row) + channel) = x;
+    } else {
+        const u32x2 h = {pack_rn(x[0], x[1]), pack_rn(x[2], x[3])};
+        *reinterpret_cast<u32x2*>(static_cast<_Float16*>(row) + channel) = h;
+    }
+}
+
+}  // namespace kvq_flash
+
+#endif
