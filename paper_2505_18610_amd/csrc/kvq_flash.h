@@ -27,12 +27,15 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 #define KVQ_FLASH_TILE_BYTES 8192  // one fp16 K or V tile in LDS
 
+#ifdef KVQ_NO_ARITHMETIC  // the measurement build (build.py) loads tiles and computes on none
+__device__ inline float4v mfma(half8, half8, float4v c) { return c; }
+#else
 __device__ inline float4v mfma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+#endif
 __device__ inline uint32_t pack_rn(float a, float b) {
     const half2v h = {(_Float16)a, (_Float16)b};
     return __builtin_bit_cast(uint32_t, h);
 }
-struct Swapped { float lo, hi; };
 // over the four lane quarters, in every lane
 __device__ inline float quarters_max(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);

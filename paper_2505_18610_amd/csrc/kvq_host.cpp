@@ -13,200 +13,11 @@
 #include <vector>
 
 #include "../../include/kvq.h"
+#include "kvq_cache.h"
 #include "kvq_internal.h"
 #include "kvq_ring.h"
 
-namespace {
-
-constexpr int kMaxOrder = 4;  // allocation blocks of 1, 2, 4, 8, 16 units; a unit is one metadata block
-constexpr int kRingSegments = 4;
-constexpr uint64_t kRingSegmentBytes = 1u << 20;  // the pinned staging ring: 4 segments of 1 MiB
-constexpr uint64_t kNoSum = 0x7ff0dead0000beefull;  // a signalling NaN
-
-// Markers of the staging ring: one HIP event per segment, recorded on the cache's stream.
-struct RingEvents {
-    hipEvent_t ev[kRingSegments] = {};
-    hipStream_t stream = nullptr;
-    bool record(int i) { return hipEventRecord(ev[i], stream) == hipSuccess; }
-    bool wait(int i) { return hipEventSynchronize(ev[i]) == hipSuccess; }
-};
-
-int order_of_bits(int bits) { return bits == 16 ? 4 : bits == 8 ? 3 : bits == 4 ? 2 : 1; }
-// Kernel time of one 2/4/8/16-bit tile, measured, in units of which a workgroup does 1,000 in 0.9 us.
-constexpr int kTileTime[4] = {100, 145, 250, 300};
-bool valid_bits(int b) { return b == 16 || b == 8 || b == 4 || b == 2; }
-
-// A set of numbers below n that finds its smallest: a bit for each, and a bit per word of the level below on the levels above.
-class NumberSet {
-public:
-    bool init(uint64_t n, bool full) {
-        levels_.clear();
-        for (uint64_t bits = n;;) {
-            const uint64_t words = std::max<uint64_t>(1, (bits + 63) / 64);
-            levels_.emplace_back(static_cast<uint64_t*>(std::calloc(words, sizeof(uint64_t))));  // (pages of zeros cost nothing until written)
-            if (!levels_.back()) return false;
-            if (full) {
-                std::memset(levels_.back().get(), 0xff, (size_t)(bits / 64) * sizeof(uint64_t));
-                if (bits % 64) levels_.back()[(size_t)(bits / 64)] = (1ull << (bits % 64)) - 1;
-            }
-            if (words == 1) return true;
-            bits = words;
-        }
-    }
-    bool empty() const { return levels_.back()[0] == 0; }
-    uint32_t smallest() const {
-        uint64_t i = 0;
-        for (size_t l = levels_.size(); l-- > 0;) i = i * 64 + (uint64_t)__builtin_ctzll(levels_[l][i]);
-        return (uint32_t)i;
-    }
-    bool has(uint32_t i) const { return levels_[0][i / 64] >> (i % 64) & 1; }
-    void add(uint32_t i) {
-        for (auto& words : levels_) {
-            const uint64_t old = words[i / 64];
-            words[i / 64] = old | 1ull << (i % 64);
-            if (old) return;
-            i /= 64;
-        }
-    }
-    void remove(uint32_t i) {
-        for (auto& words : levels_) {
-            if (words[i / 64] &= ~(1ull << (i % 64))) return;
-            i /= 64;
-        }
-    }
-
-private:
-    struct Free { void operator()(uint64_t* p) const { std::free(p); } };
-    std::vector<std::unique_ptr<uint64_t[], Free>> levels_;
-};
-
-// Buddy allocator in units.  Code blocks need 2^order units (2-bit: 2, 4-bit: 4, 8-bit: 8, 16-bit: 16),
-// metadata blocks one unit, so every size is a power of two and freed space coalesces without compaction.
-// (With the free blocks in std::set a prompt of 16,000 tokens that is shrunk twice spent 55 of the host's 137 us here, and more than a
-// launch takes on most calls.)
-class Buddy {
-public:
-    bool init(uint32_t n_super) {
-        for (int o = 0; o <= kMaxOrder; ++o)
-            if (!free_[o].init((uint64_t)n_super << (kMaxOrder - o), o == kMaxOrder)) return false;
-        free_units_ = (uint64_t)n_super << kMaxOrder;
-        return true;
-    }
-    bool alloc(int order, uint32_t* off) {
-        int o = order;
-        while (o <= kMaxOrder && free_[o].empty()) ++o;
-        if (o > kMaxOrder) return false;
-        uint32_t blk = free_[o].smallest();
-        free_[o].remove(blk);
-        blk <<= o;
-        while (o > order) {
-            --o;
-            free_[o].add((blk >> o) + 1);
-        }
-        free_units_ -= 1u << order;
-        *off = blk;
-        return true;
-    }
-    void release(uint32_t off, int order) {
-        free_units_ += 1u << order;
-        uint32_t blk = off >> order;
-        while (order < kMaxOrder && free_[order].has(blk ^ 1)) {
-            free_[order].remove(blk ^ 1);
-            blk >>= 1;
-            ++order;
-        }
-        free_[order].add(blk);
-    }
-    uint64_t free_units() const { return free_units_; }
-
-private:
-    NumberSet free_[kMaxOrder + 1];
-    uint64_t free_units_ = 0;
-};
-
-struct Page {
-    int bits = 16;
-    int n = 0;              // tokens stored
-    uint32_t code_unit = 0; // allocation offsets in units
-    uint32_t meta_unit = 0; // valid when the page has metadata (bits < 16, or the integer 16-bit tier)
-};
-
-struct Run {  // neighbouring pages of one width
-    int page_end, bits;
-};
-
-struct Layer {
-    uint64_t budget = 0;
-    int fbit = 2;
-    int T = 0;
-    bool reparam = false;  // keys stored as K / lambda, queries multiplied by lambda (Sec. 3.3)
-    bool poisoned = false; // an enqueue failed after the host tables had been updated: unusable until kvq_cache_reset
-    std::vector<Page> pages;
-    // the pages as runs of one width, of the state runs_version; see runs_of
-    mutable std::vector<Run> runs;
-    mutable uint64_t runs_version = ~0ull;
-    // what the split count was worked out from and the count itself; split plan cache of kvq_decode_attention
-    uint64_t count_key[3] = {};
-    int count_splits = 1;
-    int plan_tiles = -1, plan_splits = 0;
-    bool plan_side_by_side = false;
-    uint64_t version = 0, plan_version = ~0ull;
-    int32_t split_begin[KVQ_MAX_SPLITS + 1];
-};
-
-}  // namespace
-
-struct kvq_cache {
-    kvq_config_t cfg;
-    int units = 0, tpp = 0, gqa = 0, max_pages = 0;
-    bool dry = false;
-    uint8_t* arena = nullptr;
-    uint64_t arena_bytes = 0;
-    uint64_t unit_bytes = 0;
-    uint64_t table_off = 0, jobs_off = 0, part_o_off = 0, part_ml_off = 0, counters_off = 0, flags_off = 0, pages_off = 0;
-    uint64_t reparam_off = 0;  // per block: lambda [n_kv_heads][128] fp32, then 1 / lambda
-    uint32_t v_epoch = 4;      // see KvqVMark; 0 is what a cleared word holds
-    uint32_t v_turn = 1;       // tag of the next launch that appends below 16 bits, above the epoch; see kvq_v_marked
-    KvqVMark v_mark() const { return KvqVMark{reinterpret_cast<uint32_t*>(arena + flags_off), v_epoch}; }
-    Buddy buddy;
-    std::vector<Layer> layers;
-    uint8_t* ring = nullptr;
-    uint8_t* ring_dev = nullptr;  // the same pinned memory as the device addresses it
-    KvqStagingRing<RingEvents, kRingSegments> ring_ctl;
-    RingEvents ring_events;
-    uint64_t* sums = nullptr;   // behind the ring: 2 sums for each workgroup of the error kernel, kNoSum between calls
-    bool sums_at_rest = false;
-    bool device_ready = false;
-    bool enqueue_failed = false;  // a block was left unusable since the device's counters were last cleared
-    int splits_override = 0;
-    int fused_merge = 1;
-    int deterministic = 0;
-    int shift_strategy = KVQ_SHIFT_EQUIVALENT;  // how 2b -> b steps treat codes, S and Z (Sec. 4.3.1)
-    int tier16 = KVQ_TIER16_FP16;               // what a 16-bit token is: raw fp16, or 16-bit codes with (S, Z)
-    bool int16() const { return tier16 == KVQ_TIER16_INT16; }
-    bool has_meta(int bits) const { return bits < 16 || int16(); }
-    int tile_cost[4] = {kTileTime[0], kTileTime[1], kTileTime[2], kTileTime[3]};  // KVQ_OPT_TILE_COST_*
-    int target_workgroups = 256;
-
-    uint64_t bpth(int bits) const {
-        return kvq_bytes_per_token_head(bits, cfg.head_dim, cfg.group, cfg.count_metadata_in_budget, int16() ? 1 : 0);
-    }
-    uint64_t unit_off_bytes(uint32_t unit) const { return pages_off + (uint64_t)unit * unit_bytes; }
-    KvqPageDesc desc(const Page& p) const {
-        KvqPageDesc d;
-        d.code_off256 = (uint32_t)(unit_off_bytes(p.code_unit) / 256);
-        d.meta_off256 = has_meta(p.bits) ? (uint32_t)(unit_off_bytes(p.meta_unit) / 256) : 0u;
-        d.bits = (uint32_t)p.bits;
-        d.int16 = (p.bits == 16 && int16()) ? 1u : 0u;
-        return d;
-    }
-    float* lambda_dev(int layer) const {  // lambda of the block; its reciprocals follow
-        return reinterpret_cast<float*>(arena + reparam_off) + (size_t)layer * 2 * cfg.n_kv_heads * KVQ_D;
-    }
-    KvqPageDesc* table_dev(int layer) const {
-        return reinterpret_cast<KvqPageDesc*>(arena + table_off) + (size_t)layer * max_pages;
-    }
-};
+using namespace kvq_host;
 
 namespace {
 
@@ -245,8 +56,8 @@ Regions layout_regions(const kvq_config_t* c) {
     return r;
 }
 
-hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
-
+}  // namespace
+namespace kvq_host {
 // Copy `bytes` of host data to device memory in stream order through the pinned staging ring (in pieces of at most
 // one ring segment).  The host waits only if it is a whole ring ahead of the device.
 kvq_status_t upload(kvq_cache* c, void* dst_dev, const void* src, uint64_t bytes, hipStream_t s) {
@@ -263,6 +74,8 @@ kvq_status_t upload(kvq_cache* c, void* dst_dev, const void* src, uint64_t bytes
     }
     return KVQ_OK;
 }
+}  // namespace kvq_host
+namespace {
 
 // Place `bytes` of host data (at most one ring segment) in the pinned staging ring and return where (a host address
 // the device can read as well); the space is not reused before the work enqueued on s after this call has completed.
@@ -276,6 +89,8 @@ kvq_status_t stage(kvq_cache* c, const void* src, uint64_t bytes, hipStream_t s,
     return KVQ_OK;
 }
 
+}  // namespace
+namespace kvq_host {
 kvq_status_t ensure_device(kvq_cache* c, hipStream_t s) {
     if (c->dry || c->device_ready) return KVQ_OK;
     // counters and flags are adjacent regions: one fill clears both
@@ -285,6 +100,8 @@ kvq_status_t ensure_device(kvq_cache* c, hipStream_t s) {
     c->device_ready = true;
     return KVQ_OK;
 }
+}  // namespace kvq_host
+namespace {
 
 kvq_status_t upload_table(kvq_cache* c, int layer, int first, int last, hipStream_t s) {
     if (c->dry || last <= first) return KVQ_OK;
@@ -307,6 +124,8 @@ const std::vector<Run>& runs_of(const Layer& L) {
     return L.runs;
 }
 
+}  // namespace
+namespace kvq_host {
 // (every page but the last is full)
 uint64_t bytes_used(const kvq_cache* c, const Layer& L) {
     uint64_t u = 0;
@@ -318,6 +137,8 @@ uint64_t bytes_used(const kvq_cache* c, const Layer& L) {
     }
     return u;
 }
+}  // namespace kvq_host
+namespace {
 
 // Width of the block's bulk: smallest width among pages after the sink (16 if there is none).
 int current_bits(const kvq_cache* c, const Layer& L) {
@@ -1589,30 +1410,37 @@ kvq_status_t kvq_stream_read_probe(kvq_cache_t* c, const void* buf_dev, uint64_t
     return kvq_launch_stream_read(buf_dev, bytes, n_workgroups, sink, as_stream(hip_stream)) == hipSuccess ? KVQ_OK : KVQ_E_HIP;
 }
 
-kvq_status_t kvq_cache_reset(kvq_cache_t* c, int32_t layer) {
-    if (!c || layer < -1 || layer >= c->cfg.n_layers) return KVQ_E_INVALID;
-    const int first = layer < 0 ? 0 : layer, last = layer < 0 ? c->cfg.n_layers : layer + 1;
-    for (int l = first; l < last; ++l) {
-        Layer& L = c->layers[(size_t)l];
-        c->enqueue_failed = c->enqueue_failed || L.poisoned;
-        for (const Page& p : L.pages) {
-            c->buddy.release(p.code_unit, order_of_bits(p.bits));
-            if (c->has_meta(p.bits)) c->buddy.release(p.meta_unit, 0);
-        }
-        L.pages.clear();
-        L.T = 0;
-        L.version++;
-        L.plan_tiles = -1;
-        L.poisoned = false;
+}  // extern "C"
+// Takes every token of a block away.
+void kvq_host::empty_block(kvq_cache* c, Layer& L) {
+    c->enqueue_failed = c->enqueue_failed || L.poisoned;
+    for (const Page& p : L.pages) {
+        c->buddy.release(p.code_unit, order_of_bits(p.bits));
+        if (c->has_meta(p.bits)) c->buddy.release(p.meta_unit, 0);
     }
-    // An empty cache starts over: the mark that some V scale was large must not outlive the data that set it, and if an
-    // enqueue had failed the next call that enqueues work clears the device's counters and mark again, in stream order.
+    L.pages.clear();
+    L.T = 0;
+    L.version++;
+    L.plan_tiles = -1;
+    L.poisoned = false;
+}
+// An empty cache starts over: the mark that some V scale was large must not outlive the data that set it, and if an
+// enqueue had failed the next call that enqueues work clears the device's counters and mark again, in stream order.
+void kvq_host::start_over_if_empty(kvq_cache* c) {
     bool all_empty = true;
-    for (const Layer& L : c->layers) all_empty = all_empty && L.T == 0;
+    for (const Layer& l : c->layers) all_empty = all_empty && l.T == 0;
     if (all_empty) {
         if ((c->v_epoch += 4) == 0) c->v_epoch = 4;
         if (c->enqueue_failed) c->device_ready = c->enqueue_failed = false;
     }
+}
+extern "C" {
+
+kvq_status_t kvq_cache_reset(kvq_cache_t* c, int32_t layer) {
+    if (!c || layer < -1 || layer >= c->cfg.n_layers) return KVQ_E_INVALID;
+    const int first = layer < 0 ? 0 : layer, last = layer < 0 ? c->cfg.n_layers : layer + 1;
+    for (int l = first; l < last; ++l) empty_block(c, c->layers[(size_t)l]);
+    start_over_if_empty(c);
     return KVQ_OK;
 }
 
