@@ -245,6 +245,27 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* prompt, const void* q_dev,
                                   void* out_dev, float* lse_dev, const int32_t* q_begin_host, const int32_t* k_begin_host,
                                   int32_t n_seqs, void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
 
+/* Attention of drafted tokens -- the nodes of a tree, or any set with a mask among themselves -- over a block's whole cache and
+ * over one another (speculative decoding: one call scores every branch).  The nodes are not in the cache and do not enter it.
+ *   out[b, h, i, :] = softmax over the cached tokens t and the nodes j with bit j of mask row i set, of
+ *     q[b, h, i, :] . K_hat[b, h/g, t, :] * softmax_scale  and  q[b, h, i, :] . k[b, h/g, j, :] * softmax_scale,
+ *   times V_hat and v.  A node sees itself only if its own bit is set.  With an empty cache the nodes have only each other; a
+ *   node that sees nothing gets zeros.  What a node does not see does not reach it, whatever it holds.
+ *   q_dev, out_dev: [batch, n_q_heads, n_nodes, 128], fp16 and fp16 or fp32; k_dev, v_dev: fp16 [batch, n_kv_heads, n_nodes, 128],
+ *   keys rotated at the nodes' positions and, in a block with factors (kvq_cache_set_reparam), as they are: the factors
+ *   apply to the cached keys alone.  1 <= n_nodes <= 1024; addresses of 16 bytes.
+ *   mask_dev: words of 32 bits, [n_nodes][(n_nodes + 31) / 32], bit j % 32 of word j / 32; with mask_per_sequence one such table for
+ *   each sequence, one after the other.  softmax_scale 0 means 1 / sqrt(128).
+ *   workspace_dev: kvq_tree_workspace_bytes() bytes for the results of ranges of the cache, 16-byte aligned; with less, or NULL,
+ *   the cache is cut into fewer ranges or none, which is slower.  It may be reused by the next call on the stream.
+ * Cached values are formed as code * S + Z and rounded to fp16; fp32 accumulation.  Enqueues kernels only and may be captured
+ * (the cache must not change between capture and replay).  Sums run in a fixed order.  KVQ_E_STATE on an accounting-only cache. */
+uint64_t kvq_tree_workspace_bytes(const kvq_cache_t* cache, int32_t n_nodes);
+kvq_status_t kvq_tree_attention(kvq_cache_t* cache, int32_t layer, const void* q_dev, const void* k_dev, const void* v_dev,
+                                int32_t n_nodes, const uint32_t* mask_dev, int32_t mask_per_sequence, void* out_dev,
+                                int32_t out_is_fp32, float softmax_scale, void* workspace_dev, uint64_t workspace_bytes,
+                                void* hip_stream);
+
 /* Bookkeeping read-out (host only): maximal runs of pages with equal width, oldest first.
  *   segs_host[cap] receives min(cap, *n) entries; n, bytes_used, n_tokens, current_bits may each be NULL.
  *   bytes_used = sum over tokens of batch * n_kv_heads * kvq_bytes_per_token_head(bits of that token). */

@@ -89,6 +89,9 @@ _SIGNATURES = {
     "kvq_prompt_workspace_bytes": (C.c_uint64, [C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32]),
     "kvq_prompt_attention": (C.c_int, [C.POINTER(_Prompt), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "kvq_tree_workspace_bytes": (C.c_uint64, [C.c_void_p, C.c_int32]),
+    "kvq_tree_attention": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32,
+                                     C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_uint64, C.c_void_p]),
     "kvq_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -305,6 +308,23 @@ class KvqCache:
         self._check(self.lib.kvq_append_decode_attention(self.handle, layer, _ptr(k), _ptr(v), _ptr(cos_sin), _ptr(q),
                                                          _ptr(out), out_is_fp32, float(softmax_scale), _stream(stream)),
                     "kvq_append_decode_attention")
+
+    def kvq_tree_workspace_bytes(self, n_nodes) -> int:
+        return int(self.lib.kvq_tree_workspace_bytes(self.handle, n_nodes))
+
+    def kvq_tree_attention(self, layer, q, k, v, mask, out, softmax_scale=0.0, workspace=None, stream=None):
+        """Drafted tokens over the cache and each other.  q, out [batch, n_q_heads, n, 128], k, v [batch, n_kv_heads, n, 128];
+        mask: int32 device tensor [n, words] for every sequence or [batch, n, words], bit j % 32 of word j // 32 of row i: node i
+        sees node j.  workspace: uint8 device tensor of kvq_tree_workspace_bytes(n), or None."""
+        c, n = self.cfg, q.shape[2]
+        assert tuple(q.shape) == tuple(out.shape) == (c.batch, c.n_q_heads, n, 128)
+        assert tuple(k.shape) == tuple(v.shape) == (c.batch, c.n_kv_heads, n, 128)
+        assert all(t.dtype.itemsize == 2 for t in (q, k, v)) and mask.dtype.itemsize == 4
+        assert tuple(mask.shape) in ((n, (n + 31) // 32), (c.batch, n, (n + 31) // 32))
+        self._check(self.lib.kvq_tree_attention(self.handle, layer, _ptr(q), _ptr(k), _ptr(v), n, _ptr(mask), int(mask.dim() == 3),
+                                                _ptr(out), 1 if out.dtype.itemsize == 4 else 0, float(softmax_scale), _ptr(workspace),
+                                                0 if workspace is None else workspace.numel(), _stream(stream)),
+                    "kvq_tree_attention")
 
     def kvq_cache_describe(self, layer):
         """Returns (segments [(token_begin, token_end, bits)], bytes_used, n_tokens, current_bits)."""

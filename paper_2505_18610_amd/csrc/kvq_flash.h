@@ -28,11 +28,11 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 #define KVQ_FLASH_TILE_BYTES 8192  // one fp16 K or V tile in LDS
 
 #ifdef KVQ_NO_ARITHMETIC  // the measurement build (build.py) loads tiles and computes on none
-__device__ inline float4v mfma(half8, half8, float4v c) { return c; }
+__device__ inline float4v mma(half8, half8, float4v c) { return c; }
 #else
-__device__ inline float4v mfma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline float4v mma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 #endif
-__device__ inline uint32_t pack_rn(float a, float b) {
+__device__ inline uint32_t pack2(float a, float b) {
     const half2v h = {(_Float16)a, (_Float16)b};
     return __builtin_bit_cast(uint32_t, h);
 }
@@ -102,21 +102,21 @@ __device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT]
             }
         if constexpr (PAIRED) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) p[t][v] = pack_rn(e[0][v], e[1][v]);
+            for (int v = 0; v < 4; ++v) p[t][v] = pack2(e[0][v], e[1][v]);
         } else {
-            p[t][0] = pack_rn(e[0][0], e[0][1]);
-            p[t][1] = pack_rn(e[0][2], e[0][3]);
-            p[t][2] = pack_rn(e[1][0], e[1][1]);
-            p[t][3] = pack_rn(e[1][2], e[1][3]);
+            p[t][0] = pack2(e[0][0], e[0][1]);
+            p[t][1] = pack2(e[0][2], e[0][3]);
+            p[t][2] = pack2(e[1][0], e[1][1]);
+            p[t][3] = pack2(e[1][2], e[1][3]);
         }
     }
 }
 
-__device__ inline half8 as_half8(const uint32_t (&w)[4]) {
+__device__ inline half8 to_half8(const uint32_t (&w)[4]) {
     const u32x4 v = {w[0], w[1], w[2], w[3]};
     return __builtin_bit_cast(half8, v);
 }
-__device__ inline half8 as_half8(u32x4 v) { return __builtin_bit_cast(half8, v); }
+__device__ inline half8 to_half8(u32x4 v) { return __builtin_bit_cast(half8, v); }
 
 // A V tile in LDS, row-major in blocks that the transposing read takes whole: token 8 j + 4 h + k, channel 16 nt + c at byte
 // ((2 nt + h) 64 + 16 j + 4 k) 8 + 2 c.  A read covers 512 consecutive bytes; of 16 lanes, lane n receives channel n of four tokens.
@@ -163,11 +163,11 @@ __device__ inline float4v mfma_nonfinite(half8 v, half8 p, half8 seen, float4v o
         kind[1][e] = w == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
         kind[2][e] = size > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
     }
-    o = mfma(finite, p, o);
+    o = mma(finite, p, o);
     const float values[3] = {INFINITY, -INFINITY, __builtin_nanf("")};
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        const float4v count = mfma(kind[k], seen, float4v{0.f, 0.f, 0.f, 0.f});
+        const float4v count = mma(kind[k], seen, float4v{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] += count[i] > 0.f ? values[k] : 0.f;
     }
@@ -236,12 +236,35 @@ __device__ inline void store_partial(const State<R>& st, int r, float* part, int
     }
 }
 
+// Joins n partial results of a group of rows, `step` floats apart: a lane's four channels of block nt of row n, and the row's statistics.
+struct Joined {
+    float4v o;
+    float m, l;
+};
+__device__ inline Joined join_partials(const float* part, int64_t step, int n_parts, int nt, int lane) {
+    const int n = lane & 15;
+    float m = -INFINITY;
+    for (int s = 0; s < n_parts; ++s) m = fmaxf(m, part[s * step + KVQ_PART_O_FLOATS + 2 * n]);
+    const float ref = reference_of(m);
+    Joined x{float4v{0.f, 0.f, 0.f, 0.f}, m, 0.f};
+    for (int s = 0; s < n_parts; ++s) {
+        const float* at = part + s * step;
+        const float w = __builtin_amdgcn_exp2f(at[KVQ_PART_O_FLOATS + 2 * n] - ref);
+        x.l += w * at[KVQ_PART_O_FLOATS + 2 * n + 1];
+        x.o += *reinterpret_cast<const float4v*>(at + (nt * 64 + lane) * 4) * w;
+    }
+    return x;
+}
+
+// What the sum of a row's weights divides by: a row that saw nothing gives zeros.
+__device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
 // Four channels of an output row.
 __device__ inline void store_out4(void* row, int fp32, int channel, float4v x) {
     if (fp32) {
         *reinterpret_cast<float4v*>(static_cast<float*>(row) + channel) = x;
     } else {
-        const u32x2 h = {pack_rn(x[0], x[1]), pack_rn(x[2], x[3])};
+        const u32x2 h = {pack2(x[0], x[1]), pack2(x[2], x[3])};
         *reinterpret_cast<u32x2*>(static_cast<_Float16*>(row) + channel) = h;
     }
 }

@@ -195,6 +195,8 @@ inline bool kvq_batch_fits_args(const KvqAttnParams* p, int n) {
     return ranges <= KVQ_BATCH_ARG_SPLITS;
 }
 
+#define KVQ_MAX_TREE_NODES 1024  // of one kvq_tree_attention
+
 // Static scratch of kvq_decode_attention_static (kvq_attention.hip): room for the partials of KVQ_STATIC_MAX_WGS
 // workgroups (units * splits of one launch) and their arrival counters (a launch of more than one split per unit has at most
 // half as many units as workgroups).

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
             u32x4 w = *reinterpret_cast<const u32x4*>(src + 32 * grp);
             w ^= A.flip;
             if (!real) w = u32x4{0, 0, 0, 0};
-            q[r][grp] = as_half8(w);
+            q[r][grp] = to_half8(w);
         }
     }
 #pragma unroll
@@ -181,9 +181,9 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                         for (int r = 0; r < R; ++r) s[r][x][sub] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int grp = 0; grp < 4; ++grp) {
-                            const half8 a = as_half8(*reinterpret_cast<const u32x4*>(kt + x * (2 * KVQ_FLASH_TILE_BYTES) + ((sub * 4 + grp) * 64 + lane) * 16));
+                            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(kt + x * (2 * KVQ_FLASH_TILE_BYTES) + ((sub * 4 + grp) * 64 + lane) * 16));
 #pragma unroll
-                            for (int r = 0; r < R; ++r) s[r][x][sub] = mfma(a, q[r][grp], s[r][x][sub]);
+                            for (int r = 0; r < R; ++r) s[r][x][sub] = mma(a, q[r][grp], s[r][x][sub]);
                         }
                     }
                 // behind the causal border of some row, beyond the last key or beyond the range
@@ -223,9 +223,9 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) seen[i] = i < end ? (_Float16)1.f : (_Float16)0.f;
                                 asm volatile("" ::: "memory");
-                                st.o[r][nt] = mfma_nonfinite(a, as_half8(p[r][x]), seen, st.o[r][nt]);
+                                st.o[r][nt] = mfma_nonfinite(a, to_half8(p[r][x]), seen, st.o[r][nt]);
                             } else {
-                                st.o[r][nt] = mfma(a, as_half8(p[r][x]), st.o[r][nt]);
+                                st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
                             }
                         }
                     }
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         const float l = quarters_sum(st.l[r]);
         const Row row = row_of<RB>(A, S, it.block, wm * 16 * R + 16 * r + n);
         if (row.head < 0) continue;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = inverse_of(l);
         const int head = it.kv * A.gqa + row.head;
         const int64_t tok = S.q0 + row.query, at = tok * A.o_ts + (int64_t)head * A.o_hs;
         void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
@@ -272,24 +272,14 @@ __global__ __launch_bounds__(512) void kvq_prompt_merge_kernel(const PromptArgs 
     if (S.splits == 1 || it.split != 0) return;
     const int64_t step = (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4);
     const float* part = A.part + (S.part0 + (int64_t)(it.kv * S.blocks + it.block) * S.splits * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
-    float m = -INFINITY;
-    for (int s = 0; s < S.splits; ++s) m = fmaxf(m, part[s * step + KVQ_PART_O_FLOATS + 2 * n]);
-    const float ref = reference_of(m);
-    float l = 0.f;
-    float4v o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < S.splits; ++s) {
-        const float* at = part + s * step;
-        const float w = __builtin_amdgcn_exp2f(at[KVQ_PART_O_FLOATS + 2 * n] - ref);
-        l += w * at[KVQ_PART_O_FLOATS + 2 * n + 1];
-        o += *reinterpret_cast<const float4v*>(at + (nt * 64 + lane) * 4) * w;
-    }
+    const Joined x = join_partials(part, step, S.splits, nt, lane);
     const Row row = row_of<RB>(A, S, it.block, rg * 16 + n);
     if (row.head < 0) return;
     const int head = it.kv * A.gqa + row.head;
     const int64_t tok = S.q0 + row.query, to = tok * A.o_ts + (int64_t)head * A.o_hs;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
-    store_out4(dst, A.out_fp32, 16 * nt + 4 * j, o * (l == 0.f ? 0.f : 1.f / l));
-    if (A.lse && nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x.o * inverse_of(x.l));
+    if (A.lse && nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = x.l == 0.f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * 0.69314718055994530942f;
 }
 
 // ---- host side: which sequences share a launch, their blocks and ranges

@@ -1,0 +1,554 @@
+// Attention of drafted tokens (a tree of them, or any set with a mask among themselves) over a block's cache and over one another
+// (kvq_tree_attention).
+//
+// The rows of one (sequence, KV head) unit are its g query heads times the nodes.  A workgroup takes a block of rows and a range of the
+// cache's tiles.  Four wavefronts fetch a tile each, bring it to fp16 values once -- code * S + Z in one fused step, rounded to fp16,
+// which is half a step of the tensors' own type -- and leave it in LDS in operand order, from where every wavefront of the block
+// multiplies it: many rows share the work of one de-quantization, which the decode kernel, with at most 16 rows, avoids instead.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/kvq.h"
+#include "kvq_cache.h"
+#include "kvq_attention_body.h"
+#include "kvq_flash.h"
+
+namespace {
+
+using namespace kvq_flash;
+
+#define KVQ_TREE_THREADS 256
+#define KVQ_TREE_SLOT (2 * KVQ_FLASH_TILE_BYTES)  // one tile in LDS: K operands, V operands
+
+struct TreeArgs {
+    const uint8_t* arena;
+    const KvqPageDesc* table;
+    const _Float16 *q, *k, *v;
+    const uint32_t* mask;   // [sequence or 1][node][words]
+    const float* lambda;    // [n_kv_heads][128] or null
+    void* out;
+    float* part;            // [unit][block][split][16 rows of it]
+    int64_t mask_seq;       // words from one sequence's mask to the next's, 0: one for all
+    int32_t n_tokens, n_tiles, tpp;
+    uint32_t tpp_magic;
+    int32_t units, n_kv, gqa, nodes, words, rows;
+    int32_t blocks, splits;  // row blocks of a unit, ranges of tiles; beyond one range the nodes themselves are a range of their own
+    int32_t out_fp32;
+    float scale_log2;
+    uint32_t flip;
+};
+
+// Eight 16-bit values in order -> the pairs (v, v + 4) in which codes are unpacked.
+__device__ inline u32x4 paired(u32x4 w) {
+    return u32x4{__builtin_amdgcn_perm(w.z, w.x, 0x05040100u), __builtin_amdgcn_perm(w.z, w.x, 0x07060302u),
+                 __builtin_amdgcn_perm(w.w, w.y, 0x05040100u), __builtin_amdgcn_perm(w.w, w.y, 0x07060302u)};
+}
+__device__ inline uint32_t fma2(uint32_t c, uint32_t s, uint32_t z) {
+    const half2v x = __builtin_elementwise_fma(__builtin_bit_cast(half2v, c), __builtin_bit_cast(half2v, s), __builtin_bit_cast(half2v, z));
+    return __builtin_bit_cast(uint32_t, x);
+}
+// The same where the scale, being rounded, carries a value beyond the largest fp16: that is then the largest, as for every other result of
+// a rounding that leaves the range of what was stored.
+__device__ inline uint32_t fma2_clamped(uint32_t c, uint32_t s, uint32_t z) {
+    uint32_t y = fma2(c, s, z);
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+        const uint32_t inf = 0x7c00u << h;
+        if ((y & (0x7fffu << h)) == inf && (s & inf) != inf && (z & inf) != inf) y -= 1u << h;
+    }
+    return y;
+}
+// Whether the largest code of some group of a tile overflows (or its S or Z is not finite).  meta: the lane's 16 bytes of the
+// tile's metadata, of which rows 0 and 2 of 16 lanes hold scales and rows 1 and 3 the zero points that belong to them.
+__device__ inline bool overflows(u32x4 meta, int levels) {
+    const half2v top = {(_Float16)(float)levels, (_Float16)(float)levels}, zero = {(_Float16)0.f, (_Float16)0.f};
+    half2v seen = zero;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const auto r = __builtin_amdgcn_permlane16_swap(meta[e], meta[e], false, false);
+        const uint32_t s = r[0], z = r[1];
+        seen += __builtin_elementwise_fma(top, __builtin_bit_cast(half2v, s), __builtin_bit_cast(half2v, z)) * zero;
+    }
+    return __any((__builtin_bit_cast(uint32_t, seen) & 0x7fff7fffu) != 0);
+}
+__device__ inline uint32_t twice(uint32_t w, int hi) { return __builtin_amdgcn_perm(w, w, hi ? 0x03020302u : 0x01000100u); }
+
+// One tile on its way: the packed strings of a lane and its share of the metadata.
+struct Fetched {
+    uint32_t k[32], v[32];
+    u32x4 meta;
+    uint32_t bits;
+};
+
+template <int NDW>
+__device__ inline void fetch_string(const uint8_t* tile, uint32_t lane_off, uint32_t (&w)[32]) {
+#pragma unroll
+    for (int c = 0; c < NDW / 4; ++c) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(tile + lane_off + c * 1024);
+        w[4 * c] = x.x; w[4 * c + 1] = x.y; w[4 * c + 2] = x.z; w[4 * c + 3] = x.w;
+    }
+}
+template <int B>
+__device__ inline void fetch_codes(Fetched& f, const uint8_t* code, uint32_t lane_off) {
+    fetch_string<2 * B>(code, lane_off, f.k);
+    fetch_string<2 * B>(code + 512u * B, lane_off, f.v);
+}
+template <bool I16>
+__device__ inline void fetch_tile(Fetched& f, const TreeArgs& A, int unit, int tile, uint32_t lane_off) {
+    const int page = kvq_dev::div_magic(tile, A.tpp, A.tpp_magic), tip = tile - page * A.tpp;
+    const KvqPageDesc d = A.table[page];
+    const uint32_t bits = __builtin_amdgcn_readfirstlane(d.bits);
+    const uint64_t slot = (uint64_t)unit * A.tpp + tip;
+    const uint8_t* code = A.arena + (uint64_t)__builtin_amdgcn_readfirstlane(d.code_off256) * 256u + slot * (1024u * bits);
+    const uint8_t* meta = A.arena + (uint64_t)__builtin_amdgcn_readfirstlane(d.meta_off256) * 256u + slot * KVQ_META_TILE_BYTES;
+    f.bits = bits;
+    if (I16 || bits < 16) f.meta = *reinterpret_cast<const u32x4*>(meta + lane_off);
+    if (bits == 2) fetch_codes<2>(f, code, lane_off);
+    else if (bits == 4) fetch_codes<4>(f, code, lane_off);
+    else if (bits == 8) fetch_codes<8>(f, code, lane_off);
+    else fetch_codes<16>(f, code, lane_off);
+}
+
+// The values of a fetched tile into a slot of LDS, operands in (v, v + 4) pairs.  meta_lds: 1 KiB of the wavefront's own.
+template <int B, bool CLAMP>
+__device__ inline void expand_codes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    const auto value = [](uint32_t c, uint32_t s, uint32_t z) { return CLAMP ? fma2_clamped(c, s, z) : fma2(c, s, z); };
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+        const int t = 8 * (n >> 2) + 4 * sub + (n & 3);
+        const u32x2 s = *reinterpret_cast<const u32x2*>(meta_lds + t * 8), z = *reinterpret_cast<const u32x2*>(meta_lds + 256 + t * 8);
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(f.k, sub * 4 + grp));
+            const uint32_t s2 = twice(s[grp >> 1], grp & 1), z2 = twice(z[grp >> 1], grp & 1);
+            *reinterpret_cast<u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16) =
+                u32x4{value(c.x, s2, z2), value(c.y, s2, z2), value(c.z, s2, z2), value(c.w, s2, z2)};
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(meta_lds + 512 + g * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta_lds + 768 + g * 64 + j * 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(f.v, 2 * g + h));
+            *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + ((2 * g + h) * 64 + lane) * 16) =
+                u32x4{value(c.x, s.x, z.x), value(c.y, s.y, z.y), value(c.z, s.z, z.z), value(c.w, s.w, z.w)};
+        }
+    }
+}
+// Integer 16-bit tier: codes of two byte planes, whose product needs 32 bits.
+__device__ inline uint32_t value16(uint32_t hi, uint32_t lo, int byte, float s, float z) {
+    const float x = fmaf((float)(((hi >> (8 * byte)) & 255u) << 8 | ((lo >> (8 * byte)) & 255u)), s, z);
+    return (uint32_t)kvq_dev::f2h_rn(fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x);  // (as fma2_clamped)
+}
+__device__ inline void expand_planes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int t = 8 * (n >> 2) + 4 * (p >> 2) + (n & 3);
+        const u32x2 sw = *reinterpret_cast<const u32x2*>(meta_lds + t * 8), zw = *reinterpret_cast<const u32x2*>(meta_lds + 256 + t * 8);
+        const float s = mixf(sw[(p & 3) >> 1], p & 1), z = mixf(zw[(p & 3) >> 1], p & 1);
+        u32x4 w;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            w[v] = value16(f.k[2 * p], f.k[16 + 2 * p], v, s, z) | value16(f.k[2 * p + 1], f.k[17 + 2 * p], v, s, z) << 16;
+        *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = w;
+    }
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(meta_lds + 512 + (nt >> 1) * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta_lds + 768 + (nt >> 1) * 64 + j * 16);
+        u32x4 w;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            w[v] = value16(f.v[2 * nt], f.v[16 + 2 * nt], v, mixf(s[v], 0), mixf(z[v], 0)) |
+                   value16(f.v[2 * nt + 1], f.v[17 + 2 * nt], v, mixf(s[v], 1), mixf(z[v], 1)) << 16;
+        *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (nt * 64 + lane) * 16) = w;
+    }
+}
+template <bool I16>
+__device__ inline void expand_tile(const Fetched& f, uint8_t* slot, uint8_t* meta_lds, int lane) {
+    if (I16 || f.bits < 16) {
+        *reinterpret_cast<u32x4*>(meta_lds + lane * 16) = f.meta;
+        wave_lds_sync();
+    }
+    if (f.bits < 16 && overflows(f.meta, (1 << f.bits) - 1)) {
+        if (f.bits == 2) expand_codes<2, true>(f, slot, meta_lds, lane);
+        else if (f.bits == 4) expand_codes<4, true>(f, slot, meta_lds, lane);
+        else expand_codes<8, true>(f, slot, meta_lds, lane);
+    } else if (f.bits == 2) {
+        expand_codes<2, false>(f, slot, meta_lds, lane);
+    } else if (f.bits == 4) {
+        expand_codes<4, false>(f, slot, meta_lds, lane);
+    } else if (f.bits == 8) {
+        expand_codes<8, false>(f, slot, meta_lds, lane);
+    } else if constexpr (I16) {
+        expand_planes(f, slot, meta_lds, lane);
+    } else {
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+            *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = paired(u32x4{f.k[4 * p], f.k[4 * p + 1], f.k[4 * p + 2], f.k[4 * p + 3]});
+            *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (p * 64 + lane) * 16) = paired(u32x4{f.v[4 * p], f.v[4 * p + 1], f.v[4 * p + 2], f.v[4 * p + 3]});
+        }
+    }
+}
+
+// Query operands in pairs.  For the cache they are multiplied by the block's key factors (fp32 product, rounded to fp16, as for a decode
+// step); against the nodes' own keys they are what they are.
+template <int R>
+__device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    const float* lam = factors && A.lambda ? A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + 8 * j : nullptr;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + 16 * r + n;
+        const _Float16* src = A.q + ((int64_t)unit * A.rows + min(row, A.rows - 1)) * KVQ_D + 8 * j;
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            u32x4 w = *reinterpret_cast<const u32x4*>(src + 32 * grp);
+            if (lam) w = kvq_dev::scale_keys8(w, lam + 32 * grp);
+            w ^= A.flip;
+            if (row >= A.rows) w = u32x4{0, 0, 0, 0};
+            q[r][grp] = to_half8(paired(w));
+        }
+    }
+}
+
+// Scores of one tile in LDS.
+template <int R>
+__device__ inline void tile_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4], const uint8_t* slot, int lane) {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][0][sub] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16));
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r][0][sub] = mma(a, q[r][grp], s[r][0][sub]);
+        }
+    }
+}
+template <int R>
+__device__ inline void tile_products(State<R>& st, const uint32_t (&p)[R][1][4], const uint8_t* slot, int lane) {
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+        const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (nt * 64 + lane) * 16));
+#pragma unroll
+        for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
+    }
+}
+
+// What infinite and NaN values of the nodes add to a row that sees them, behind everything else: nothing takes an infinity or a NaN out of
+// a sum again, so it is added to what the same lanes have stored, a partial result or an output.  The sums before it had zeros in the
+// place of such values: a key that a row does not see must not reach it, not even as zero times infinity.
+__device__ inline void add_nonfinite(const TreeArgs& A, int unit, int row, float* part, int lane) {
+    const int j = lane >> 4, n = lane & 15, at_row = min(row, A.rows - 1);
+    const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq + (int64_t)(at_row % A.nodes) * A.words;
+    const uint16_t* const v = reinterpret_cast<const uint16_t*>(A.v) + (int64_t)unit * A.nodes * KVQ_D;
+#pragma unroll 1
+    for (int nt = 0; nt < 8; ++nt) {
+        float4v count[3] = {};  // infinities of either sign and NaNs among the nodes that the row sees
+#pragma unroll 1
+        for (int node0 = 0; node0 < A.nodes; node0 += KVQ_TILE_TOKENS) {
+            const uint32_t word = mask[node0 / KVQ_TILE_TOKENS];
+            half8 kind[3], sees;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int node = node0 + 8 * j + e;
+                const uint16_t w = node < A.nodes ? v[(int64_t)node * KVQ_D + 16 * nt + n] : (uint16_t)0;
+                kind[0][e] = w == 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+                kind[1][e] = w == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
+                kind[2][e] = (w & 0x7fffu) > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+                sees[e] = ((word >> (8 * j + e)) & 1u) ? (_Float16)1.f : (_Float16)0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 3; ++c) count[c] = mma(kind[c], sees, count[c]);
+        }
+        float4v add;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            add[i] = (count[0][i] > 0.f ? INFINITY : 0.f) + (count[1][i] > 0.f ? -INFINITY : 0.f) + (count[2][i] > 0.f ? __builtin_nanf("") : 0.f);
+        if (part) {
+            reinterpret_cast<float4v*>(part)[nt * 64 + lane] += add;
+        } else if (row < A.rows) {
+            const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D + 16 * nt + 4 * j;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (A.out_fp32) static_cast<float*>(A.out)[at + i] += add[i];
+                else static_cast<_Float16*>(A.out)[at + i] = (_Float16)((float)static_cast<_Float16*>(A.out)[at + i] + add[i]);
+            }
+        }
+    }
+}
+
+template <int R, int WM, int WT, bool I16>
+__global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const TreeArgs A) {
+    constexpr int RB = 16 * R * WM;
+    static_assert(WM * WT == 4 && WM * (WT / 2) * join_bytes<R>() <= 4 * KVQ_TREE_SLOT, "four wavefronts");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * KVQ_TREE_SLOT + 4 * KVQ_META_TILE_BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WT, wt = wave % WT;
+    const int j = lane >> 4, n = lane & 15;
+    const uint32_t lane_off = 16u * lane;
+    uint8_t* const own = lds + wave * KVQ_TREE_SLOT;
+    uint8_t* const meta_lds = lds + 4 * KVQ_TREE_SLOT + wave * KVQ_META_TILE_BYTES;
+    // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
+    const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
+    const int row0 = block * RB + wm * 16 * R;  // of this wavefront
+    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
+
+    State<R> st;
+    st.clear();
+    half8 q[R][4];
+    if (t0 < t1) {
+        load_queries<R>(q, A, unit, row0, true, lane);
+        Fetched f;
+        fetch_tile<I16>(f, A, unit, min(t0 + wave, t1 - 1), lane_off);
+        for (int t = t0; t < t1; t += 4) {
+            expand_tile<I16>(f, own, meta_lds, lane);
+            if (t + 4 < t1) fetch_tile<I16>(f, A, unit, min(t + 4 + wave, t1 - 1), lane_off);
+            if (WM > 1) __syncthreads(); else wave_lds_sync();
+#pragma unroll 1
+            for (int i = wt; i < 4; i += WT) {
+                const int tile = t + i;
+                if (tile >= t1) break;
+                const uint8_t* const slot = lds + i * KVQ_TREE_SLOT;
+                float4v s[R][1][2];
+                tile_scores<R>(s, q, slot, lane);
+                if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
+                    const int end = A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * j;
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e >= end) s[r][0][e >> 2][e & 3] = -INFINITY;
+                }
+                uint32_t p[R][1][4];
+#pragma unroll
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
+                tile_products<R>(st, p, slot, lane);
+            }
+            if (WM > 1) __syncthreads(); else wave_lds_sync();
+        }
+    }
+    // the nodes among themselves
+    bool nonfinite = false;
+    if (split == (A.splits > 1 ? A.splits : 0)) {
+        load_queries<R>(q, A, unit, row0, false, lane);
+        const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
+        const _Float16* const kn = A.k + (int64_t)unit * A.nodes * KVQ_D;
+        const _Float16* const vn = A.v + (int64_t)unit * A.nodes * KVQ_D;
+        const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+        for (int t = 0; t < tiles; t += 4) {
+            const int first = min(t + wave, tiles - 1) * KVQ_TILE_TOKENS;  // of the tile that this wavefront lays out
+            uint32_t bad = 0;
+            {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    const int node = min(first + 8 * (n >> 2) + 4 * (p >> 2) + (n & 3), A.nodes - 1);
+                    *reinterpret_cast<u32x4*>(own + (p * 64 + lane) * 16) =
+                        paired(*reinterpret_cast<const u32x4*>(kn + (int64_t)node * KVQ_D + 32 * (p & 3) + 8 * j));
+                }
+                uint8_t* const vt = own + KVQ_FLASH_TILE_BYTES;
+                const int k = (lane >> 1) & 3, chunk = (lane >> 3) * 2 + (lane & 1);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int token = 8 * (i >> 1) + 4 * (i & 1) + k;
+                    u32x4 w = *reinterpret_cast<const u32x4*>(vn + (int64_t)min(first + token, A.nodes - 1) * KVQ_D + chunk * 8);
+                    if (first + token >= A.nodes) w = u32x4{0, 0, 0, 0};
+                    *reinterpret_cast<u32x4*>(vt + v_chunk_at(token, chunk)) = w;
+                }
+                wave_lds_sync();
+                u32x4 vo[8];
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) {
+                    half8 a = read_v(vt, nt, lane);
+                    watch_nonfinite(a, bad);
+                    vo[nt] = paired(__builtin_bit_cast(u32x4, a));
+                }
+                wave_lds_sync();
+                const bool any = __any(bad != 0);
+                if (any) {  // what is not finite is added at the very end, to the rows that see it
+#pragma unroll
+                    for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w = vo[nt][e];
+                            if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
+                            if ((w & 0x7c000000u) == 0x7c000000u) w &= 0x0000ffffu;
+                            vo[nt][e] = w;
+                        }
+                }
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) *reinterpret_cast<u32x4*>(vt + (nt * 64 + lane) * 16) = vo[nt];
+                nonfinite |= any;
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int i = wt; i < 4; i += WT) {
+                const int tile = t + i;
+                if (tile >= tiles) break;
+                const uint8_t* const slot = lds + i * KVQ_TREE_SLOT;
+                float4v s[R][1][2];
+                tile_scores<R>(s, q, slot, lane);
+                uint32_t seen[R];  // which of the quarter's eight nodes the row sees
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int row = min(row0 + 16 * r + n, A.rows - 1);
+                    const int here = A.nodes - tile * KVQ_TILE_TOKENS;
+                    uint32_t w = mask[(int64_t)(row % A.nodes) * A.words + tile];
+                    if (here < KVQ_TILE_TOKENS) w &= (1u << here) - 1u;
+                    seen[r] = (w >> (8 * j)) & 255u;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!((seen[r] >> e) & 1u)) s[r][0][e >> 2][e & 3] = -INFINITY;
+                }
+                uint32_t p[R][1][4];
+#pragma unroll
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
+                tile_products<R>(st, p, slot, lane);
+            }
+            __syncthreads();
+        }
+        nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
+    }
+    if constexpr (WT > 1) join_waves<R, WM, WT>(st, lds, wm, wt, lane);
+    if (WT > 1 && wt > 0) return;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + 16 * r + n;
+        if (A.splits > 1) {
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * (RB / 16) + wm * R + r;
+            store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
+            continue;
+        }
+        const float inv = inverse_of(quarters_sum(st.l[r]));
+        if (row >= A.rows) continue;
+        const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D;
+        void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
+#pragma unroll
+        for (int nt = 0; nt < 8; ++nt) store_out4(dst, A.out_fp32, 16 * nt + 4 * j, st.o[r][nt] * inv);
+    }
+    if (nonfinite) {
+#pragma unroll 1
+        for (int r = 0; r < R; ++r) {
+            const int row = row0 + 16 * r + n;
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * (RB / 16) + wm * R + r;
+            float* const part = A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr;
+            add_nonfinite(A, unit, row, part, lane);
+        }
+    }
+}
+
+// Joins the ranges of one group of 16 rows: eight wavefronts, one for each 16 channels.
+template <int RB>
+__global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
+    const int lane = threadIdx.x & 63, nt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
+    const int rg = blockIdx.x % (RB / 16), ub = blockIdx.x / (RB / 16), block = ub % A.blocks, unit = ub / A.blocks;
+    if (block * RB + rg * 16 >= A.rows) return;
+    const float* part = A.part + ((int64_t)ub * (A.splits + 1) * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
+    const Joined x = join_partials(part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), A.splits + 1, nt, lane);
+    const int row = block * RB + rg * 16 + n;
+    if (row >= A.rows) return;
+    const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D;
+    void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
+    store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x.o * inverse_of(x.l));
+}
+
+// ---- host side
+
+struct Variant {
+    int rb;
+    void (*kernel[2])(TreeArgs);  // raw and integer 16-bit tier
+    void (*merge)(TreeArgs);
+};
+#define KVQ_TREE_VARIANT(R, WM, WT) \
+    {16 * R * WM, {kvq_tree_kernel<R, WM, WT, false>, kvq_tree_kernel<R, WM, WT, true>}, kvq_tree_merge_kernel<16 * R * WM>}
+const Variant kVariants[] = {KVQ_TREE_VARIANT(1, 1, 4), KVQ_TREE_VARIANT(2, 1, 4), KVQ_TREE_VARIANT(2, 2, 2), KVQ_TREE_VARIANT(2, 4, 1)};
+constexpr int kMostSplits = 64;
+constexpr int kLeastTiles = 8;  // of a range: two a wavefront
+
+int variant_of(int rows) { return rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3; }
+struct TreePlan {
+    int variant, blocks, splits;
+    uint64_t bytes;
+};
+// workspace: bytes there are for partial results
+TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspace) {
+    TreePlan p;
+    const int rows = c->gqa * nodes;
+    p.variant = variant_of(rows);
+    const int rb = kVariants[p.variant].rb;
+    p.blocks = (rows + rb - 1) / rb;
+    const int64_t wgs = (int64_t)c->units * p.blocks;
+    const int64_t want = std::max<int64_t>(1, 2 * c->target_workgroups / wgs);
+    const uint64_t one = (uint64_t)wgs * (rb / 16) * KVQ_PART_BYTES;  // a range's partial results
+    const int64_t room = (int64_t)std::min<uint64_t>(workspace / one, kMostSplits + 1) - 1;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(n_tiles / kLeastTiles, room)));
+    p.bytes = p.splits > 1 ? one * (uint64_t)(p.splits + 1) : 0;
+    return p;
+}
+bool nodes_ok(const kvq_cache* c, int nodes) { return c && nodes >= 1 && nodes <= KVQ_MAX_TREE_NODES; }
+
+}  // namespace
+
+extern "C" {
+
+uint64_t kvq_tree_workspace_bytes(const kvq_cache_t* c, int32_t n_nodes) {
+    if (!nodes_ok(c, n_nodes)) return 0;
+    return plan_tree(c, n_nodes, (c->cfg.max_tokens + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS, UINT64_MAX).bytes;
+}
+
+kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev, const void* k_dev, const void* v_dev, int32_t n_nodes,
+                                const uint32_t* mask_dev, int32_t mask_per_sequence, void* out_dev, int32_t out_is_fp32, float softmax_scale,
+                                void* workspace_dev, uint64_t workspace_bytes, void* hip_stream) {
+    if (!nodes_ok(c, n_nodes) || layer < 0 || layer >= c->cfg.n_layers) return KVQ_E_INVALID;
+    if (!q_dev || !k_dev || !v_dev || !mask_dev || !out_dev || !std::isfinite(softmax_scale)) return KVQ_E_INVALID;
+    for (const void* p : {q_dev, k_dev, v_dev, static_cast<const void*>(out_dev), static_cast<const void*>(workspace_dev)})
+        if (reinterpret_cast<uintptr_t>(p) & 15u) return KVQ_E_INVALID;
+    if (reinterpret_cast<uintptr_t>(mask_dev) & 3u) return KVQ_E_INVALID;
+    if (c->dry) return KVQ_E_STATE;
+    const kvq_host::Layer& L = c->layers[(size_t)layer];
+    if (L.poisoned) return KVQ_E_STATE;
+    TreeArgs A{};
+    A.n_tokens = L.T;
+    A.n_tiles = (L.T + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+    const TreePlan plan = plan_tree(c, n_nodes, A.n_tiles, workspace_dev ? workspace_bytes : 0);
+    A.arena = c->arena;
+    A.table = c->table_dev(layer);
+    A.q = static_cast<const _Float16*>(q_dev);
+    A.k = static_cast<const _Float16*>(k_dev);
+    A.v = static_cast<const _Float16*>(v_dev);
+    A.mask = mask_dev;
+    A.words = (n_nodes + 31) / 32;
+    A.mask_seq = mask_per_sequence ? (int64_t)n_nodes * A.words : 0;
+    A.lambda = L.reparam ? c->lambda_dev(layer) : nullptr;
+    A.out = out_dev;
+    A.part = static_cast<float*>(workspace_dev);
+    A.tpp = c->tpp;
+    A.tpp_magic = c->tpp > 1 ? (uint32_t)(((1ull << 32) + (uint64_t)c->tpp - 1) / (uint64_t)c->tpp) : 0u;
+    A.units = c->units;
+    A.n_kv = c->cfg.n_kv_heads;
+    A.gqa = c->gqa;
+    A.nodes = n_nodes;
+    A.rows = c->gqa * n_nodes;
+    A.blocks = plan.blocks;
+    A.splits = plan.splits;
+    A.out_fp32 = out_is_fp32 ? 1 : 0;
+    const float scale = softmax_scale != 0.f ? softmax_scale : 1.0f / std::sqrt((float)KVQ_D);
+    A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
+    A.flip = scale < 0.f ? 0x80008000u : 0u;
+    const Variant& V = kVariants[plan.variant];
+    const hipStream_t s = kvq_host::as_stream(hip_stream);
+    const unsigned row_blocks = (unsigned)(c->units * plan.blocks);
+    hipLaunchKernelGGL(V.kernel[c->int16() ? 1 : 0], dim3(row_blocks * (unsigned)(plan.splits > 1 ? plan.splits + 1 : 1)), dim3(KVQ_TREE_THREADS), 0, s, A);
+    if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
+    if (plan.splits > 1) {
+        hipLaunchKernelGGL(V.merge, dim3(row_blocks * (unsigned)(V.rb / 16)), dim3(512), 0, s, A);
+        if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
+    }
+    return KVQ_OK;
+}
+
+}  // extern "C"
