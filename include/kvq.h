@@ -266,6 +266,36 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* cache, int32_t layer, const void* q
                                 int32_t out_is_fp32, float softmax_scale, void* workspace_dev, uint64_t workspace_bytes,
                                 void* hip_stream);
 
+/* Forks a block: block `layer` of dst becomes the first n_tokens tokens (-1: all) of block `layer` of src, sequence b of dst those of
+ * sequence seq_map_dev[b] of src, bit for bit: widths, codes, scales, zero points, and in another cache the block's
+ * reparameterization factors.  What dst's block held before is gone.  Uses: beams that go on from their parents, samples of one
+ * prompt, a copy to come back to, a sequence taken out of a batch or put into one.
+ *   seq_map_dev: device, int32 [dst batch], or NULL: every sequence its own (equal batches) or all of them src's only one.  An entry
+ *   beyond src's sequences is taken as the nearest of them.
+ *   src and dst agree in n_kv_heads, page_tokens, group and 16-bit tier (else KVQ_E_INVALID; so with an accounting-only cache and one
+ *   that is not) and may differ in everything else.  dst may be src: the sequences change places inside the cache, through fresh
+ *   pages.  Pages of dst's old block are written over where the widths agree; the others are taken from the arena before anything
+ *   changes, beside the old block (KVQ_E_OOM: empty dst's block first if it need not stay).  KVQ_E_BUDGET if dst's block would
+ *   exceed its budget, KVQ_E_STATE if n_tokens exceeds what src holds or dst's max_tokens, or if fewer tokens than src holds would
+ *   end inside a page below 16 bits while dst's policy appends at 16.  On these dst is unchanged.
+ *   Enqueues kernels on the stream, which both caches' calls are issued on; not for capture. */
+kvq_status_t kvq_cache_fork(kvq_cache_t* dst, kvq_cache_t* src, int32_t layer, const int32_t* seq_map_dev, int32_t n_tokens,
+                            void* hip_stream);
+
+/* Takes the newest tokens of a block away, so that n_tokens are left (drafted tokens that were rejected, an answer to be written
+ * again): whole pages go back to the arena, the rest of the last tile is cleared on the stream.  Widths that shrinking or the window
+ * has lowered stay lowered.  KVQ_E_STATE if the block holds fewer tokens, or if it would end inside a page below 16 bits while the
+ * policy appends at 16 (OLDEST_FIRST, or a window): no token could follow.  Not for capture. */
+kvq_status_t kvq_cache_truncate(kvq_cache_t* cache, int32_t layer, int32_t n_tokens, void* hip_stream);
+
+/* Reads tokens back as values: k_out[b, h, t, :] = K_hat, v_out[b, h, t, :] = V_hat of the tokens token_begin .. token_begin +
+ * n_tokens - 1, device, [batch, n_kv_heads, n_tokens, 128], fp32 or fp16 (rounded once), 16-byte aligned: code * S + Z in
+ * fp32, or the raw value; in a block with factors keys are multiplied by them again, so that they are keys as they were appended.  For
+ * instance the prefix of a chunked prompt for kvq_prompt_attention, or what shrinking has left of a sequence.
+ * KVQ_E_STATE if the block does not hold the tokens, or on an accounting-only cache.  Enqueues one kernel, may be captured. */
+kvq_status_t kvq_cache_read(kvq_cache_t* cache, int32_t layer, int32_t token_begin, int32_t n_tokens, void* k_out_dev,
+                            void* v_out_dev, int32_t out_is_fp32, void* hip_stream);
+
 /* Bookkeeping read-out (host only): maximal runs of pages with equal width, oldest first.
  *   segs_host[cap] receives min(cap, *n) entries; n, bytes_used, n_tokens, current_bits may each be NULL.
  *   bytes_used = sum over tokens of batch * n_kv_heads * kvq_bytes_per_token_head(bits of that token). */

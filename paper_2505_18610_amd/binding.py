@@ -92,6 +92,9 @@ _SIGNATURES = {
     "kvq_tree_workspace_bytes": (C.c_uint64, [C.c_void_p, C.c_int32]),
     "kvq_tree_attention": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32,
                                      C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "kvq_cache_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]),
+    "kvq_cache_truncate": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
+    "kvq_cache_read": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "kvq_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -219,6 +222,15 @@ def kvq_prompt_attention(q, k, v, out, q_begin, k_begin=None, softmax_scale=0.0,
         raise KvqError(st, "kvq_prompt_attention")
 
 
+def kvq_cache_fork(dst, src, layer, seq_map=None, n_tokens=-1, stream=None):
+    """Block `layer` of dst takes the first n_tokens (-1: all) of src's; seq_map: int32 device tensor [dst batch], the sequence of
+    src that each of dst's continues, or None.  dst may be src."""
+    assert seq_map is None or (tuple(seq_map.shape) == (dst.cfg.batch,) and seq_map.dtype.itemsize == 4)
+    st = load_library().kvq_cache_fork(dst.handle, src.handle, layer, _ptr(seq_map), n_tokens, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_cache_fork")
+
+
 def kvq_bytes_per_token_head(bits, head_dim=128, group=32, count_metadata=1, int16_tier=0) -> int:
     return int(load_library().kvq_bytes_per_token_head(bits, head_dim, group, count_metadata, int16_tier))
 
@@ -325,6 +337,17 @@ class KvqCache:
                                                 _ptr(out), 1 if out.dtype.itemsize == 4 else 0, float(softmax_scale), _ptr(workspace),
                                                 0 if workspace is None else workspace.numel(), _stream(stream)),
                     "kvq_tree_attention")
+
+    def kvq_cache_truncate(self, layer, n_tokens, stream=None):
+        self._check(self.lib.kvq_cache_truncate(self.handle, layer, n_tokens, _stream(stream)), "kvq_cache_truncate")
+
+    def kvq_cache_read(self, layer, token_begin, k_out, v_out, stream=None):
+        """Tokens token_begin, ... into k_out, v_out: fp16 or fp32 device tensors [batch, n_kv_heads, n, 128]."""
+        c = self.cfg
+        assert k_out.shape == v_out.shape and k_out.dtype == v_out.dtype and k_out.dim() == 4
+        assert (k_out.shape[0], k_out.shape[1], k_out.shape[3]) == (c.batch, c.n_kv_heads, 128)
+        self._check(self.lib.kvq_cache_read(self.handle, layer, token_begin, k_out.shape[2], _ptr(k_out), _ptr(v_out),
+                                            1 if k_out.dtype.itemsize == 4 else 0, _stream(stream)), "kvq_cache_read")
 
     def kvq_cache_describe(self, layer):
         """Returns (segments [(token_begin, token_end, bits)], bytes_used, n_tokens, current_bits)."""
