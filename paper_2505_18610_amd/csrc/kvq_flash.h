@@ -19,6 +19,7 @@
 namespace kvq_flash {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -29,8 +30,10 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 #ifdef KVQ_NO_ARITHMETIC  // the measurement build (build.py) loads tiles and computes on none
 __device__ inline float4v mma(half8, half8, float4v c) { return c; }
+__device__ inline float4v mma16(half4, half4, float4v c) { return c; }
 #else
 __device__ inline float4v mma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline float4v mma16(half4 a, half4 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
 #endif
 __device__ inline uint32_t pack2(float a, float b) {
     const half2v h = {(_Float16)a, (_Float16)b};

@@ -2,9 +2,9 @@
 // (kvq_tree_attention).
 //
 // The rows of one (sequence, KV head) unit are its g query heads times the nodes.  A workgroup takes a block of rows and a range of the
-// cache's tiles.  Four wavefronts fetch a tile each, bring it to fp16 values once -- code * S + Z in one fused step, rounded to fp16,
-// which is half a step of the tensors' own type -- and leave it in LDS in operand order, from where every wavefront of the block
-// multiplies it: many rows share the work of one de-quantization, which the decode kernel, with at most 16 rows, avoids instead.
+// cache's tiles.  Four wavefronts fetch a tile each, unpack it once and leave it in LDS in operand order, from where every wavefront of the
+// block multiplies it: K as its codes, V as code * S + Z in one fused step, rounded to fp16.  Many rows share the work of one
+// unpacking, which the decode kernel, with at most 16 rows, avoids instead.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -19,7 +19,8 @@ namespace {
 using namespace kvq_flash;
 
 #define KVQ_TREE_THREADS 256
-#define KVQ_TREE_SLOT (2 * KVQ_FLASH_TILE_BYTES)  // one tile in LDS: K operands, V operands
+#define KVQ_TREE_V KVQ_FLASH_TILE_BYTES                 // one tile in LDS: K operands, V operands,
+#define KVQ_TREE_K_LOW (2 * KVQ_FLASH_TILE_BYTES)       // in the integer 16-bit tier the low bytes of K
 
 struct TreeArgs {
     const uint8_t* arena;
@@ -72,7 +73,6 @@ __device__ inline bool overflows(u32x4 meta, int levels) {
     }
     return __any((__builtin_bit_cast(uint32_t, seen) & 0x7fff7fffu) != 0);
 }
-__device__ inline uint32_t twice(uint32_t w, int hi) { return __builtin_amdgcn_perm(w, w, hi ? 0x03020302u : 0x01000100u); }
 
 // One tile on its way: the packed strings of a lane and its share of the metadata.
 struct Fetched {
@@ -111,50 +111,41 @@ __device__ inline void fetch_tile(Fetched& f, const TreeArgs& A, int unit, int t
 }
 
 // The values of a fetched tile into a slot of LDS, operands in (v, v + 4) pairs.  meta_lds: 1 KiB of the wavefront's own.
+// K stays codes (exact in fp16, in (v, v + 4) pairs): its scales and zero points are applied to the sums of 32 channels, in fp32.
+// (With K_hat rounded to fp16 as V_hat is, keys with channels 20 times the others moved scores by 5e-4, three times what all else does.)
 template <int B, bool CLAMP>
-__device__ inline void expand_codes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
-    const int j = lane >> 4, n = lane & 15;
+__device__ inline void expand_v(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
+    const int j = lane >> 4;
     const auto value = [](uint32_t c, uint32_t s, uint32_t z) { return CLAMP ? fma2_clamped(c, s, z) : fma2(c, s, z); };
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-        const int t = 8 * (n >> 2) + 4 * sub + (n & 3);
-        const u32x2 s = *reinterpret_cast<const u32x2*>(meta_lds + t * 8), z = *reinterpret_cast<const u32x2*>(meta_lds + 256 + t * 8);
-#pragma unroll
-        for (int grp = 0; grp < 4; ++grp) {
-            const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(f.k, sub * 4 + grp));
-            const uint32_t s2 = twice(s[grp >> 1], grp & 1), z2 = twice(z[grp >> 1], grp & 1);
-            *reinterpret_cast<u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16) =
-                u32x4{value(c.x, s2, z2), value(c.y, s2, z2), value(c.z, s2, z2), value(c.w, s2, z2)};
-        }
-    }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const u32x4 s = *reinterpret_cast<const u32x4*>(meta_lds + 512 + g * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta_lds + 768 + g * 64 + j * 16);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(f.v, 2 * g + h));
-            *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + ((2 * g + h) * 64 + lane) * 16) =
+            *reinterpret_cast<u32x4*>(slot + KVQ_TREE_V + ((2 * g + h) * 64 + lane) * 16) =
                 u32x4{value(c.x, s.x, z.x), value(c.y, s.y, z.y), value(c.z, s.z, z.z), value(c.w, s.w, z.w)};
         }
     }
 }
-// Integer 16-bit tier: codes of two byte planes, whose product needs 32 bits.
+template <int B>
+__device__ inline void expand_codes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
+#pragma unroll
+    for (int p = 0; p < 8; ++p) *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<B>(f.k, p));
+    if (overflows(f.meta, (1 << B) - 1)) expand_v<B, true>(f, slot, meta_lds, lane);
+    else expand_v<B, false>(f, slot, meta_lds, lane);
+}
+// Integer 16-bit tier: of K both byte planes as integers and as 256ths of them (both exact); of V the values, whose product needs 32 bits.
 __device__ inline uint32_t value16(uint32_t hi, uint32_t lo, int byte, float s, float z) {
     const float x = fmaf((float)(((hi >> (8 * byte)) & 255u) << 8 | ((lo >> (8 * byte)) & 255u)), s, z);
     return (uint32_t)kvq_dev::f2h_rn(fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x);  // (as fma2_clamped)
 }
 __device__ inline void expand_planes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
-    const int j = lane >> 4, n = lane & 15;
+    const int j = lane >> 4;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-        const int t = 8 * (n >> 2) + 4 * (p >> 2) + (n & 3);
-        const u32x2 sw = *reinterpret_cast<const u32x2*>(meta_lds + t * 8), zw = *reinterpret_cast<const u32x2*>(meta_lds + 256 + t * 8);
-        const float s = mixf(sw[(p & 3) >> 1], p & 1), z = mixf(zw[(p & 3) >> 1], p & 1);
-        u32x4 w;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            w[v] = value16(f.k[2 * p], f.k[16 + 2 * p], v, s, z) | value16(f.k[2 * p + 1], f.k[17 + 2 * p], v, s, z) << 16;
-        *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = w;
+        *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<8>(f.k, p));
+        *reinterpret_cast<u32x4*>(slot + KVQ_TREE_K_LOW + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece_frac(f.k + 16, p));
     }
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
@@ -164,32 +155,29 @@ __device__ inline void expand_planes(const Fetched& f, uint8_t* slot, const uint
         for (int v = 0; v < 4; ++v)
             w[v] = value16(f.v[2 * nt], f.v[16 + 2 * nt], v, mixf(s[v], 0), mixf(z[v], 0)) |
                    value16(f.v[2 * nt + 1], f.v[17 + 2 * nt], v, mixf(s[v], 1), mixf(z[v], 1)) << 16;
-        *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (nt * 64 + lane) * 16) = w;
+        *reinterpret_cast<u32x4*>(slot + KVQ_TREE_V + (nt * 64 + lane) * 16) = w;
     }
 }
+// A raw tile has scales of one and zero points of zero.
 template <bool I16>
 __device__ inline void expand_tile(const Fetched& f, uint8_t* slot, uint8_t* meta_lds, int lane) {
-    if (I16 || f.bits < 16) {
-        *reinterpret_cast<u32x4*>(meta_lds + lane * 16) = f.meta;
-        wave_lds_sync();
-    }
-    if (f.bits < 16 && overflows(f.meta, (1 << f.bits) - 1)) {
-        if (f.bits == 2) expand_codes<2, true>(f, slot, meta_lds, lane);
-        else if (f.bits == 4) expand_codes<4, true>(f, slot, meta_lds, lane);
-        else expand_codes<8, true>(f, slot, meta_lds, lane);
-    } else if (f.bits == 2) {
-        expand_codes<2, false>(f, slot, meta_lds, lane);
+    u32x4 meta = f.meta;
+    if (!I16 && f.bits == 16) meta = lane < 16 ? u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u} : u32x4{0u, 0u, 0u, 0u};
+    *reinterpret_cast<u32x4*>(meta_lds + lane * 16) = meta;
+    wave_lds_sync();
+    if (f.bits == 2) {
+        expand_codes<2>(f, slot, meta_lds, lane);
     } else if (f.bits == 4) {
-        expand_codes<4, false>(f, slot, meta_lds, lane);
+        expand_codes<4>(f, slot, meta_lds, lane);
     } else if (f.bits == 8) {
-        expand_codes<8, false>(f, slot, meta_lds, lane);
+        expand_codes<8>(f, slot, meta_lds, lane);
     } else if constexpr (I16) {
         expand_planes(f, slot, meta_lds, lane);
     } else {
 #pragma unroll
         for (int p = 0; p < 8; ++p) {
             *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = paired(u32x4{f.k[4 * p], f.k[4 * p + 1], f.k[4 * p + 2], f.k[4 * p + 3]});
-            *reinterpret_cast<u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (p * 64 + lane) * 16) = paired(u32x4{f.v[4 * p], f.v[4 * p + 1], f.v[4 * p + 2], f.v[4 * p + 3]});
+            *reinterpret_cast<u32x4*>(slot + KVQ_TREE_V + (p * 64 + lane) * 16) = paired(u32x4{f.v[4 * p], f.v[4 * p + 1], f.v[4 * p + 2], f.v[4 * p + 3]});
         }
     }
 }
@@ -214,10 +202,87 @@ __device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int uni
         }
     }
 }
-
-// Scores of one tile in LDS.
+// Sums of q over the channels of each group, for the zero points: a high part in lane quarter 0, what it leaves in quarter 1, the B operand
+// of a product with 16 channels whose A operand repeats a token's four zero points.  Queries so large that a sum passes the fp16
+// range are made smaller by 2^10, all of the wavefront's; returns what the scale grows by.
 template <int R>
-__device__ inline void tile_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4], const uint8_t* slot, int lane) {
+__device__ inline float sum_queries(half8 (&q)[R][4], half4 (&qs)[R], int lane) {
+    const int j = lane >> 4;
+    float sum[R][4];
+    bool large = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            float x = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x += (float)q[r][grp][e];
+            sum[r][grp] = quarters_sum(x);
+            large |= fabsf(sum[r][grp]) >= 65504.f;
+        }
+    float grow = 1.f;
+    if (__any(large)) {
+        grow = 1024.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int grp = 0; grp < 4; ++grp) {
+                sum[r][grp] *= 1.f / 1024.f;
+                q[r][grp] *= (_Float16)(1.f / 1024.f);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            const _Float16 high = (_Float16)sum[r][grp], low = (_Float16)(sum[r][grp] - (float)high);
+            qs[r][grp] = j == 0 ? high : j == 1 ? low : (_Float16)0.f;
+        }
+    return grow;
+}
+
+// Scores of one tile of the cache in LDS: sums of codes times queries over the 32 channels of a scale, times it, plus the zero points' part.
+template <int R, bool I16>
+__device__ inline void cache_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4], const half4 (&qs)[R], const uint8_t* slot, const uint8_t* meta,
+                                    bool planes, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    const float4v zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+        const int t = 8 * (n >> 2) + 4 * sub + (n & 3);
+        const half4 z = __builtin_bit_cast(half4, *reinterpret_cast<const u32x2*>(meta + 256 + t * 8));
+        uint32_t scale[8];  // of the quarter's four tokens of this half: two words of two groups each
+        const u32x4 a0 = *reinterpret_cast<const u32x4*>(meta + j * 64 + sub * 32), a1 = *reinterpret_cast<const u32x4*>(meta + j * 64 + sub * 32 + 16);
+        scale[0] = a0.x; scale[1] = a0.y; scale[2] = a0.z; scale[3] = a0.w;
+        scale[4] = a1.x; scale[5] = a1.y; scale[6] = a1.z; scale[7] = a1.w;
+        if (I16 && planes) {  // (times 256: the low bytes are 256ths; a scale is at most 2)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scale[e] = pk_mul(scale[e], 0x5c005c00u);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][0][sub] = mma16(z, qs[r], zero);
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16));
+            float4v part[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) part[r] = mma(a, q[r][grp], zero);
+            if (I16 && planes) {
+                const half8 b = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_TREE_K_LOW + ((sub * 4 + grp) * 64 + lane) * 16));
+#pragma unroll
+                for (int r = 0; r < R; ++r) part[r] = mma(b, q[r][grp], part[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s[r][0][sub][i] = fmaf(mixf(scale[2 * i + (grp >> 1)], grp & 1), part[r][i], s[r][0][sub][i]);
+        }
+    }
+}
+// Scores of one tile of the nodes' keys.
+template <int R>
+__device__ inline void node_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4], const uint8_t* slot, int lane) {
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
 #pragma unroll
@@ -234,7 +299,7 @@ template <int R>
 __device__ inline void tile_products(State<R>& st, const uint32_t (&p)[R][1][4], const uint8_t* slot, int lane) {
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
-        const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_FLASH_TILE_BYTES + (nt * 64 + lane) * 16));
+        const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_TREE_V + (nt * 64 + lane) * 16));
 #pragma unroll
         for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
     }
@@ -284,15 +349,16 @@ __device__ inline void add_nonfinite(const TreeArgs& A, int unit, int row, float
 }
 
 template <int R, int WM, int WT, bool I16>
-__global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const TreeArgs A) {
-    constexpr int RB = 16 * R * WM;
-    static_assert(WM * WT == 4 && WM * (WT / 2) * join_bytes<R>() <= 4 * KVQ_TREE_SLOT, "four wavefronts");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * KVQ_TREE_SLOT + 4 * KVQ_META_TILE_BYTES];
+__global__ __launch_bounds__(KVQ_TREE_THREADS, I16 ? 1 : 2) void kvq_tree_kernel(const TreeArgs A) {
+    constexpr int RB = 16 * R * WM, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
+    static_assert(WM * WT == 4 && WM * (WT / 2) * join_bytes<R>() <= 4 * SLOT, "four wavefronts");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * SLOT + 4 * KVQ_META_TILE_BYTES];
+    __shared__ uint32_t widths[4];  // of the tiles in the slots
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WT, wt = wave % WT;
     const int j = lane >> 4, n = lane & 15;
     const uint32_t lane_off = 16u * lane;
-    uint8_t* const own = lds + wave * KVQ_TREE_SLOT;
-    uint8_t* const meta_lds = lds + 4 * KVQ_TREE_SLOT + wave * KVQ_META_TILE_BYTES;
+    uint8_t* const own = lds + wave * SLOT;
+    uint8_t* const meta_lds = lds + 4 * SLOT + wave * KVQ_META_TILE_BYTES;
     // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
     const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
     const int row0 = block * RB + wm * 16 * R;  // of this wavefront
@@ -303,19 +369,22 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const Tre
     half8 q[R][4];
     if (t0 < t1) {
         load_queries<R>(q, A, unit, row0, true, lane);
+        half4 qs[R];
+        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
         Fetched f;
         fetch_tile<I16>(f, A, unit, min(t0 + wave, t1 - 1), lane_off);
         for (int t = t0; t < t1; t += 4) {
             expand_tile<I16>(f, own, meta_lds, lane);
+            if (I16 && lane == 0) widths[wave] = f.bits;
             if (t + 4 < t1) fetch_tile<I16>(f, A, unit, min(t + 4 + wave, t1 - 1), lane_off);
             if (WM > 1) __syncthreads(); else wave_lds_sync();
 #pragma unroll 1
             for (int i = wt; i < 4; i += WT) {
                 const int tile = t + i;
                 if (tile >= t1) break;
-                const uint8_t* const slot = lds + i * KVQ_TREE_SLOT;
+                const uint8_t* const slot = lds + i * SLOT;
                 float4v s[R][1][2];
-                tile_scores<R>(s, q, slot, lane);
+                cache_scores<R, I16>(s, q, qs, slot, lds + 4 * SLOT + i * KVQ_META_TILE_BYTES, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, lane);
                 if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
                     const int end = A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * j;
 #pragma unroll
@@ -326,7 +395,7 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const Tre
                 }
                 uint32_t p[R][1][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
                 tile_products<R>(st, p, slot, lane);
             }
             if (WM > 1) __syncthreads(); else wave_lds_sync();
@@ -350,7 +419,7 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const Tre
                     *reinterpret_cast<u32x4*>(own + (p * 64 + lane) * 16) =
                         paired(*reinterpret_cast<const u32x4*>(kn + (int64_t)node * KVQ_D + 32 * (p & 3) + 8 * j));
                 }
-                uint8_t* const vt = own + KVQ_FLASH_TILE_BYTES;
+                uint8_t* const vt = own + KVQ_TREE_V;
                 const int k = (lane >> 1) & 3, chunk = (lane >> 3) * 2 + (lane & 1);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -389,9 +458,9 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, 2) void kvq_tree_kernel(const Tre
             for (int i = wt; i < 4; i += WT) {
                 const int tile = t + i;
                 if (tile >= tiles) break;
-                const uint8_t* const slot = lds + i * KVQ_TREE_SLOT;
+                const uint8_t* const slot = lds + i * SLOT;
                 float4v s[R][1][2];
-                tile_scores<R>(s, q, slot, lane);
+                node_scores<R>(s, q, slot, lane);
                 uint32_t seen[R];  // which of the quarter's eight nodes the row sees
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
