@@ -239,24 +239,57 @@ __device__ inline void store_partial(const State<R>& st, int r, float* part, int
     }
 }
 
-// Joins n partial results of a group of rows, `step` floats apart: a lane's four channels of block nt of row n, and the row's statistics.
+// Joins n_parts (at most KVQ_MOST_PARTS) partial results of one group of 16 rows, `step` floats apart.  A workgroup of eight wavefronts
+// takes 32 of the 128 channels: two blocks of 16 in four slices of the parts each, so that the loads of a thread are few and all in
+// flight together; `pair` says which two blocks.  True in the wavefronts that hold the result: the lane's four channels of block nt of row n, and the
+// row's statistics.  (One wavefront a block and the parts one after the other: 20 us for 36 parts.)
+#define KVQ_MOST_PARTS 65
 struct Joined {
     float4v o;
     float m, l;
+    int nt;
 };
-__device__ inline Joined join_partials(const float* part, int64_t step, int n_parts, int nt, int lane) {
-    const int n = lane & 15;
-    float m = -INFINITY;
-    for (int s = 0; s < n_parts; ++s) m = fmaxf(m, part[s * step + KVQ_PART_O_FLOATS + 2 * n]);
-    const float ref = reference_of(m);
-    Joined x{float4v{0.f, 0.f, 0.f, 0.f}, m, 0.f};
-    for (int s = 0; s < n_parts; ++s) {
-        const float* at = part + s * step;
-        const float w = __builtin_amdgcn_exp2f(at[KVQ_PART_O_FLOATS + 2 * n] - ref);
-        x.l += w * at[KVQ_PART_O_FLOATS + 2 * n + 1];
-        x.o += *reinterpret_cast<const float4v*>(at + (nt * 64 + lane) * 4) * w;
+struct JoinLds {
+    float w[KVQ_MOST_PARTS][16];  // maxima, then weights
+    float l[KVQ_MOST_PARTS][16];
+    float4v o[6][64];
+};
+__device__ inline bool join_partials(JoinLds& lds, const float* part, int64_t step, int n_parts, int pair, Joined& x) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15;
+    const int slice = wave >> 1;
+    x.nt = 2 * pair + (wave & 1);
+    for (int i = tid; i < n_parts * 16; i += 512) {
+        const float* at = part + (i >> 4) * step + KVQ_PART_O_FLOATS + 2 * (i & 15);
+        lds.w[i >> 4][i & 15] = at[0];
+        lds.l[i >> 4][i & 15] = at[1];
     }
-    return x;
+    // the slice's first eight parts are on their way meanwhile
+    float4v o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int s = min(slice + 4 * k, n_parts - 1);
+        o[k] = *reinterpret_cast<const float4v*>(part + s * step + (x.nt * 64 + lane) * 4);
+    }
+    __syncthreads();
+    x.m = -INFINITY;
+    for (int s = 0; s < n_parts; ++s) x.m = fmaxf(x.m, lds.w[s][n]);
+    const float ref = reference_of(x.m);
+    x.o = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int s = slice + 4 * k;
+        if (s < n_parts) x.o += o[k] * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+    }
+    for (int s = slice + 32; s < n_parts; s += 4)
+        x.o += *reinterpret_cast<const float4v*>(part + s * step + (x.nt * 64 + lane) * 4) * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+    if (slice) lds.o[wave - 2][lane] = x.o;
+    __syncthreads();
+    if (slice) return false;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) x.o += lds.o[2 * k + wave][lane];
+    x.l = 0.f;
+    for (int s = 0; s < n_parts; ++s) x.l += lds.l[s][n] * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+    return true;
 }
 
 // What the sum of a row's weights divides by: a row that saw nothing gives zeros.

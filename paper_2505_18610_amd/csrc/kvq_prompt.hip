@@ -261,25 +261,26 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
     }
 }
 
-// Joins the ranges of keys of one group of 16 rows: eight wavefronts, one for each 16 channels.  RB: rows of a block.
+// Joins the ranges of keys of one group of 16 rows, 32 channels a workgroup.  RB: rows of a block.
 template <int RB>
 __global__ __launch_bounds__(512) void kvq_prompt_merge_kernel(const PromptArgs A) {
-    const int lane = threadIdx.x & 63, nt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
-    // one workgroup for each (workgroup of the first launch with range 0, group of 16 rows)
-    const int id = blockIdx.x / (RB / 16), rg = blockIdx.x % (RB / 16);
-    const Item it = item_of(A, id);
+    __shared__ JoinLds lds;
+    const int lane = threadIdx.x & 63, j = lane >> 4, n = lane & 15;
+    // for each (workgroup of the first launch with range 0, group of 16 rows)
+    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % (RB / 16);
+    const Item it = item_of(A, (blockIdx.x >> 2) / (RB / 16));
     const PromptSeq& S = A.seq[it.seq];
     if (S.splits == 1 || it.split != 0) return;
-    const int64_t step = (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4);
     const float* part = A.part + (S.part0 + (int64_t)(it.kv * S.blocks + it.block) * S.splits * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
-    const Joined x = join_partials(part, step, S.splits, nt, lane);
+    Joined x;
+    if (!join_partials(lds, part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), S.splits, pair, x)) return;
     const Row row = row_of<RB>(A, S, it.block, rg * 16 + n);
     if (row.head < 0) return;
     const int head = it.kv * A.gqa + row.head;
     const int64_t tok = S.q0 + row.query, to = tok * A.o_ts + (int64_t)head * A.o_hs;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
-    store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x.o * inverse_of(x.l));
-    if (A.lse && nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = x.l == 0.f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * 0.69314718055994530942f;
+    store_out4(dst, A.out_fp32, 16 * x.nt + 4 * j, x.o * inverse_of(x.l));
+    if (A.lse && x.nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = x.l == 0.f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * 0.69314718055994530942f;
 }
 
 // ---- host side: which sequences share a launch, their blocks and ranges
@@ -295,7 +296,7 @@ const Variant kVariants[] = {KVQ_PROMPT_VARIANT(1, 1, 4, 4), KVQ_PROMPT_VARIANT(
 constexpr int kNumVariants = 4;
 constexpr int kTargetWorkgroups = 512;  // two a compute unit
 constexpr int kLeastTiles = 8;          // of a range of keys
-constexpr int kMostSplits = 64;
+constexpr int kMostSplits = KVQ_MOST_PARTS;
 
 int variant_of(int gqa, int nq) {
     const int64_t rows = (int64_t)gqa * nq;
@@ -432,7 +433,7 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* d, const void* q_dev, cons
         hipLaunchKernelGGL(V.kernel, dim3((unsigned)wgs), dim3(KVQ_PROMPT_THREADS), 0, s, args);
         if (hipGetLastError() != hipSuccess) return false;
         if (!split) return true;
-        hipLaunchKernelGGL(V.merge, dim3((unsigned)wgs * (unsigned)(V.rb / 16)), dim3(512), 0, s, args);
+        hipLaunchKernelGGL(V.merge, dim3((unsigned)wgs * (unsigned)(V.rb / 16 * 4)), dim3(512), 0, s, args);
         return hipGetLastError() == hipSuccess;
     });
     return got == -1 ? KVQ_E_INVALID : got < 0 ? KVQ_E_HIP : KVQ_OK;

@@ -386,6 +386,7 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, I16 ? 1 : 2) void kvq_tree_kernel
                 float4v s[R][1][2];
                 cache_scores<R, I16>(s, q, qs, slot, lds + 4 * SLOT + i * KVQ_META_TILE_BYTES, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, lane);
                 if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
+                    asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
                     const int end = A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * j;
 #pragma unroll
                     for (int r = 0; r < R; ++r)
@@ -510,19 +511,21 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, I16 ? 1 : 2) void kvq_tree_kernel
     }
 }
 
-// Joins the ranges of one group of 16 rows: eight wavefronts, one for each 16 channels.
+// Joins the ranges of one group of 16 rows, 32 channels a workgroup.
 template <int RB>
 __global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
-    const int lane = threadIdx.x & 63, nt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
-    const int rg = blockIdx.x % (RB / 16), ub = blockIdx.x / (RB / 16), block = ub % A.blocks, unit = ub / A.blocks;
+    __shared__ JoinLds lds;
+    const int lane = threadIdx.x & 63, j = lane >> 4, n = lane & 15;
+    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % (RB / 16), ub = (blockIdx.x >> 2) / (RB / 16), block = ub % A.blocks, unit = ub / A.blocks;
     if (block * RB + rg * 16 >= A.rows) return;
     const float* part = A.part + ((int64_t)ub * (A.splits + 1) * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
-    const Joined x = join_partials(part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), A.splits + 1, nt, lane);
+    Joined x;
+    if (!join_partials(lds, part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), A.splits + 1, pair, x)) return;
     const int row = block * RB + rg * 16 + n;
     if (row >= A.rows) return;
     const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
-    store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x.o * inverse_of(x.l));
+    store_out4(dst, A.out_fp32, 16 * x.nt + 4 * j, x.o * inverse_of(x.l));
 }
 
 // ---- host side
@@ -535,7 +538,7 @@ struct Variant {
 #define KVQ_TREE_VARIANT(R, WM, WT) \
     {16 * R * WM, {kvq_tree_kernel<R, WM, WT, false>, kvq_tree_kernel<R, WM, WT, true>}, kvq_tree_merge_kernel<16 * R * WM>}
 const Variant kVariants[] = {KVQ_TREE_VARIANT(1, 1, 4), KVQ_TREE_VARIANT(2, 1, 4), KVQ_TREE_VARIANT(2, 2, 2), KVQ_TREE_VARIANT(2, 4, 1)};
-constexpr int kMostSplits = 64;
+constexpr int kMostSplits = KVQ_MOST_PARTS - 1;
 constexpr int kLeastTiles = 8;  // of a range: two a wavefront
 
 int variant_of(int rows) { return rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3; }
@@ -614,7 +617,7 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
     hipLaunchKernelGGL(V.kernel[c->int16() ? 1 : 0], dim3(row_blocks * (unsigned)(plan.splits > 1 ? plan.splits + 1 : 1)), dim3(KVQ_TREE_THREADS), 0, s, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (plan.splits > 1) {
-        hipLaunchKernelGGL(V.merge, dim3(row_blocks * (unsigned)(V.rb / 16)), dim3(512), 0, s, A);
+        hipLaunchKernelGGL(V.merge, dim3(row_blocks * (unsigned)(V.rb / 16 * 4)), dim3(512), 0, s, A);
         if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     }
     return KVQ_OK;
