@@ -187,35 +187,32 @@ __device__ inline void join_row(State<R>& st, int r, float m_x, float l_x, float
     st.m[r] = m_new;
 }
 
-// Bytes of LDS that join_waves needs for half of a workgroup's wavefronts.
-template <int R> constexpr int join_bytes() { return R * (8 * 64 * 16 + 2 * 64 * 4); }
-// The WT wavefronts wt = 0 .. WT - 1 that share rows (the same wm) hand their states to wt = 0, halving by halving.  lds: WM * WT / 2
-// times join_bytes<R>().  Every wavefront of the workgroup takes part.
+// Bytes of LDS that join_waves needs for each of half of a workgroup's wavefronts.
+#define KVQ_JOIN_BYTES (8 * 64 * 16 + 2 * 64 * 4)
+// The WT wavefronts wt = 0 .. WT - 1 that share rows (the same wm) hand their states to wt = 0, halving by halving, a group of rows after
+// the other.  lds: WM * WT / 2 times KVQ_JOIN_BYTES.  Every wavefront of the workgroup takes part.
 template <int R, int WM, int WT>
 __device__ inline void join_waves(State<R>& st, uint8_t* lds, int wm, int wt, int lane) {
 #pragma unroll
     for (int half = WT / 2; half >= 1; half /= 2) {
-        __syncthreads();
-        uint8_t* const at = lds + (wm * (WT / 2) + (wt % half)) * join_bytes<R>();
+        uint8_t* const at = lds + (wm * (WT / 2) + (wt % half)) * KVQ_JOIN_BYTES;
         float4v* const o = reinterpret_cast<float4v*>(at);
-        float* const ml = reinterpret_cast<float*>(at + R * 8 * 64 * 16);
-        if (wt >= half && wt < 2 * half) {
+        float* const ml = reinterpret_cast<float*>(at + 8 * 64 * 16);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < R; ++r) {
+            __syncthreads();
+            if (wt >= half && wt < 2 * half) {
 #pragma unroll
-                for (int nt = 0; nt < 8; ++nt) o[(r * 8 + nt) * 64 + lane] = st.o[r][nt];
-                ml[(r * 2) * 64 + lane] = st.m[r];
-                ml[(r * 2 + 1) * 64 + lane] = st.l[r];
+                for (int nt = 0; nt < 8; ++nt) o[nt * 64 + lane] = st.o[r][nt];
+                ml[lane] = st.m[r];
+                ml[64 + lane] = st.l[r];
             }
-        }
-        __syncthreads();
-        if (wt < half) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
+            __syncthreads();
+            if (wt < half) {
                 float a, b;
-                join_row<R>(st, r, ml[(r * 2) * 64 + lane], ml[(r * 2 + 1) * 64 + lane], a, b);
+                join_row<R>(st, r, ml[lane], ml[64 + lane], a, b);
 #pragma unroll
-                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] = st.o[r][nt] * a + o[(r * 8 + nt) * 64 + lane] * b;
+                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] = st.o[r][nt] * a + o[nt * 64 + lane] * b;
             }
         }
     }

@@ -70,7 +70,7 @@ __device__ inline Row row_of(const PromptArgs& A, const PromptSeq& S, int block,
 template <int R, int WM, int WT, int NT>
 __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) void kvq_prompt_kernel(const PromptArgs A) {
     constexpr int RB = 16 * R * WM, TT = NT / WT, STAGE = NT * 2 * KVQ_FLASH_TILE_BYTES;
-    static_assert(WM * WT == 4 && WM * (WT / 2) * join_bytes<R>() <= 2 * STAGE, "four wavefronts");
+    static_assert(WM * WT == 4 && WM * (WT / 2) * KVQ_JOIN_BYTES <= 2 * STAGE, "four wavefronts");
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];  // [2][NT]{K tile, V tile}
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WT, wt = wave % WT;
     const int j = lane >> 4, n = lane & 15;

@@ -18,7 +18,6 @@ namespace {
 
 using namespace kvq_flash;
 
-#define KVQ_TREE_THREADS 256
 #define KVQ_TREE_V KVQ_FLASH_TILE_BYTES                 // one tile in LDS: K operands, V operands,
 #define KVQ_TREE_K_LOW (2 * KVQ_FLASH_TILE_BYTES)       // in the integer 16-bit tier the low bytes of K
 
@@ -35,6 +34,8 @@ struct TreeArgs {
     uint32_t tpp_magic;
     int32_t units, n_kv, gqa, nodes, words, rows;
     int32_t blocks, splits;  // row blocks of a unit, ranges of tiles; beyond one range the nodes themselves are a range of their own
+    int32_t groups;          // of 16 rows in a block
+    int32_t wt;              // many rows: wavefronts that share rows and take an iteration's tiles in turn
     int32_t out_fp32;
     float scale_log2;
     uint32_t flip;
@@ -48,17 +49,6 @@ __device__ inline u32x4 paired(u32x4 w) {
 __device__ inline uint32_t fma2(uint32_t c, uint32_t s, uint32_t z) {
     const half2v x = __builtin_elementwise_fma(__builtin_bit_cast(half2v, c), __builtin_bit_cast(half2v, s), __builtin_bit_cast(half2v, z));
     return __builtin_bit_cast(uint32_t, x);
-}
-// The same where the scale, being rounded, carries a value beyond the largest fp16: that is then the largest, as for every other result of
-// a rounding that leaves the range of what was stored.
-__device__ inline uint32_t fma2_clamped(uint32_t c, uint32_t s, uint32_t z) {
-    uint32_t y = fma2(c, s, z);
-#pragma unroll
-    for (int h = 0; h < 32; h += 16) {
-        const uint32_t inf = 0x7c00u << h;
-        if ((y & (0x7fffu << h)) == inf && (s & inf) != inf && (z & inf) != inf) y -= 1u << h;
-    }
-    return y;
 }
 // Whether the largest code of some group of a tile overflows (or its S or Z is not finite).  meta: the lane's 16 bytes of the
 // tile's metadata, of which rows 0 and 2 of 16 lanes hold scales and rows 1 and 3 the zero points that belong to them.
@@ -74,7 +64,24 @@ __device__ inline bool overflows(u32x4 meta, int levels) {
     return __any((__builtin_bit_cast(uint32_t, seen) & 0x7fff7fffu) != 0);
 }
 
-// One tile on its way: the packed strings of a lane and its share of the metadata.
+// Behind such a tile's values: what the rounded scale has carried beyond the largest fp16 becomes the largest, as every other value stays
+// within half a step of its scale of what was stored.  to: the lane's values of V; meta: scales and zero points of V.
+__device__ inline void clamp_values(uint8_t* to, const uint8_t* meta, int lane) {
+#pragma unroll 1
+    for (int nt = 0; nt < 8; ++nt) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(meta + (nt >> 1) * 64 + (lane >> 4) * 16), z = *reinterpret_cast<const u32x4*>(meta + 256 + (nt >> 1) * 64 + (lane >> 4) * 16);
+        u32x4 y = *reinterpret_cast<const u32x4*>(to + (nt * 64 + lane) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int h = 0; h < 32; h += 16) {
+                const uint32_t inf = 0x7c00u << h;
+                if ((y[e] & (0x7fffu << h)) == inf && (s[e] & inf) != inf && (z[e] & inf) != inf) y[e] -= 1u << h;
+            }
+        *reinterpret_cast<u32x4*>(to + (nt * 64 + lane) * 16) = y;
+    }
+}
+// One tile on its way through registers: the packed strings of a lane and its share of the metadata.
 struct Fetched {
     uint32_t k[32], v[32];
     u32x4 meta;
@@ -94,10 +101,17 @@ __device__ inline void fetch_codes(Fetched& f, const uint8_t* code, uint32_t lan
     fetch_string<2 * B>(code, lane_off, f.k);
     fetch_string<2 * B>(code + 512u * B, lane_off, f.v);
 }
+// The page entry of a tile.  It is asked for an iteration ahead of its use: a trip to memory in front of the tile's own.
+// (By scalar loads: nothing writes the table while the kernel runs, and a vector load under way holds up what reuses its registers.)
+__device__ inline KvqPageDesc entry_of(const TreeArgs& A, int tile) {
+    typedef const __attribute__((address_space(4))) uint32_t* constant;
+    const constant e = reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(A.table)) +
+                       4 * __builtin_amdgcn_readfirstlane(kvq_dev::div_magic(tile, A.tpp, A.tpp_magic));
+    return KvqPageDesc{e[0], e[1], e[2], e[3]};
+}
 template <bool I16>
-__device__ inline void fetch_tile(Fetched& f, const TreeArgs& A, int unit, int tile, uint32_t lane_off) {
+__device__ inline void fetch_tile(Fetched& f, const TreeArgs& A, const KvqPageDesc& d, int unit, int tile, uint32_t lane_off) {
     const int page = kvq_dev::div_magic(tile, A.tpp, A.tpp_magic), tip = tile - page * A.tpp;
-    const KvqPageDesc d = A.table[page];
     const uint32_t bits = __builtin_amdgcn_readfirstlane(d.bits);
     const uint64_t slot = (uint64_t)unit * A.tpp + tip;
     const uint8_t* code = A.arena + (uint64_t)__builtin_amdgcn_readfirstlane(d.code_off256) * 256u + slot * (1024u * bits);
@@ -113,10 +127,9 @@ __device__ inline void fetch_tile(Fetched& f, const TreeArgs& A, int unit, int t
 // The values of a fetched tile into a slot of LDS, operands in (v, v + 4) pairs.  meta_lds: 1 KiB of the wavefront's own.
 // K stays codes (exact in fp16, in (v, v + 4) pairs): its scales and zero points are applied to the sums of 32 channels, in fp32.
 // (With K_hat rounded to fp16 as V_hat is, keys with channels 20 times the others moved scores by 5e-4, three times what all else does.)
-template <int B, bool CLAMP>
+template <int B>
 __device__ inline void expand_v(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
     const int j = lane >> 4;
-    const auto value = [](uint32_t c, uint32_t s, uint32_t z) { return CLAMP ? fma2_clamped(c, s, z) : fma2(c, s, z); };
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const u32x4 s = *reinterpret_cast<const u32x4*>(meta_lds + 512 + g * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta_lds + 768 + g * 64 + j * 16);
@@ -124,7 +137,7 @@ __device__ inline void expand_v(const Fetched& f, uint8_t* slot, const uint8_t* 
         for (int h = 0; h < 2; ++h) {
             const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(f.v, 2 * g + h));
             *reinterpret_cast<u32x4*>(slot + KVQ_TREE_V + ((2 * g + h) * 64 + lane) * 16) =
-                u32x4{value(c.x, s.x, z.x), value(c.y, s.y, z.y), value(c.z, s.z, z.z), value(c.w, s.w, z.w)};
+                u32x4{fma2(c.x, s.x, z.x), fma2(c.y, s.y, z.y), fma2(c.z, s.z, z.z), fma2(c.w, s.w, z.w)};
         }
     }
 }
@@ -132,31 +145,34 @@ template <int B>
 __device__ inline void expand_codes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<B>(f.k, p));
-    if (overflows(f.meta, (1 << B) - 1)) expand_v<B, true>(f, slot, meta_lds, lane);
-    else expand_v<B, false>(f, slot, meta_lds, lane);
+    expand_v<B>(f, slot, meta_lds, lane);
+    if (overflows(f.meta, (1 << B) - 1)) clamp_values(slot + KVQ_TREE_V, meta_lds + 512, lane);
 }
 // Integer 16-bit tier: of K both byte planes as integers and as 256ths of them (both exact); of V the values, whose product needs 32 bits.
 __device__ inline uint32_t value16(uint32_t hi, uint32_t lo, int byte, float s, float z) {
     const float x = fmaf((float)(((hi >> (8 * byte)) & 255u) << 8 | ((lo >> (8 * byte)) & 255u)), s, z);
-    return (uint32_t)kvq_dev::f2h_rn(fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x);  // (as fma2_clamped)
+    return (uint32_t)kvq_dev::f2h_rn(fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x);  // (as clamp_values)
+}
+__device__ inline void values_of_planes(const uint32_t (&v)[32], const uint8_t* meta, uint8_t* to, int lane) {  // meta: scales and zero points of V
+    const int j = lane >> 4;
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(meta + (nt >> 1) * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta + 256 + (nt >> 1) * 64 + j * 16);
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = value16(v[2 * nt], v[16 + 2 * nt], e, mixf(s[e], 0), mixf(z[e], 0)) |
+                   value16(v[2 * nt + 1], v[17 + 2 * nt], e, mixf(s[e], 1), mixf(z[e], 1)) << 16;
+        *reinterpret_cast<u32x4*>(to + (nt * 64 + lane) * 16) = w;
+    }
 }
 __device__ inline void expand_planes(const Fetched& f, uint8_t* slot, const uint8_t* meta_lds, int lane) {
-    const int j = lane >> 4;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
         *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<8>(f.k, p));
         *reinterpret_cast<u32x4*>(slot + KVQ_TREE_K_LOW + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece_frac(f.k + 16, p));
     }
-#pragma unroll
-    for (int nt = 0; nt < 8; ++nt) {
-        const u32x4 s = *reinterpret_cast<const u32x4*>(meta_lds + 512 + (nt >> 1) * 64 + j * 16), z = *reinterpret_cast<const u32x4*>(meta_lds + 768 + (nt >> 1) * 64 + j * 16);
-        u32x4 w;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            w[v] = value16(f.v[2 * nt], f.v[16 + 2 * nt], v, mixf(s[v], 0), mixf(z[v], 0)) |
-                   value16(f.v[2 * nt + 1], f.v[17 + 2 * nt], v, mixf(s[v], 1), mixf(z[v], 1)) << 16;
-        *reinterpret_cast<u32x4*>(slot + KVQ_TREE_V + (nt * 64 + lane) * 16) = w;
-    }
+    values_of_planes(f.v, meta_lds + 512, slot + KVQ_TREE_V, lane);
 }
 // A raw tile has scales of one and zero points of zero.
 template <bool I16>
@@ -249,6 +265,7 @@ __device__ inline void cache_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4
     const float4v zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
+        __builtin_amdgcn_sched_barrier(0);
         const int t = 8 * (n >> 2) + 4 * sub + (n & 3);
         const half4 z = __builtin_bit_cast(half4, *reinterpret_cast<const u32x2*>(meta + 256 + t * 8));
         uint32_t scale[8];  // of the quarter's four tokens of this half: two words of two groups each
@@ -348,148 +365,202 @@ __device__ inline void add_nonfinite(const TreeArgs& A, int unit, int row, float
     }
 }
 
-template <int R, int WM, int WT, bool I16>
-__global__ __launch_bounds__(KVQ_TREE_THREADS, I16 ? 1 : 2) void kvq_tree_kernel(const TreeArgs A) {
-    constexpr int RB = 16 * R * WM, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
-    static_assert(WM * WT == 4 && WM * (WT / 2) * join_bytes<R>() <= 4 * SLOT, "four wavefronts");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * SLOT + 4 * KVQ_META_TILE_BYTES];
-    __shared__ uint32_t widths[4];  // of the tiles in the slots
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WT, wt = wave % WT;
-    const int j = lane >> 4, n = lane & 15;
-    const uint32_t lane_off = 16u * lane;
-    uint8_t* const own = lds + wave * SLOT;
-    uint8_t* const meta_lds = lds + 4 * SLOT + wave * KVQ_META_TILE_BYTES;
-    // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
-    const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
-    const int row0 = block * RB + wm * 16 * R;  // of this wavefront
-    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
 
-    State<R> st;
-    st.clear();
-    half8 q[R][4];
-    if (t0 < t1) {
-        load_queries<R>(q, A, unit, row0, true, lane);
-        half4 qs[R];
-        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
-        Fetched f;
-        fetch_tile<I16>(f, A, unit, min(t0 + wave, t1 - 1), lane_off);
-        for (int t = t0; t < t1; t += 4) {
-            expand_tile<I16>(f, own, meta_lds, lane);
-            if (I16 && lane == 0) widths[wave] = f.bits;
-            if (t + 4 < t1) fetch_tile<I16>(f, A, unit, min(t + 4 + wave, t1 - 1), lane_off);
-            if (WM > 1) __syncthreads(); else wave_lds_sync();
-#pragma unroll 1
-            for (int i = wt; i < 4; i += WT) {
-                const int tile = t + i;
-                if (tile >= t1) break;
-                const uint8_t* const slot = lds + i * SLOT;
-                float4v s[R][1][2];
-                cache_scores<R, I16>(s, q, qs, slot, lds + 4 * SLOT + i * KVQ_META_TILE_BYTES, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, lane);
-                if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
-                    asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
-                    const int end = A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * j;
+// ---- many rows: eight wavefronts that share the unpacked tiles
+
+// One of the operands of a tile on its way to the workgroup's staging area in LDS, past the registers: the lanes' packed strings of K or of V
+// and 512 bytes of metadata (scales, zero points).  Strings of 16 bits are not staged, there is no room for them: they are
+// loaded when they are unpacked.
+#define KVQ_TREE_STAGE (KVQ_FLASH_TILE_BYTES / 2 + KVQ_META_TILE_BYTES / 2)
+#define KVQ_TREE_STAGE_META (KVQ_FLASH_TILE_BYTES / 2)
+struct Staged {
+    const uint8_t* code;  // of 16 bits: where the strings are
+    uint32_t bits;
+};
+__device__ inline void stage16(const uint8_t* from, uint8_t* to) {  // to: the wavefront's address, lane l writes 16 bytes at 16 l
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t*>(reinterpret_cast<uintptr_t>(from)),
+                                     (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+__device__ inline Staged stage_tile(const TreeArgs& A, const KvqPageDesc& d, int unit, int tile, int part, uint8_t* to, int lane) {
+    const int page = kvq_dev::div_magic(tile, A.tpp, A.tpp_magic), tip = tile - page * A.tpp;
+    const uint32_t bits = __builtin_amdgcn_readfirstlane(d.bits);
+    const uint64_t slot = (uint64_t)unit * A.tpp + tip;
+    const uint8_t* code = A.arena + (uint64_t)__builtin_amdgcn_readfirstlane(d.code_off256) * 256u + slot * (1024u * bits) + (uint32_t)part * 512u * bits;
+    const uint8_t* meta = A.arena + (uint64_t)__builtin_amdgcn_readfirstlane(d.meta_off256) * 256u + slot * KVQ_META_TILE_BYTES + part * (KVQ_META_TILE_BYTES / 2);
+    if (bits < 16)
+        for (uint32_t c = 0; c < bits / 2; ++c) stage16(code + c * 1024 + lane * 16, to + c * 1024);
+    if ((bits < 16 || __builtin_amdgcn_readfirstlane(d.int16)) && lane < 32) stage16(meta + lane * 16, to + KVQ_TREE_STAGE_META);
+    return Staged{code, bits};
+}
+// Waits for what the wavefront has under way to LDS; a barrier that does not (it orders LDS alone).
+__device__ inline void wait_staged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int NDW>
+__device__ inline void staged_string(const uint8_t* from, int lane, uint32_t (&w)[NDW]) {
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
+    for (int c = 0; c < NDW / 4; ++c) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(from + (c * 64 + lane) * 16);
+        w[4 * c] = x.x; w[4 * c + 1] = x.y; w[4 * c + 2] = x.z; w[4 * c + 3] = x.w;
+    }
+}
+template <int B>
+__device__ inline void unpack_k(const uint8_t* from, uint8_t* to, int lane) {
+    uint32_t w[2 * B];
+    staged_string<2 * B>(from, lane, w);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e >= end) s[r][0][e >> 2][e & 3] = -INFINITY;
-                }
-                uint32_t p[R][1][4];
+    for (int p = 0; p < 8; ++p) *reinterpret_cast<u32x4*>(to + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<B>(w, p));
+}
+template <int B>
+__device__ inline void unpack_v(const uint8_t* from, uint8_t* to, int lane) {
+    const uint8_t* const meta = from + KVQ_TREE_STAGE_META + (lane >> 4) * 16;
+    uint32_t w[2 * B];
+    staged_string<2 * B>(from, lane, w);
 #pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
-                tile_products<R>(st, p, slot, lane);
-            }
-            if (WM > 1) __syncthreads(); else wave_lds_sync();
+    for (int g = 0; g < 4; ++g) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(meta + g * 64), z = *reinterpret_cast<const u32x4*>(meta + 256 + g * 64);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32x4 c = __builtin_bit_cast(u32x4, dq_piece<B>(w, 2 * g + h));
+            *reinterpret_cast<u32x4*>(to + ((2 * g + h) * 64 + lane) * 16) =
+                u32x4{fma2(c.x, s.x, z.x), fma2(c.y, s.y, z.y), fma2(c.z, s.z, z.z), fma2(c.w, s.w, z.w)};
         }
     }
-    // the nodes among themselves
-    bool nonfinite = false;
-    if (split == (A.splits > 1 ? A.splits : 0)) {
-        load_queries<R>(q, A, unit, row0, false, lane);
-        const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
-        const _Float16* const kn = A.k + (int64_t)unit * A.nodes * KVQ_D;
-        const _Float16* const vn = A.v + (int64_t)unit * A.nodes * KVQ_D;
-        const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
-        for (int t = 0; t < tiles; t += 4) {
-            const int first = min(t + wave, tiles - 1) * KVQ_TILE_TOKENS;  // of the tile that this wavefront lays out
-            uint32_t bad = 0;
-            {
+}
+__device__ inline void unpack_raw(const uint8_t* from, uint8_t* to, int lane) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) {
-                    const int node = min(first + 8 * (n >> 2) + 4 * (p >> 2) + (n & 3), A.nodes - 1);
-                    *reinterpret_cast<u32x4*>(own + (p * 64 + lane) * 16) =
-                        paired(*reinterpret_cast<const u32x4*>(kn + (int64_t)node * KVQ_D + 32 * (p & 3) + 8 * j));
-                }
-                uint8_t* const vt = own + KVQ_TREE_V;
-                const int k = (lane >> 1) & 3, chunk = (lane >> 3) * 2 + (lane & 1);
+    for (int p = 0; p < 8; ++p) *reinterpret_cast<u32x4*>(to + (p * 64 + lane) * 16) = paired(*reinterpret_cast<const u32x4*>(from + (p * 64 + lane) * 16));
+}
+// A staged operand into its place in a slot (slot: K operands, V operands, and the low bytes of K in the integer 16-bit tier); meta: where
+// the scales and zero points of K go, ones and zeros for a raw tile.
+template <bool I16>
+__device__ inline void unpack_staged(const Staged& f, const uint8_t* from, uint8_t* slot, uint8_t* meta, int part, int lane) {
+    const uint32_t bits = f.bits;
+    if (part == 0) {
+        u32x4 m = *reinterpret_cast<const u32x4*>(from + KVQ_TREE_STAGE_META + (lane & 31) * 16);
+        if (!I16 && bits == 16) m = lane < 16 ? u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u} : u32x4{0u, 0u, 0u, 0u};
+        if (lane < 32) *reinterpret_cast<u32x4*>(meta + lane * 16) = m;
+        if (bits == 2) unpack_k<2>(from, slot, lane);
+        else if (bits == 4) unpack_k<4>(from, slot, lane);
+        else if (bits == 8) unpack_k<8>(from, slot, lane);
+        else if constexpr (I16) {
+            uint32_t w[32];
+            staged_string<32>(f.code, lane, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int token = 8 * (i >> 1) + 4 * (i & 1) + k;
-                    u32x4 w = *reinterpret_cast<const u32x4*>(vn + (int64_t)min(first + token, A.nodes - 1) * KVQ_D + chunk * 8);
-                    if (first + token >= A.nodes) w = u32x4{0, 0, 0, 0};
-                    *reinterpret_cast<u32x4*>(vt + v_chunk_at(token, chunk)) = w;
-                }
-                wave_lds_sync();
-                u32x4 vo[8];
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt) {
-                    half8 a = read_v(vt, nt, lane);
-                    watch_nonfinite(a, bad);
-                    vo[nt] = paired(__builtin_bit_cast(u32x4, a));
-                }
-                wave_lds_sync();
-                const bool any = __any(bad != 0);
-                if (any) {  // what is not finite is added at the very end, to the rows that see it
-#pragma unroll
-                    for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            uint32_t w = vo[nt][e];
-                            if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
-                            if ((w & 0x7c000000u) == 0x7c000000u) w &= 0x0000ffffu;
-                            vo[nt][e] = w;
-                        }
-                }
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt) *reinterpret_cast<u32x4*>(vt + (nt * 64 + lane) * 16) = vo[nt];
-                nonfinite |= any;
+            for (int p = 0; p < 8; ++p) {
+                *reinterpret_cast<u32x4*>(slot + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece<8>(w, p));
+                *reinterpret_cast<u32x4*>(slot + KVQ_TREE_K_LOW + (p * 64 + lane) * 16) = __builtin_bit_cast(u32x4, dq_piece_frac(w + 16, p));
             }
-            __syncthreads();
-#pragma unroll 1
-            for (int i = wt; i < 4; i += WT) {
-                const int tile = t + i;
-                if (tile >= tiles) break;
-                const uint8_t* const slot = lds + i * SLOT;
-                float4v s[R][1][2];
-                node_scores<R>(s, q, slot, lane);
-                uint32_t seen[R];  // which of the quarter's eight nodes the row sees
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int row = min(row0 + 16 * r + n, A.rows - 1);
-                    const int here = A.nodes - tile * KVQ_TILE_TOKENS;
-                    uint32_t w = mask[(int64_t)(row % A.nodes) * A.words + tile];
-                    if (here < KVQ_TILE_TOKENS) w &= (1u << here) - 1u;
-                    seen[r] = (w >> (8 * j)) & 255u;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!((seen[r] >> e) & 1u)) s[r][0][e >> 2][e & 3] = -INFINITY;
-                }
-                uint32_t p[R][1][4];
-#pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
-                tile_products<R>(st, p, slot, lane);
-            }
-            __syncthreads();
-        }
-        nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
+        } else unpack_raw(f.code, slot, lane);
+        return;
     }
-    if constexpr (WT > 1) join_waves<R, WM, WT>(st, lds, wm, wt, lane);
-    if (WT > 1 && wt > 0) return;
+    uint8_t* const to = slot + KVQ_TREE_V;
+    if (bits == 16) {
+        if constexpr (!I16) {
+            unpack_raw(f.code, to, lane);
+        } else {
+            uint32_t w[32];
+            staged_string<32>(f.code, lane, w);
+            values_of_planes(w, from + KVQ_TREE_STAGE_META, to, lane);
+        }
+        return;
+    }
+    if (bits == 2) unpack_v<2>(from, to, lane);
+    else if (bits == 4) unpack_v<4>(from, to, lane);
+    else unpack_v<8>(from, to, lane);
+    const u32x4 m = *reinterpret_cast<const u32x4*>(from + KVQ_TREE_STAGE_META + (lane & 31) * 16);  // (twice: rows 0 and 2 scales, 1 and 3 zero points)
+    if (overflows(m, (1 << bits) - 1)) clamp_values(to, from + KVQ_TREE_STAGE_META, lane);
+}
+
+// The nodes' own keys or values of one tile as operands in a slot (part 0: K, 1: V), infinite and NaN values as zeros; true if there were any.
+__device__ inline bool lay_out_k(const TreeArgs& A, int unit, int first, uint8_t* to, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    const _Float16* const kn = A.k + (int64_t)unit * A.nodes * KVQ_D;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int node = min(first + 8 * (n >> 2) + 4 * (p >> 2) + (n & 3), A.nodes - 1);
+        *reinterpret_cast<u32x4*>(to + (p * 64 + lane) * 16) = paired(*reinterpret_cast<const u32x4*>(kn + (int64_t)node * KVQ_D + 32 * (p & 3) + 8 * j));
+    }
+    return false;
+}
+__device__ inline bool lay_out_v(const TreeArgs& A, int unit, int first, uint8_t* to, int lane) {
+    const _Float16* const vn = A.v + (int64_t)unit * A.nodes * KVQ_D;
+    const int k = (lane >> 1) & 3, chunk = (lane >> 3) * 2 + (lane & 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int token = 8 * (i >> 1) + 4 * (i & 1) + k;
+        u32x4 w = *reinterpret_cast<const u32x4*>(vn + (int64_t)min(first + token, A.nodes - 1) * KVQ_D + chunk * 8);
+        if (first + token >= A.nodes) w = u32x4{0, 0, 0, 0};
+        *reinterpret_cast<u32x4*>(to + v_chunk_at(token, chunk)) = w;
+    }
+    wave_lds_sync();
+    uint32_t bad = 0;
+    u32x4 vo[8];
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+        const half8 a = read_v(to, nt, lane);
+        watch_nonfinite(a, bad);
+        vo[nt] = paired(__builtin_bit_cast(u32x4, a));
+    }
+    wave_lds_sync();
+    const bool any = __any(bad != 0);
+    if (any) {  // what is not finite is added at the very end, to the rows that see it
+#pragma unroll
+        for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t w = vo[nt][e];
+                if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
+                if ((w & 0x7c000000u) == 0x7c000000u) w &= 0x0000ffffu;
+                vo[nt][e] = w;
+            }
+    }
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) *reinterpret_cast<u32x4*>(to + (nt * 64 + lane) * 16) = vo[nt];
+    return any;
+}
+
+// Masks what lies behind the cache's last token.
+template <int R>
+__device__ inline void mask_end(float4v (&s)[R][1][2], int end) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= end) s[r][0][e >> 2][e & 3] = -INFINITY;
+}
+// One tile of nodes that is laid out in a slot, for a wavefront's rows.
+template <int R>
+__device__ inline void take_nodes(State<R>& st, const half8 (&q)[R][4], const TreeArgs& A, const uint32_t* mask, const uint8_t* slot, int row0, int tile,
+                                  int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    float4v s[R][1][2];
+    node_scores<R>(s, q, slot, lane);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = row0 + 16 * r + n;
+        const int row = min(row0 + 16 * r + n, A.rows - 1);
+        const int here = A.nodes - tile * KVQ_TILE_TOKENS;
+        uint32_t w = mask[(int64_t)(row % A.nodes) * A.words + tile];
+        if (here < KVQ_TILE_TOKENS) w &= (1u << here) - 1u;
+        w >>= 8 * j;  // the quarter's eight nodes
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!((w >> e) & 1u)) s[r][0][e >> 2][e & 3] = -INFINITY;
+    }
+    uint32_t p[R][1][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
+    tile_products<R>(st, p, slot, lane);
+}
+// A wavefront's results: partial ones beyond one range, else the output.
+template <int R>
+__device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int unit, int block, int split, int group0, bool nonfinite, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = (block * A.groups + group0 + r) * 16 + n;
         if (A.splits > 1) {
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * (RB / 16) + wm * R + r;
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * A.groups + group0 + r;
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
             continue;
         }
@@ -503,25 +574,173 @@ __global__ __launch_bounds__(KVQ_TREE_THREADS, I16 ? 1 : 2) void kvq_tree_kernel
     if (nonfinite) {
 #pragma unroll 1
         for (int r = 0; r < R; ++r) {
-            const int row = row0 + 16 * r + n;
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * (RB / 16) + wm * R + r;
-            float* const part = A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr;
-            add_nonfinite(A, unit, row, part, lane);
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * A.groups + group0 + r;
+            add_nonfinite(A, unit, (block * A.groups + group0 + r) * 16 + n, A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
         }
     }
 }
 
+// Many rows: 16 R for each of four wavefronts or, wt == 2, for each of two pairs.  An iteration unpacks two tiles, K and V of each in a
+// wavefront of its own, while the next ones are on their way into the staging area.  Three workgroups fit a compute unit, a wavefront of
+// each on every SIMD, so that one computes where another unpacks or waits at its barrier.
+template <int R, bool I16>
+__global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const TreeArgs A) {
+    constexpr int NT = 2, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
+    static_assert(2 * KVQ_JOIN_BYTES <= NT * SLOT, "two pairs of wavefronts");
+    // (the staging area is an object of its own: reads of the others then do not wait for what is on its way into it)
+    __shared__ __attribute__((aligned(16))) uint8_t lds[NT * SLOT + NT * 512];
+    __shared__ __attribute__((aligned(16))) uint8_t staging[2 * NT * KVQ_TREE_STAGE];
+    __shared__ uint32_t widths[NT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int WT = A.wt, wm = WT == 2 ? wave >> 1 : wave, wt = WT == 2 ? wave & 1 : 0;
+    const int part = wave & 1, own = wave >> 1;  // what this wavefront unpacks
+    uint8_t* const slot = lds + own * SLOT;
+    uint8_t* const stage = staging + wave * KVQ_TREE_STAGE;
+    uint8_t* const meta = lds + NT * SLOT;
+    // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
+    const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
+    const int row0 = (block * A.groups + wm * R) * 16;  // of this wavefront
+    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
+    State<R> st;
+    st.clear();
+    half8 q[R][4];
+    if (t0 < t1) {
+        Staged f = stage_tile(A, entry_of(A, min(t0 + own, t1 - 1)), unit, min(t0 + own, t1 - 1), part, stage, lane);
+        KvqPageDesc next = entry_of(A, min(t0 + NT + own, t1 - 1));
+        load_queries<R>(q, A, unit, row0, true, lane);
+        half4 qs[R];
+        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
+        for (int t = t0; t < t1; t += NT) {
+            wait_staged();
+            int l = lane;  // (addresses derived from it are not to be kept over the loop: there are no registers for them)
+            asm volatile("" : "+v"(l));
+            unpack_staged<I16>(f, stage, slot, meta + own * 512, part, l);
+            if (I16 && part == 0 && lane == 0) widths[own] = f.bits;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the staging area has been read
+            if (t + NT < t1) {
+                f = stage_tile(A, next, unit, min(t + NT + own, t1 - 1), part, stage, lane);
+                next = entry_of(A, min(t + 2 * NT + own, t1 - 1));
+            }
+            lds_barrier();
+#pragma unroll 1
+            for (int i = wt; i < NT; i += WT) {
+                const int tile = t + i;
+                if (tile >= t1) break;
+                int l = lane;
+                asm volatile("" : "+v"(l));
+                float4v s[R][1][2];
+                cache_scores<R, I16>(s, q, qs, lds + i * SLOT, meta + i * 512, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, l);
+                if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
+                    asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
+                    mask_end<R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
+                }
+                uint32_t p[R][1][4];
+#pragma unroll
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
+                tile_products<R>(st, p, lds + i * SLOT, l);
+            }
+            lds_barrier();
+        }
+    }
+    // the nodes among themselves
+    bool nonfinite = false;
+    if (split == (A.splits > 1 ? A.splits : 0)) {
+        const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
+        const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+        for (int t = 0; t < tiles; t += NT) {
+            if (t + own < tiles)
+                nonfinite |= part == 0 ? lay_out_k(A, unit, (t + own) * KVQ_TILE_TOKENS, slot, lane)
+                                       : lay_out_v(A, unit, (t + own) * KVQ_TILE_TOKENS, slot + KVQ_TREE_V, lane);
+            __syncthreads();
+            load_queries<R>(q, A, unit, row0, false, lane);  // (here, where they do not take registers from the lines above)
+#pragma unroll 1
+            for (int i = wt; i < NT && t + i < tiles; i += WT) take_nodes<R>(st, q, A, mask, lds + i * SLOT, row0, t + i, lane);
+            __syncthreads();
+        }
+        nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
+    }
+    if (WT == 2) {
+        join_waves<R, 2, 2>(st, lds, wm, wt, lane);
+        if (wt > 0) return;
+    }
+    store_rows<R>(st, A, unit, block, split, wm * R, nonfinite, lane);
+}
+
+// Few rows, 16 R: four wavefronts that all have them and take a tile each, unpacked for themselves alone.
+template <int R, bool I16>
+__global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeArgs A) {
+    constexpr int SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
+    static_assert(2 * KVQ_JOIN_BYTES <= 4 * SLOT, "four wavefronts");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * SLOT + 4 * KVQ_META_TILE_BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane_off = 16u * lane;
+    uint8_t* const slot = lds + wave * SLOT;
+    uint8_t* const meta_lds = lds + 4 * SLOT + wave * KVQ_META_TILE_BYTES;
+    const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
+    const int row0 = block * A.groups * 16;
+    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
+    State<R> st;
+    st.clear();
+    half8 q[R][4];
+    if (t0 + wave < t1) {
+        Fetched f;
+        fetch_tile<I16>(f, A, entry_of(A, t0 + wave), unit, t0 + wave, lane_off);
+        KvqPageDesc next = entry_of(A, min(t0 + wave + 4, t1 - 1));
+        load_queries<R>(q, A, unit, row0, true, lane);
+        half4 qs[R];
+        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
+        for (int tile = t0 + wave; tile < t1; tile += 4) {
+            expand_tile<I16>(f, slot, meta_lds, lane);
+            const bool planes = I16 && f.bits == 16;
+            if (tile + 4 < t1) {
+                fetch_tile<I16>(f, A, next, unit, tile + 4, lane_off);
+                next = entry_of(A, min(tile + 8, t1 - 1));
+            }
+            wave_lds_sync();
+            float4v s[R][1][2];
+            cache_scores<R, I16>(s, q, qs, slot, meta_lds, planes, lane);
+            if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
+                asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
+                mask_end<R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
+            }
+            uint32_t p[R][1][4];
+#pragma unroll
+            for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
+            tile_products<R>(st, p, slot, lane);
+            wave_lds_sync();
+        }
+    }
+    // the nodes among themselves
+    bool nonfinite = false;
+    if (split == (A.splits > 1 ? A.splits : 0)) {
+        load_queries<R>(q, A, unit, row0, false, lane);
+        const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
+        const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+        for (int t = wave; t < tiles; t += 4) {
+            lay_out_k(A, unit, t * KVQ_TILE_TOKENS, slot, lane);
+            nonfinite |= lay_out_v(A, unit, t * KVQ_TILE_TOKENS, slot + KVQ_TREE_V, lane);
+            wave_lds_sync();
+            take_nodes<R>(st, q, A, mask, slot, row0, t, lane);
+            wave_lds_sync();
+        }
+        nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
+    }
+    join_waves<R, 1, 4>(st, lds, 0, wave, lane);
+    if (wave > 0) return;
+    store_rows<R>(st, A, unit, block, split, 0, nonfinite, lane);
+}
+
 // Joins the ranges of one group of 16 rows, 32 channels a workgroup.
-template <int RB>
 __global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
     __shared__ JoinLds lds;
     const int lane = threadIdx.x & 63, j = lane >> 4, n = lane & 15;
-    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % (RB / 16), ub = (blockIdx.x >> 2) / (RB / 16), block = ub % A.blocks, unit = ub / A.blocks;
-    if (block * RB + rg * 16 >= A.rows) return;
-    const float* part = A.part + ((int64_t)ub * (A.splits + 1) * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
+    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % A.groups, ub = (blockIdx.x >> 2) / A.groups, block = ub % A.blocks, unit = ub / A.blocks;
+    const int row0 = (block * A.groups + rg) * 16;
+    if (row0 >= A.rows) return;
+    const float* part = A.part + ((int64_t)ub * (A.splits + 1) * A.groups + rg) * (KVQ_PART_BYTES / 4);
     Joined x;
-    if (!join_partials(lds, part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), A.splits + 1, pair, x)) return;
-    const int row = block * RB + rg * 16 + n;
+    if (!join_partials(lds, part, (int64_t)A.groups * (KVQ_PART_BYTES / 4), A.splits + 1, pair, x)) return;
+    const int row = row0 + n;
     if (row >= A.rows) return;
     const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
@@ -530,32 +749,29 @@ __global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
 
 // ---- host side
 
-struct Variant {
-    int rb;
-    void (*kernel[2])(TreeArgs);  // raw and integer 16-bit tier
-    void (*merge)(TreeArgs);
-};
-#define KVQ_TREE_VARIANT(R, WM, WT) \
-    {16 * R * WM, {kvq_tree_kernel<R, WM, WT, false>, kvq_tree_kernel<R, WM, WT, true>}, kvq_tree_merge_kernel<16 * R * WM>}
-const Variant kVariants[] = {KVQ_TREE_VARIANT(1, 1, 4), KVQ_TREE_VARIANT(2, 1, 4), KVQ_TREE_VARIANT(2, 2, 2), KVQ_TREE_VARIANT(2, 4, 1)};
 constexpr int kMostSplits = KVQ_MOST_PARTS - 1;
-constexpr int kLeastTiles = 8;  // of a range: two a wavefront
-
-int variant_of(int rows) { return rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3; }
+constexpr int kLeastTiles = 8;  // of a range: two a wavefront of the kernel for few rows
 struct TreePlan {
-    int variant, blocks, splits;
+    bool many;
+    int groups, wt, blocks, splits;  // groups of 16 rows in a block
     uint64_t bytes;
 };
 // workspace: bytes there are for partial results
 TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspace) {
     TreePlan p;
     const int rows = c->gqa * nodes;
-    p.variant = variant_of(rows);
-    const int rb = kVariants[p.variant].rb;
-    p.blocks = (rows + rb - 1) / rb;
+    p.many = rows > 32;
+    if (p.many) {
+        p.wt = rows <= 64 ? 2 : 1;
+        p.groups = 8 / p.wt;
+        p.blocks = (rows + 16 * p.groups - 1) / (16 * p.groups);
+    } else {
+        p.groups = rows <= 16 ? 1 : 2;
+        p.blocks = p.wt = 1;
+    }
     const int64_t wgs = (int64_t)c->units * p.blocks;
-    const int64_t want = std::max<int64_t>(1, 2 * c->target_workgroups / wgs);
-    const uint64_t one = (uint64_t)wgs * (rb / 16) * KVQ_PART_BYTES;  // a range's partial results
+    const int64_t want = std::max<int64_t>(1, (p.many && !c->int16() ? 3 : 2) * c->target_workgroups / wgs);
+    const uint64_t one = (uint64_t)wgs * p.groups * KVQ_PART_BYTES;  // a range's partial results
     const int64_t room = (int64_t)std::min<uint64_t>(workspace / one, kMostSplits + 1) - 1;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(n_tiles / kLeastTiles, room)));
     p.bytes = p.splits > 1 ? one * (uint64_t)(p.splits + 1) : 0;
@@ -611,13 +827,17 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
     const float scale = softmax_scale != 0.f ? softmax_scale : 1.0f / std::sqrt((float)KVQ_D);
     A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
     A.flip = scale < 0.f ? 0x80008000u : 0u;
-    const Variant& V = kVariants[plan.variant];
+    A.groups = plan.groups;
+    A.wt = plan.wt;
+    void (*const kernels[2][2][2])(TreeArgs) = {{{kvq_tree_kernel<1, false>, kvq_tree_kernel<1, true>}, {kvq_tree_kernel<2, false>, kvq_tree_kernel<2, true>}},
+                                                {{}, {kvq_tree_shared_kernel<2, false>, kvq_tree_shared_kernel<2, true>}}};
     const hipStream_t s = kvq_host::as_stream(hip_stream);
     const unsigned row_blocks = (unsigned)(c->units * plan.blocks);
-    hipLaunchKernelGGL(V.kernel[c->int16() ? 1 : 0], dim3(row_blocks * (unsigned)(plan.splits > 1 ? plan.splits + 1 : 1)), dim3(KVQ_TREE_THREADS), 0, s, A);
+    hipLaunchKernelGGL(kernels[plan.many][plan.groups > 1][c->int16()], dim3(row_blocks * (unsigned)(plan.splits > 1 ? plan.splits + 1 : 1)),
+                       dim3(256), 0, s, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (plan.splits > 1) {
-        hipLaunchKernelGGL(V.merge, dim3(row_blocks * (unsigned)(V.rb / 16 * 4)), dim3(512), 0, s, A);
+        hipLaunchKernelGGL(kvq_tree_merge_kernel, dim3(row_blocks * (unsigned)plan.groups * 4), dim3(512), 0, s, A);
         if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     }
     return KVQ_OK;
