@@ -7,9 +7,10 @@
 // after exponentiation are the B operand of the second product as they stand: nothing crosses lanes between the products.  A
 // wavefront carries R groups of 16 rows, so an operand read from LDS serves R products.
 //
-// Statistics: the maximum is kept per row in log2 units, the sum in 32 bits from the unrounded probabilities.  Probabilities are
-// rounded to fp16 for the second product (relative to the running maximum: at most 2^-12 of the largest weight).  The accumulators are
-// rescaled only when some row's maximum moves.
+// Statistics, in 32 bits: a reference per row in log2 units, which follows the row's maximum when that is more than 2^8 above it (a
+// rescaling of the accumulators then; with every new maximum 38 % of the tiles of 128 had one, 20 instructions a tile and group of
+// rows), and the sum of the probabilities as rounded to fp16 for the second product, so that a row that one key dominates gets its
+// values back as they are.  Where the caller asks for the log of the sum it is taken from the unrounded ones beside it.
 #ifndef KVQ_FLASH_H
 #define KVQ_FLASH_H
 
@@ -56,13 +57,14 @@ __device__ inline float quarters_sum(float x) {
 template <int R>
 struct State {
     float4v o[R][8];  // o[r][nt][i]: channel 16 nt + 4 j + i of row n of group r
-    float m[R];       // running maximum (log2 units), equal in the four quarters
+    float m[R];       // the reference (log2 units), equal in the four quarters
     float l[R];       // this quarter's share of the sum
+    float fine[R];    // the same of the unrounded probabilities
     __device__ void clear() {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             m[r] = -INFINITY;
-            l[r] = 0.f;
+            l[r] = fine[r] = 0.f;
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) o[r][nt] = float4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -73,9 +75,9 @@ struct State {
 __device__ inline float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // Probabilities of TT tiles for row group r from raw scores s (before the scale), masked ones at -inf; p in the order of the V
-// operand: natural, or (v, v + 4) pairs of a quarter's eight tokens.
-template <int R, int TT, bool PAIRED>
-__device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT][2], float scale_log2, uint32_t (&p)[TT][4]) {
+// operand: natural, or (v, v + 4) pairs of a quarter's eight tokens.  FINE: whether `fine` may be asked for.
+template <int R, int TT, bool PAIRED, bool FINE>
+__device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT][2], float scale_log2, bool fine, uint32_t (&p)[TT][4]) {
     float lmax = -INFINITY;
 #pragma unroll
     for (int t = 0; t < TT; ++t)
@@ -84,25 +86,30 @@ __device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT]
 #pragma unroll
             for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, s[t][sub][i]);
     lmax *= scale_log2;
-    if (__any(lmax > st.m[r])) {
+    if (__any(lmax > st.m[r] + 8.f)) {
         const float m_new = fmaxf(st.m[r], quarters_max(lmax));
         const float alpha = __builtin_amdgcn_exp2f(st.m[r] - reference_of(m_new));  // 0 for the first scores
         st.l[r] *= alpha;
+        if (FINE) st.fine[r] *= alpha;
 #pragma unroll
         for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= alpha;
         st.m[r] = m_new;
     }
     const float ref = reference_of(st.m[r]);
+    const half2v ones = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
         float e[2][4];
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[sub][i] = __builtin_amdgcn_exp2f(fmaf(s[t][sub][i], scale_log2, -ref));
-                st.l[r] += e[sub][i];
-            }
+            for (int i = 0; i < 4; ++i) e[sub][i] = __builtin_amdgcn_exp2f(fmaf(s[t][sub][i], scale_log2, -ref));
+        if (FINE && fine) {
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.fine[r] += e[sub][i];
+        }
         if constexpr (PAIRED) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) p[t][v] = pack2(e[0][v], e[1][v]);
@@ -111,6 +118,11 @@ __device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT]
             p[t][1] = pack2(e[0][2], e[0][3]);
             p[t][2] = pack2(e[1][0], e[1][1]);
             p[t][3] = pack2(e[1][2], e[1][3]);
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const uint32_t two = p[t][v];
+            st.l[r] = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), ones, st.l[r], false);
         }
     }
 }
@@ -179,16 +191,17 @@ __device__ inline float4v mfma_nonfinite(half8 v, half8 p, half8 seen, float4v o
 
 // Joins the states of two wavefronts that saw different tokens of the same rows: x of the other one.
 template <int R>
-__device__ inline void join_row(State<R>& st, int r, float m_x, float l_x, float& w_mine, float& w_x) {
+__device__ inline void join_row(State<R>& st, int r, float m_x, float l_x, float fine_x, float& w_mine, float& w_x) {
     const float m_new = fmaxf(st.m[r], m_x), ref = reference_of(m_new);
     w_mine = __builtin_amdgcn_exp2f(st.m[r] - ref);
     w_x = __builtin_amdgcn_exp2f(m_x - ref);
     st.l[r] = st.l[r] * w_mine + l_x * w_x;
+    st.fine[r] = st.fine[r] * w_mine + fine_x * w_x;
     st.m[r] = m_new;
 }
 
 // Bytes of LDS that join_waves needs for each of half of a workgroup's wavefronts.
-#define KVQ_JOIN_BYTES (8 * 64 * 16 + 2 * 64 * 4)
+#define KVQ_JOIN_BYTES (8 * 64 * 16 + 3 * 64 * 4)
 // The WT wavefronts wt = 0 .. WT - 1 that share rows (the same wm) hand their states to wt = 0, halving by halving, a group of rows after
 // the other.  lds: WM * WT / 2 times KVQ_JOIN_BYTES.  Every wavefront of the workgroup takes part.
 template <int R, int WM, int WT>
@@ -206,11 +219,12 @@ __device__ inline void join_waves(State<R>& st, uint8_t* lds, int wm, int wt, in
                 for (int nt = 0; nt < 8; ++nt) o[nt * 64 + lane] = st.o[r][nt];
                 ml[lane] = st.m[r];
                 ml[64 + lane] = st.l[r];
+                ml[128 + lane] = st.fine[r];
             }
             __syncthreads();
             if (wt < half) {
                 float a, b;
-                join_row<R>(st, r, ml[lane], ml[64 + lane], a, b);
+                join_row<R>(st, r, ml[lane], ml[64 + lane], ml[128 + lane], a, b);
 #pragma unroll
                 for (int nt = 0; nt < 8; ++nt) st.o[r][nt] = st.o[r][nt] * a + o[nt * 64 + lane] * b;
             }
@@ -219,9 +233,9 @@ __device__ inline void join_waves(State<R>& st, uint8_t* lds, int wm, int wt, in
 }
 
 // Partial results of one group of 16 rows and one split, 32 bits, as the lanes hold them: 8 KiB of un-normalised outputs
-// [nt][lane][4] and the pairs (maximum, sum) of the 16 rows.
+// [nt][lane][4] and of each of the 16 rows the reference, the sum and the sum of the unrounded probabilities.
 #define KVQ_PART_O_FLOATS (8 * 64 * 4)
-#define KVQ_PART_ML_FLOATS 32
+#define KVQ_PART_ML_FLOATS 64
 #define KVQ_PART_BYTES ((KVQ_PART_O_FLOATS + KVQ_PART_ML_FLOATS) * 4)
 
 template <int R>
@@ -229,11 +243,8 @@ __device__ inline void store_partial(const State<R>& st, int r, float* part, int
     float4v* const o = reinterpret_cast<float4v*>(part);
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) o[nt * 64 + lane] = st.o[r][nt];
-    const float l = quarters_sum(st.l[r]);
-    if (lane < 16) {
-        part[KVQ_PART_O_FLOATS + 2 * lane] = st.m[r];
-        part[KVQ_PART_O_FLOATS + 2 * lane + 1] = l;
-    }
+    const float l = quarters_sum(st.l[r]), fine = quarters_sum(st.fine[r]);
+    if (lane < 16) reinterpret_cast<float4v*>(part + KVQ_PART_O_FLOATS)[lane] = float4v{st.m[r], l, fine, 0.f};
 }
 
 // Joins n_parts (at most KVQ_MOST_PARTS) partial results of one group of 16 rows, `step` floats apart.  A workgroup of eight wavefronts
@@ -243,12 +254,12 @@ __device__ inline void store_partial(const State<R>& st, int r, float* part, int
 #define KVQ_MOST_PARTS 65
 struct Joined {
     float4v o;
-    float m, l;
+    float m, l, fine;
     int nt;
 };
 struct JoinLds {
-    float w[KVQ_MOST_PARTS][16];  // maxima, then weights
-    float l[KVQ_MOST_PARTS][16];
+    float w[KVQ_MOST_PARTS][16];  // references
+    float l[KVQ_MOST_PARTS][16], fine[KVQ_MOST_PARTS][16];
     float4v o[6][64];
 };
 __device__ inline bool join_partials(JoinLds& lds, const float* part, int64_t step, int n_parts, int pair, Joined& x) {
@@ -256,9 +267,10 @@ __device__ inline bool join_partials(JoinLds& lds, const float* part, int64_t st
     const int slice = wave >> 1;
     x.nt = 2 * pair + (wave & 1);
     for (int i = tid; i < n_parts * 16; i += 512) {
-        const float* at = part + (i >> 4) * step + KVQ_PART_O_FLOATS + 2 * (i & 15);
+        const float4v at = reinterpret_cast<const float4v*>(part + (i >> 4) * step + KVQ_PART_O_FLOATS)[i & 15];
         lds.w[i >> 4][i & 15] = at[0];
         lds.l[i >> 4][i & 15] = at[1];
+        lds.fine[i >> 4][i & 15] = at[2];
     }
     // the slice's first eight parts are on their way meanwhile
     float4v o[8];
@@ -284,8 +296,12 @@ __device__ inline bool join_partials(JoinLds& lds, const float* part, int64_t st
     if (slice) return false;
 #pragma unroll
     for (int k = 0; k < 3; ++k) x.o += lds.o[2 * k + wave][lane];
-    x.l = 0.f;
-    for (int s = 0; s < n_parts; ++s) x.l += lds.l[s][n] * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+    x.l = x.fine = 0.f;
+    for (int s = 0; s < n_parts; ++s) {
+        const float w = __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+        x.l += lds.l[s][n] * w;
+        x.fine += lds.fine[s][n] * w;
+    }
     return true;
 }
 

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                 }
                 uint32_t p[R][TT][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, TT, false>(st, r, s[r], A.scale_log2, p[r]);
+                for (int r = 0; r < R; ++r) softmax_group<R, TT, false, true>(st, r, s[r], A.scale_log2, A.lse != nullptr, p[r]);
 #pragma unroll
                 for (int x = 0; x < TT; ++x)
 #pragma unroll
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
             continue;
         }
-        const float l = quarters_sum(st.l[r]);
+        const float l = quarters_sum(st.l[r]), fine = quarters_sum(st.fine[r]);
         const Row row = row_of<RB>(A, S, it.block, wm * 16 * R + 16 * r + n);
         if (row.head < 0) continue;
         const float inv = inverse_of(l);
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + at) : static_cast<void*>(static_cast<_Float16*>(A.out) + at);
 #pragma unroll
         for (int nt = 0; nt < 8; ++nt) store_out4(dst, A.out_fp32, 16 * nt + 4 * j, st.o[r][nt] * inv);
-        if (A.lse && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = l == 0.f ? -INFINITY : (st.m[r] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+        if (A.lse && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = fine == 0.f ? -INFINITY : (st.m[r] + __builtin_amdgcn_logf(fine)) * 0.69314718055994530942f;
     }
 }
 
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(512) void kvq_prompt_merge_kernel(const PromptArgs 
     const int64_t tok = S.q0 + row.query, to = tok * A.o_ts + (int64_t)head * A.o_hs;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
     store_out4(dst, A.out_fp32, 16 * x.nt + 4 * j, x.o * inverse_of(x.l));
-    if (A.lse && x.nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = x.l == 0.f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * 0.69314718055994530942f;
+    if (A.lse && x.nt == 0 && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = x.fine == 0.f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.fine)) * 0.69314718055994530942f;
 }
 
 // ---- host side: which sequences share a launch, their blocks and ranges

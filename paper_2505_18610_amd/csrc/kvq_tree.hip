@@ -549,7 +549,7 @@ __device__ inline void take_nodes(State<R>& st, const half8 (&q)[R][4], const Tr
     }
     uint32_t p[R][1][4];
 #pragma unroll
-    for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], A.scale_log2, p[r]);
+    for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], A.scale_log2, false, p[r]);
     tile_products<R>(st, p, slot, lane);
 }
 // A wavefront's results: partial ones beyond one range, else the output.
@@ -636,7 +636,7 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
                 }
                 uint32_t p[R][1][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
                 tile_products<R>(st, p, lds + i * SLOT, l);
             }
             lds_barrier();
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
             }
             uint32_t p[R][1][4];
 #pragma unroll
-            for (int r = 0; r < R; ++r) softmax_group<R, 1, true>(st, r, s[r], scale_log2, p[r]);
+            for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
             tile_products<R>(st, p, slot, lane);
             wave_lds_sync();
         }
