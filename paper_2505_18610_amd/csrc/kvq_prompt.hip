@@ -19,9 +19,10 @@ using namespace kvq_flash;
 struct PromptSeq {
     int32_t q0, nq, k0, nk;  // first row and rows of queries, of keys
     int32_t item0;           // first workgroup
-    int32_t blocks, splits;  // row blocks of a KV head, ranges of keys of a row block
+    int32_t blocks;          // row blocks of a KV head, those with the most keys first
+    int32_t whole, splits;   // the first `whole` of them are taken whole, the others in so many ranges of keys
     int32_t flat;            // 1: the rows of all heads of a group follow one another; 0: every head has blocks of its own
-    int32_t part0;           // first group of 16 rows in the workspace (splits > 1)
+    int32_t part0, merge0;   // of the blocks in ranges: first group of 16 rows in the workspace, first block that the second kernel joins
 };
 struct PromptArgs {
     const _Float16 *q, *k, *v;
@@ -37,18 +38,24 @@ struct PromptArgs {
 static_assert(sizeof(PromptArgs) <= 4096 - 64, "kernel arguments end at 4 KiB");
 
 // Which workgroup does what: items of a sequence run through its KV heads first (neighbouring workgroups go to different XCDs, so the
-// workgroups of one KV head meet in one L2 where the heads are eight), then through its ranges of keys, then through its row
-// blocks, those with the most keys first.
+// workgroups of one KV head meet in one L2 where the heads are eight), then through the ranges of keys, then through its row blocks.
 struct Item {
-    int seq, kv, block, split;
+    int seq, kv, block, split, splits;
 };
 __device__ inline Item item_of(const PromptArgs& A, int id) {
     int s = 0;
     for (int step = KVQ_PROMPT_SEQS / 2; step; step >>= 1)
         if (s + step < A.n_seqs && A.seq[s + step].item0 <= id) s += step;
     const PromptSeq& S = A.seq[s];
-    const int x = id - S.item0, y = x / A.n_kv, z = y / S.splits;
-    return Item{s, x - y * A.n_kv, z, y - z * S.splits};
+    const int x = id - S.item0, y = x / A.n_kv;
+    if (y < S.whole) return Item{s, x - y * A.n_kv, y, 0, 1};
+    const int z = (y - S.whole) / S.splits;
+    return Item{s, x - y * A.n_kv, S.whole + z, y - S.whole - z * S.splits, S.splits};
+}
+// The partial results of a block in ranges: its first group of 16 rows, range 0.
+template <int RB>
+__device__ inline int64_t parts_of(const PromptSeq& S, int kv, int block) {
+    return S.part0 + ((int64_t)kv * (S.blocks - S.whole) + (block - S.whole)) * S.splits * (RB / 16);
 }
 // Row r of a block: head inside the group and query; head < 0: no such row.
 struct Row {
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         }
         tiles = (last + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
     }
-    const int per = (tiles + S.splits - 1) / S.splits, t0 = min(tiles, it.split * per), t1 = min(tiles, t0 + per);
+    const int per = (tiles + it.splits - 1) / it.splits, t0 = min(tiles, it.split * per), t1 = min(tiles, t0 + per);
 
     State<R> st;
     st.clear();
@@ -186,6 +193,15 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                             for (int r = 0; r < R; ++r) s[r][x][sub] = mma(a, q[r][grp], s[r][x][sub]);
                         }
                     }
+                if constexpr (!APART) {  // operands are read four ahead of their products
+                    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                    for (int g = 0; g < 8 * TT - 4; ++g) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, R, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    }
+                    __builtin_amdgcn_sched_group_barrier(0x008, 4 * R, 0);
+                }
                 // behind the causal border of some row, beyond the last key or beyond the range
                 const bool masked = min(least, t1 * KVQ_TILE_TOKENS) < tok + TT * KVQ_TILE_TOKENS;
                 if (masked) {
@@ -229,6 +245,15 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                             }
                         }
                     }
+                if constexpr (!APART) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+                    for (int g = 0; g < 8 * TT - 4; ++g) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, R, 1);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                    }
+                    __builtin_amdgcn_sched_group_barrier(0x008, 4 * R, 1);
+                }
             }
             if (more) store(buf ^ 1);
             __syncthreads();
@@ -243,8 +268,8 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
     if (WT > 1 && wt > 0) return;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (S.splits > 1) {
-            const int64_t group = S.part0 + ((int64_t)(it.kv * S.blocks + it.block) * S.splits + it.split) * (RB / 16) + wm * R + r;
+        if (it.splits > 1) {
+            const int64_t group = parts_of<RB>(S, it.kv, it.block) + it.split * (RB / 16) + wm * R + r;
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
             continue;
         }
@@ -266,17 +291,18 @@ template <int RB>
 __global__ __launch_bounds__(512) void kvq_prompt_merge_kernel(const PromptArgs A) {
     __shared__ JoinLds lds;
     const int lane = threadIdx.x & 63, j = lane >> 4, n = lane & 15;
-    // for each (workgroup of the first launch with range 0, group of 16 rows)
-    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % (RB / 16);
-    const Item it = item_of(A, (blockIdx.x >> 2) / (RB / 16));
-    const PromptSeq& S = A.seq[it.seq];
-    if (S.splits == 1 || it.split != 0) return;
-    const float* part = A.part + (S.part0 + (int64_t)(it.kv * S.blocks + it.block) * S.splits * (RB / 16) + rg) * (KVQ_PART_BYTES / 4);
+    const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % (RB / 16), id = (blockIdx.x >> 2) / (RB / 16);
+    int q = 0;
+    for (int step = KVQ_PROMPT_SEQS / 2; step; step >>= 1)
+        if (q + step < A.n_seqs && A.seq[q + step].merge0 <= id) q += step;
+    const PromptSeq& S = A.seq[q];
+    const int at = id - S.merge0, kv = at % A.n_kv, block = S.whole + at / A.n_kv;
+    const float* part = A.part + (parts_of<RB>(S, kv, block) + rg) * (KVQ_PART_BYTES / 4);
     Joined x;
     if (!join_partials(lds, part, (int64_t)(RB / 16) * (KVQ_PART_BYTES / 4), S.splits, pair, x)) return;
-    const Row row = row_of<RB>(A, S, it.block, rg * 16 + n);
+    const Row row = row_of<RB>(A, S, block, rg * 16 + n);
     if (row.head < 0) return;
-    const int head = it.kv * A.gqa + row.head;
+    const int head = kv * A.gqa + row.head;
     const int64_t tok = S.q0 + row.query, to = tok * A.o_ts + (int64_t)head * A.o_hs;
     void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
     store_out4(dst, A.out_fp32, 16 * x.nt + 4 * j, x.o * inverse_of(x.l));
@@ -287,14 +313,13 @@ __global__ __launch_bounds__(512) void kvq_prompt_merge_kernel(const PromptArgs 
 
 // Kernels by the rows of a block.  Few rows leave wavefronts over, which then share the rows and take the tiles in turn.
 struct Variant {
-    int rb;
+    int rb, slots;  // slots: workgroups that the device takes at a time
     void (*kernel)(PromptArgs), (*merge)(PromptArgs);
 };
-#define KVQ_PROMPT_VARIANT(R, WM, WT, NT) {16 * R * WM, kvq_prompt_kernel<R, WM, WT, NT>, kvq_prompt_merge_kernel<16 * R * WM>}
-const Variant kVariants[] = {KVQ_PROMPT_VARIANT(1, 1, 4, 4), KVQ_PROMPT_VARIANT(2, 1, 4, 4), KVQ_PROMPT_VARIANT(2, 2, 2, 4),
-                             KVQ_PROMPT_VARIANT(2, 4, 1, 2)};
+#define KVQ_PROMPT_VARIANT(R, WM, WT, NT, SLOTS) {16 * R * WM, SLOTS, kvq_prompt_kernel<R, WM, WT, NT>, kvq_prompt_merge_kernel<16 * R * WM>}
+const Variant kVariants[] = {KVQ_PROMPT_VARIANT(1, 1, 4, 4, 256), KVQ_PROMPT_VARIANT(2, 1, 4, 4, 256), KVQ_PROMPT_VARIANT(2, 2, 2, 4, 256),
+                             KVQ_PROMPT_VARIANT(2, 4, 1, 2, 512)};
 constexpr int kNumVariants = 4;
-constexpr int kTargetWorkgroups = 512;  // two a compute unit
 constexpr int kLeastTiles = 8;          // of a range of keys
 constexpr int kMostSplits = KVQ_MOST_PARTS;
 
@@ -307,53 +332,67 @@ PromptSeq describe(int v, int gqa, int q0, int nq, int k0, int nk) {
     PromptSeq s{};
     s.q0 = q0; s.nq = nq; s.k0 = k0; s.nk = nk;
     s.flat = nq <= rb ? 1 : 0;
-    s.blocks = s.flat ? (int)(((int64_t)gqa * nq + rb - 1) / rb) : gqa * ((nq + rb - 1) / rb);
+    s.blocks = s.whole = s.flat ? (int)(((int64_t)gqa * nq + rb - 1) / rb) : gqa * ((nq + rb - 1) / rb);
     s.splits = 1;
     return s;
 }
 
-// Calls launch(variant, args) for every launch of the call, with everything in args that depends on the lengths; workspace: bytes there are
-// (0: no ranges).  Returns the most bytes of workspace a launch uses, or -1 if the call is too large.
+// Cuts blocks of a launch into ranges of keys where whole ones would leave the device idle: all of them if they are fewer than the
+// workgroups it takes at a time, else those that are left over when it has been filled as often as they fill it, the last ones of the order
+// (640 equal blocks: 512, then 128 in four ranges each, 904 -> 748 us), unless the fillings are many.
+void cut_blocks(PromptArgs& A, int64_t items, int slots) {
+    if (items >= 4 * (int64_t)slots) return;
+    int64_t left = items % slots;
+    if (2 * left > slots || left == 0) return;
+    const int64_t want = std::min<int64_t>(slots / left, kMostSplits);
+    for (int k = A.n_seqs - 1; k >= 0 && left > 0; --k) {
+        PromptSeq& s = A.seq[k];
+        const int64_t mine = std::min<int64_t>(s.blocks, (left + A.n_kv - 1) / A.n_kv);
+        left -= mine * A.n_kv;
+        const int tiles = (s.nk + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, tiles / kLeastTiles));
+        if (s.splits > 1) s.whole = s.blocks - (int)mine;
+    }
+}
+
+// Calls launch(variant, args, workgroups, blocks in ranges) for every launch of the call, with everything in args that depends on the
+// lengths; workspace: bytes there are (0: no ranges).  Returns the most bytes of workspace a launch uses, -1 if the call is
+// too large, -2 if a launch fails.
 template <class Launch>
 int64_t plan_prompt(PromptArgs& A, const int32_t* qb, const int32_t* kb, int n_seqs, int64_t workspace, Launch launch) {
     int64_t most = 0;
     for (int v = 0; v < kNumVariants; ++v) {
-        int64_t items = 0;
-        for (int i = 0; i < n_seqs; ++i) {
-            const int nq = qb[i + 1] - qb[i];
-            if (nq && variant_of(A.gqa, nq) == v) items += (int64_t)A.n_kv * describe(v, A.gqa, 0, nq, 0, 0).blocks;
-        }
-        if (!items) continue;
-        const int64_t want = (kTargetWorkgroups + items - 1) / items;
         for (int i = 0; i < n_seqs;) {
             A.n_seqs = 0;
+            int64_t items = 0;
             for (; i < n_seqs && A.n_seqs < KVQ_PROMPT_SEQS; ++i) {
                 const int nq = qb[i + 1] - qb[i], nk = kb[i + 1] - kb[i];
                 if (!nq || variant_of(A.gqa, nq) != v) continue;
-                PromptSeq s = describe(v, A.gqa, qb[i], nq, kb[i], nk);
-                const int tiles = (nk + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
-                s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), tiles / kLeastTiles));
-                A.seq[A.n_seqs++] = s;
+                A.seq[A.n_seqs] = describe(v, A.gqa, qb[i], nq, kb[i], nk);
+                items += (int64_t)A.n_kv * A.seq[A.n_seqs++].blocks;
             }
             if (!A.n_seqs) continue;
+            if (items > (1 << 30) / kMostSplits) return -1;
             // the longest first: what starts last ends last
             std::sort(A.seq, A.seq + A.n_seqs, [](const PromptSeq& a, const PromptSeq& b) { return a.nk != b.nk ? a.nk > b.nk : a.q0 < b.q0; });
+            cut_blocks(A, items, kVariants[v].slots);
             for (int pass = 0;; ++pass) {  // a second time without ranges where the workspace does not hold their partial results
-                int64_t at = 0, groups = 0;
+                int64_t at = 0, groups = 0, merges = 0;
                 for (int k = 0; k < A.n_seqs; ++k) {
                     PromptSeq& s = A.seq[k];
-                    if (pass) s.splits = 1;
-                    const int64_t wgs = (int64_t)A.n_kv * s.blocks * s.splits;
+                    if (pass) s.whole = s.blocks;
                     s.item0 = (int32_t)at;
                     s.part0 = (int32_t)groups;
-                    at += wgs;
-                    if (s.splits > 1) groups += wgs * (kVariants[v].rb / 16);
-                    if (at > (1 << 30) || groups > (1 << 30)) return -1;
+                    s.merge0 = (int32_t)merges;
+                    const int64_t cut = (int64_t)A.n_kv * (s.blocks - s.whole);
+                    at += (int64_t)A.n_kv * s.whole + cut * s.splits;
+                    groups += cut * s.splits * (kVariants[v].rb / 16);
+                    merges += cut;
                 }
                 const int64_t bytes = groups * KVQ_PART_BYTES;
                 if (bytes > workspace && !pass) continue;
                 most = std::max(most, bytes);
-                if (!launch(v, A, (int)at, groups > 0)) return -2;
+                if (!launch(v, A, (int)at, (int)merges)) return -2;
                 break;
             }
         }
@@ -383,7 +422,7 @@ uint64_t kvq_prompt_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, const
     PromptArgs A{};
     A.gqa = n_q_heads / n_kv_heads;
     A.n_kv = n_kv_heads;
-    const int64_t most = plan_prompt(A, q_begin_host, k_begin_host, n_seqs, INT64_MAX, [](int, const PromptArgs&, int, bool) { return true; });
+    const int64_t most = plan_prompt(A, q_begin_host, k_begin_host, n_seqs, INT64_MAX, [](int, const PromptArgs&, int, int) { return true; });
     return most < 0 ? 0 : (uint64_t)most;
 }
 
@@ -428,12 +467,12 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* d, const void* q_dev, cons
     A.flip = scale < 0.f ? 0x80008000u : 0u;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int64_t got = plan_prompt(A, q_begin_host, k_begin_host, n_seqs, workspace_dev ? (int64_t)std::min<uint64_t>(workspace_bytes, INT64_MAX) : 0,
-                                    [&](int v, const PromptArgs& args, int wgs, bool split) {
+                                    [&](int v, const PromptArgs& args, int wgs, int merges) {
         const Variant& V = kVariants[v];
         hipLaunchKernelGGL(V.kernel, dim3((unsigned)wgs), dim3(KVQ_PROMPT_THREADS), 0, s, args);
         if (hipGetLastError() != hipSuccess) return false;
-        if (!split) return true;
-        hipLaunchKernelGGL(V.merge, dim3((unsigned)wgs * (unsigned)(V.rb / 16 * 4)), dim3(512), 0, s, args);
+        if (!merges) return true;
+        hipLaunchKernelGGL(V.merge, dim3((unsigned)merges * (unsigned)(V.rb / 16 * 4)), dim3(512), 0, s, args);
         return hipGetLastError() == hipSuccess;
     });
     return got == -1 ? KVQ_E_INVALID : got < 0 ? KVQ_E_HIP : KVQ_OK;
