@@ -151,12 +151,12 @@ __device__ inline uint32_t slot_code(const uint32_t* w, int bits, int s) {  // s
 // Eight consecutive channels of one token.
 __device__ inline void store8(void* out, int fp32, int64_t at, const float (&x)[8]) {
     if (fp32) {
-        float* p = static_cast<float*>(out) + at;
-        *reinterpret_cast<kvq_dev::f32x4*>(p) = kvq_dev::f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<kvq_dev::f32x4*>(p + 4) = kvq_dev::f32x4{x[4], x[5], x[6], x[7]};
+        kvq_dev::f32x4* p = reinterpret_cast<kvq_dev::f32x4*>(static_cast<float*>(out) + at);
+        __builtin_nontemporal_store(kvq_dev::f32x4{x[0], x[1], x[2], x[3]}, p);
+        __builtin_nontemporal_store(kvq_dev::f32x4{x[4], x[5], x[6], x[7]}, p + 1);
     } else {
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + at) =
-            u32x4{kvq_dev::pack_rn2(x[0], x[1]), kvq_dev::pack_rn2(x[2], x[3]), kvq_dev::pack_rn2(x[4], x[5]), kvq_dev::pack_rn2(x[6], x[7])};
+        __builtin_nontemporal_store(u32x4{kvq_dev::pack_rn2(x[0], x[1]), kvq_dev::pack_rn2(x[2], x[3]), kvq_dev::pack_rn2(x[4], x[5]),
+                                          kvq_dev::pack_rn2(x[6], x[7])}, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + at));
     }
 }
 
@@ -192,68 +192,83 @@ __device__ inline void piece_values(const uint8_t* tile, int lane, int p, const 
         }
     }
 }
-template <int B>
-__device__ inline void read_k(const ReadArgs& A, const uint8_t* code, const uint16_t* meta, int unit, int tile, int lane) {
-    const int j = lane >> 4, n = lane & 15;
+// Rows of 64 channels that the wavefront has put together in LDS: eight lanes store 128 consecutive bytes of a row (256 of fp32).
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ inline void store_rows(const ReadArgs& A, void* out, int unit, int tile, int half, const float* lds, int lane) {
     const int64_t rows = A.n_tokens - A.begin;
-    for (int p = 0; p < 8; ++p) {
-        const int t = 8 * (n >> 2) + 4 * (p >> 2) + (n & 3), tok = tile * KVQ_TILE_TOKENS + t, channel = 32 * (p & 3) + 8 * j;
-        float s[8] = {}, z[8] = {}, x[8];
-        if (B != 16) {
-            const float s1 = h2f(meta[t * 4 + (p & 3)]), z1 = h2f(meta[128 + t * 4 + (p & 3)]);
+    wave_sync();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { s[i] = s1; z[i] = z1; }
-        }
-        piece_values<B>(code, lane, p, s, z, x);
-        if (A.lambda) {
-            const float* l = A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + channel;
+    for (int i = 0; i < 4; ++i) {
+        const int t = 8 * i + (lane >> 3), c = 8 * (lane & 7), tok = tile * KVQ_TILE_TOKENS + t;
+        float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= l[i];
+        for (int e = 0; e < 8; ++e) x[e] = lds[t * KVQ_READ_PITCH + c + e];
+        if (tok >= A.begin && tok < A.n_tokens) store8(out, A.fp32, ((int64_t)unit * rows + (tok - A.begin)) * KVQ_D + 64 * half + c, x);
+    }
+    wave_sync();
+}
+// A lane holds eight channels of a token ...
+template <int B>
+__device__ inline void read_k(const ReadArgs& A, const uint8_t* code, const uint16_t* meta, int unit, int tile, float* lds, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int sub = q >> 1, grp = 2 * half + (q & 1);
+            const int t = 8 * (n >> 2) + 4 * sub + (n & 3), channel = 32 * grp + 8 * j;
+            float s[8] = {}, z[8] = {}, x[8];
+            if (B != 16) {
+                const float s1 = h2f(meta[t * 4 + grp]), z1 = h2f(meta[128 + t * 4 + grp]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { s[i] = s1; z[i] = z1; }
+            }
+            piece_values<B>(code, lane, sub * 4 + grp, s, z, x);
+            if (A.lambda) {
+                const float* l = A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + channel;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] *= l[i];
+            }
+            kvq_dev::f32x4* const to = reinterpret_cast<kvq_dev::f32x4*>(lds + t * KVQ_READ_PITCH + (channel & 63));
+            to[0] = kvq_dev::f32x4{x[0], x[1], x[2], x[3]};
+            to[1] = kvq_dev::f32x4{x[4], x[5], x[6], x[7]};
         }
-        if (tok >= A.begin && tok < A.n_tokens) store8(A.k_out, A.fp32, ((int64_t)unit * rows + (tok - A.begin)) * KVQ_D + channel, x);
+        store_rows(A, A.k_out, unit, tile, half, lds, lane);
     }
 }
-// The lanes hold eight tokens of a channel each; rows are put together in LDS, 64 channels at a time.
+// ... or eight tokens of a channel.
 template <int B>
 __device__ inline void read_v(const ReadArgs& A, const uint8_t* code, const uint16_t* meta, int unit, int tile, float* lds, int lane) {
     const int j = lane >> 4, n = lane & 15;
-    const int64_t rows = A.n_tokens - A.begin;
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
+#pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int nt = 4 * half + q;
             float s[8] = {}, z[8] = {}, x[8];
-            if (B != 16) {
+            if (B != 16) {  // the quarter's eight tokens, in pairs (v, v + 4)
+                const u32x4 sw = *reinterpret_cast<const u32x4*>(meta + 256 + (nt >> 1) * 32 + j * 8), zw = *reinterpret_cast<const u32x4*>(meta + 384 + (nt >> 1) * 32 + j * 8);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int at = (nt >> 1) * 32 + j * 8 + (i & 3) * 2 + (i >> 2);
-                    s[i] = h2f(meta[256 + at]);
-                    z[i] = h2f(meta[384 + at]);
+                    const uint32_t sp = sw[i & 3], zp = zw[i & 3];
+                    s[i] = h2f((uint16_t)(i < 4 ? sp : sp >> 16));
+                    z[i] = h2f((uint16_t)(i < 4 ? zp : zp >> 16));
                 }
             }
             piece_values<B>(code, lane, nt, s, z, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) lds[(8 * j + i) * KVQ_READ_PITCH + 16 * q + n] = x[i];
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = 8 * i + (lane >> 3), c = 8 * (lane & 7), tok = tile * KVQ_TILE_TOKENS + t;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = lds[t * KVQ_READ_PITCH + c + e];
-            if (tok >= A.begin && tok < A.n_tokens)
-                store8(A.v_out, A.fp32, ((int64_t)unit * rows + (tok - A.begin)) * KVQ_D + 64 * half + c, x);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        store_rows(A, A.v_out, unit, tile, half, lds, lane);
     }
 }
 // A wavefront takes K or V of one tile of one unit.
 __global__ __launch_bounds__(256) void kvq_read_kernel(const ReadArgs A) {
-    __shared__ __attribute__((aligned(16))) float lds[2][KVQ_TILE_TOKENS * KVQ_READ_PITCH];
+    __shared__ __attribute__((aligned(16))) float lds[4][KVQ_TILE_TOKENS * KVQ_READ_PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item = (int64_t)blockIdx.x * 2 + (wave >> 1);
     if (item >= A.items) return;
@@ -264,15 +279,15 @@ __global__ __launch_bounds__(256) void kvq_read_kernel(const ReadArgs A) {
     const uint8_t* code = A.arena + (uint64_t)d.code_off256 * 256u + slot * (1024u * d.bits);
     const uint16_t* meta = reinterpret_cast<const uint16_t*>(A.arena + (uint64_t)d.meta_off256 * 256u + slot * KVQ_META_TILE_BYTES);
     const int width = d.bits == 16 && d.int16 ? 17 : (int)d.bits;
+    float* const own = lds[wave];
     if (!(wave & 1)) {
-        if (width == 2) read_k<2>(A, code, meta, unit, tile, lane);
-        else if (width == 4) read_k<4>(A, code, meta, unit, tile, lane);
-        else if (width == 8) read_k<8>(A, code, meta, unit, tile, lane);
-        else if (width == 16) read_k<16>(A, code, meta, unit, tile, lane);
-        else read_k<17>(A, code, meta, unit, tile, lane);
+        if (width == 2) read_k<2>(A, code, meta, unit, tile, own, lane);
+        else if (width == 4) read_k<4>(A, code, meta, unit, tile, own, lane);
+        else if (width == 8) read_k<8>(A, code, meta, unit, tile, own, lane);
+        else if (width == 16) read_k<16>(A, code, meta, unit, tile, own, lane);
+        else read_k<17>(A, code, meta, unit, tile, own, lane);
     } else {
         code += 512u * d.bits;
-        float* const own = lds[wave >> 1];
         if (width == 2) read_v<2>(A, code, meta, unit, tile, own, lane);
         else if (width == 4) read_v<4>(A, code, meta, unit, tile, own, lane);
         else if (width == 8) read_v<8>(A, code, meta, unit, tile, own, lane);
