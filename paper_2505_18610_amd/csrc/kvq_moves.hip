@@ -43,7 +43,17 @@ struct ForkArgs {
 };
 static_assert(sizeof(ForkArgs) <= 4096 - 64, "kernel arguments end at 4 KiB");
 
+// Forks that write more than the device's last-level cache holds go past it (sixteen samples of 32,768 tokens, 361 MB, 90 -> 75 us);
+// what fits is left there for the attention that follows (eight beams of 2,500 tokens, 45 MB: the same 16.5 us, but the next
+// kernel reads them in 21.6 us and not in 32).
+#define KVQ_FORK_STREAM_BYTES (256ull << 20)
+template <bool STREAM>
+__device__ inline void store16(uint8_t* to, u32x4 w) {
+    if (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(to));
+    else *reinterpret_cast<u32x4*>(to) = w;
+}
 // Copies `bytes` (a multiple of 1 KiB, 1 KiB or more) with 256 threads, four loads in flight a thread.
+template <bool STREAM>
 __device__ inline void copy_bytes(uint8_t* dst, const uint8_t* src, uint32_t bytes, int tid) {
     uint32_t at = 16u * tid;
     for (; at + 3 * 4096 < bytes; at += 4 * 4096) {
@@ -51,13 +61,14 @@ __device__ inline void copy_bytes(uint8_t* dst, const uint8_t* src, uint32_t byt
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const u32x4*>(src + at + i * 4096);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(dst + at + i * 4096) = w[i];
+        for (int i = 0; i < 4; ++i) store16<STREAM>(dst + at + i * 4096, w[i]);
     }
-    for (; at < bytes; at += 4096) *reinterpret_cast<u32x4*>(dst + at) = *reinterpret_cast<const u32x4*>(src + at);
+    for (; at < bytes; at += 4096) store16<STREAM>(dst + at, *reinterpret_cast<const u32x4*>(src + at));
 }
 
 // One workgroup: up to four neighbouring tiles of one page, KV head and sequence, codes and metadata.  Workgroups of one place follow
 // one another over the sequences, so that sequences with the same parent read it while it is in the caches.
+template <bool STREAM>
 __global__ __launch_bounds__(256) void kvq_fork_kernel(const ForkArgs A) {
     const int tid = threadIdx.x;
     int x = blockIdx.x;
@@ -82,10 +93,10 @@ __global__ __launch_bounds__(256) void kvq_fork_kernel(const ForkArgs A) {
     const uint64_t src_slot = (uint64_t)(parent * A.n_kv + h) * A.tpp + group * KVQ_FORK_TILES;
     const uint64_t dst_slot = (uint64_t)(b * A.n_kv + h) * A.tpp + group * KVQ_FORK_TILES;
     const uint32_t tile_bytes = 1024u * from.bits;
-    copy_bytes(A.dst + (uint64_t)to.code_off256 * 256u + dst_slot * tile_bytes, A.src + (uint64_t)from.code_off256 * 256u + src_slot * tile_bytes,
+    copy_bytes<STREAM>(A.dst + (uint64_t)to.code_off256 * 256u + dst_slot * tile_bytes, A.src + (uint64_t)from.code_off256 * 256u + src_slot * tile_bytes,
                (uint32_t)tiles * tile_bytes, tid);
     if (from.bits < 16 || from.int16)
-        copy_bytes(A.dst + (uint64_t)to.meta_off256 * 256u + dst_slot * KVQ_META_TILE_BYTES,
+        copy_bytes<STREAM>(A.dst + (uint64_t)to.meta_off256 * 256u + dst_slot * KVQ_META_TILE_BYTES,
                    A.src + (uint64_t)from.meta_off256 * 256u + src_slot * KVQ_META_TILE_BYTES, (uint32_t)tiles * KVQ_META_TILE_BYTES, tid);
 }
 
@@ -410,6 +421,7 @@ kvq_status_t fork_impl(kvq_cache* dst, kvq_cache* src, int32_t layer, const int3
     A.in_place = src == dst ? 1 : 0;
     const int64_t per_page = (int64_t)A.groups * dst->units;
     const int most = (int)std::max<int64_t>(1, std::min<int64_t>(KVQ_FORK_ARG_PAGES, (1 << 30) / per_page));
+    const bool stream = bytes > KVQ_FORK_STREAM_BYTES;
     hipError_t e = hipSuccess;
     for (int at = 0; at < A.n_pages && e == hipSuccess; at += most) {
         A.page0 = at;
@@ -419,7 +431,7 @@ kvq_status_t fork_impl(kvq_cache* dst, kvq_cache* src, int32_t layer, const int3
             A.code_off256[i] = d.code_off256;
             A.meta_off256[i] = d.meta_off256;
         }
-        hipLaunchKernelGGL(kvq_fork_kernel, dim3((unsigned)(per_page * A.n_here)), dim3(256), 0, s, A);
+        hipLaunchKernelGGL(stream ? kvq_fork_kernel<true> : kvq_fork_kernel<false>, dim3((unsigned)(per_page * A.n_here)), dim3(256), 0, s, A);
         e = hipGetLastError();
         if (e == hipSuccess && A.in_place) {
             hipLaunchKernelGGL(kvq_fork_table_kernel, dim3(1), dim3(256), 0, s, A);
