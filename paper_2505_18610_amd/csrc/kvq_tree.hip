@@ -203,19 +203,34 @@ __device__ inline void expand_tile(const Fetched& f, uint8_t* slot, uint8_t* met
 template <int R>
 __device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
     const int j = lane >> 4, n = lane & 15;
-    const float* lam = factors && A.lambda ? A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + 8 * j : nullptr;
+    u32x4 w[R][4];  // (all loads first, under no branch: they are the start of a chain)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = row0 + 16 * r + n;
         const _Float16* src = A.q + ((int64_t)unit * A.rows + min(row, A.rows - 1)) * KVQ_D + 8 * j;
 #pragma unroll
-        for (int grp = 0; grp < 4; ++grp) {
-            u32x4 w = *reinterpret_cast<const u32x4*>(src + 32 * grp);
-            if (lam) w = kvq_dev::scale_keys8(w, lam + 32 * grp);
-            w ^= A.flip;
-            if (row >= A.rows) w = u32x4{0, 0, 0, 0};
-            q[r][grp] = to_half8(paired(w));
-        }
+        for (int grp = 0; grp < 4; ++grp) w[r][grp] = *reinterpret_cast<const u32x4*>(src + 32 * grp);
+    }
+    if (factors && A.lambda) {
+        const float* lam = A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + 8 * j;
+        kvq_dev::f32x4 l[4][2];
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) l[grp][h] = *reinterpret_cast<const kvq_dev::f32x4_any*>(lam + 32 * grp + 4 * h);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int grp = 0; grp < 4; ++grp)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[r][grp][e] = kvq_dev::scale_pair(w[r][grp][e], l[grp][e >> 1][(2 * e) & 3], l[grp][e >> 1][(2 * e + 1) & 3]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool real = row0 + 16 * r + n < A.rows;
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) q[r][grp] = to_half8(real ? paired(w[r][grp] ^ A.flip) : u32x4{0, 0, 0, 0});
     }
 }
 // Sums of q over the channels of each group, for the zero points: a high part in lane quarter 0, what it leaves in quarter 1, the B operand
