@@ -33,7 +33,9 @@ struct TreeArgs {
     int32_t n_tokens, n_tiles, tpp;
     uint32_t tpp_magic;
     int32_t units, n_kv, gqa, nodes, words, rows;
-    int32_t blocks, splits;  // row blocks of a unit, ranges of tiles; beyond one range the nodes themselves are a range of their own
+    int32_t blocks, splits;  // row blocks of a unit, ranges (partial results of a block, if more than one)
+    int32_t per;             // tiles of a range
+    int32_t node_tiles;      // what the nodes count for, in tiles: they come first in the line that is cut into ranges, in range 0
     int32_t groups;          // of 16 rows in a block
     int32_t wt;              // many rows: wavefronts that share rows and take an iteration's tiles in turn
     int32_t out_fp32;
@@ -201,9 +203,8 @@ __device__ inline void expand_tile(const Fetched& f, uint8_t* slot, uint8_t* met
 // Query operands in pairs.  For the cache they are multiplied by the block's key factors (fp32 product, rounded to fp16, as for a decode
 // step); against the nodes' own keys they are what they are.
 template <int R>
-__device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+__device__ inline void ask_queries(u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, int lane) {  // (all loads first: they are the start of a chain)
     const int j = lane >> 4, n = lane & 15;
-    u32x4 w[R][4];  // (all loads first, under no branch: they are the start of a chain)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = row0 + 16 * r + n;
@@ -211,6 +212,10 @@ __device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int uni
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) w[r][grp] = *reinterpret_cast<const u32x4*>(src + 32 * grp);
     }
+}
+template <int R>
+__device__ inline void set_queries(half8 (&q)[R][4], u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+    const int j = lane >> 4, n = lane & 15;
     if (factors && A.lambda) {
         const float* lam = A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + 8 * j;
         kvq_dev::f32x4 l[4][2];
@@ -233,22 +238,28 @@ __device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int uni
         for (int grp = 0; grp < 4; ++grp) q[r][grp] = to_half8(real ? paired(w[r][grp] ^ A.flip) : u32x4{0, 0, 0, 0});
     }
 }
+template <int R>
+__device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+    u32x4 w[R][4];
+    ask_queries<R>(w, A, unit, row0, lane);
+    set_queries<R>(q, w, A, unit, row0, factors, lane);
+}
 // Sums of q over the channels of each group, for the zero points: a high part in lane quarter 0, what it leaves in quarter 1, the B operand
 // of a product with 16 channels whose A operand repeats a token's four zero points.  Queries so large that a sum passes the fp16
 // range are made smaller by 2^10, all of the wavefront's; returns what the scale grows by.
 template <int R>
 __device__ inline float sum_queries(half8 (&q)[R][4], half4 (&qs)[R], int lane) {
     const int j = lane >> 4;
+    half8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
     float sum[R][4];
     bool large = false;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) {
-            float x = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x += (float)q[r][grp][e];
-            sum[r][grp] = quarters_sum(x);
+            sum[r][grp] = mma(ones, q[r][grp], float4v{0.f, 0.f, 0.f, 0.f})[0];  // (the same for every row of the result)
             large |= fabsf(sum[r][grp]) >= 65504.f;
         }
     float grow = 1.f;
@@ -535,6 +546,11 @@ __device__ inline bool lay_out_v(const TreeArgs& A, int unit, int first, uint8_t
     return any;
 }
 
+// The cache's tiles of a range.
+__device__ inline void range_of(const TreeArgs& A, int split, int& t0, int& t1) {
+    t0 = min(A.n_tiles, max(0, split * A.per - A.node_tiles));
+    t1 = min(A.n_tiles, max(0, (split + 1) * A.per - A.node_tiles));
+}
 // Masks what lies behind the cache's last token.
 template <int R>
 __device__ inline void mask_end(float4v (&s)[R][1][2], int end) {
@@ -575,7 +591,7 @@ __device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int uni
     for (int r = 0; r < R; ++r) {
         const int row = (block * A.groups + group0 + r) * 16 + n;
         if (A.splits > 1) {
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * A.groups + group0 + r;
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + r;
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
             continue;
         }
@@ -589,7 +605,7 @@ __device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int uni
     if (nonfinite) {
 #pragma unroll 1
         for (int r = 0; r < R; ++r) {
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * (A.splits + 1) + split) * A.groups + group0 + r;
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + r;
             add_nonfinite(A, unit, (block * A.groups + group0 + r) * 16 + n, A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
         }
     }
@@ -615,14 +631,18 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
     // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
     const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
     const int row0 = (block * A.groups + wm * R) * 16;  // of this wavefront
-    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
+    int t0, t1;
+    range_of(A, split, t0, t1);
     State<R> st;
     st.clear();
     half8 q[R][4];
     if (t0 < t1) {
-        Staged f = stage_tile(A, entry_of(A, min(t0 + own, t1 - 1)), unit, min(t0 + own, t1 - 1), part, stage, lane);
+        const KvqPageDesc first = entry_of(A, min(t0 + own, t1 - 1));
         KvqPageDesc next = entry_of(A, min(t0 + NT + own, t1 - 1));
-        load_queries<R>(q, A, unit, row0, true, lane);
+        u32x4 w[R][4];
+        ask_queries<R>(w, A, unit, row0, lane);
+        Staged f = stage_tile(A, first, unit, min(t0 + own, t1 - 1), part, stage, lane);
+        set_queries<R>(q, w, A, unit, row0, true, lane);
         half4 qs[R];
         const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
         for (int t = t0; t < t1; t += NT) {
@@ -659,7 +679,7 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
     }
     // the nodes among themselves
     bool nonfinite = false;
-    if (split == (A.splits > 1 ? A.splits : 0)) {
+    if (split == 0) {
         const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
         const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
         for (int t = 0; t < tiles; t += NT) {
@@ -693,15 +713,19 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
     uint8_t* const meta_lds = lds + 4 * SLOT + wave * KVQ_META_TILE_BYTES;
     const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
     const int row0 = block * A.groups * 16;
-    const int per = (A.n_tiles + A.splits - 1) / A.splits, t0 = min(A.n_tiles, split * per), t1 = min(A.n_tiles, t0 + per);
+    int t0, t1;
+    range_of(A, split, t0, t1);
     State<R> st;
     st.clear();
     half8 q[R][4];
     if (t0 + wave < t1) {
-        Fetched f;
-        fetch_tile<I16>(f, A, entry_of(A, t0 + wave), unit, t0 + wave, lane_off);
+        const KvqPageDesc first = entry_of(A, t0 + wave);
         KvqPageDesc next = entry_of(A, min(t0 + wave + 4, t1 - 1));
-        load_queries<R>(q, A, unit, row0, true, lane);
+        u32x4 w[R][4];
+        Fetched f;
+        fetch_tile<I16>(f, A, first, unit, t0 + wave, lane_off);
+        ask_queries<R>(w, A, unit, row0, lane);
+        set_queries<R>(q, w, A, unit, row0, true, lane);
         half4 qs[R];
         const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
         for (int tile = t0 + wave; tile < t1; tile += 4) {
@@ -727,7 +751,7 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
     }
     // the nodes among themselves
     bool nonfinite = false;
-    if (split == (A.splits > 1 ? A.splits : 0)) {
+    if (split == 0) {
         load_queries<R>(q, A, unit, row0, false, lane);
         const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
         const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
@@ -752,9 +776,9 @@ __global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
     const int pair = blockIdx.x & 3, rg = (blockIdx.x >> 2) % A.groups, ub = (blockIdx.x >> 2) / A.groups, block = ub % A.blocks, unit = ub / A.blocks;
     const int row0 = (block * A.groups + rg) * 16;
     if (row0 >= A.rows) return;
-    const float* part = A.part + ((int64_t)ub * (A.splits + 1) * A.groups + rg) * (KVQ_PART_BYTES / 4);
+    const float* part = A.part + ((int64_t)ub * A.splits * A.groups + rg) * (KVQ_PART_BYTES / 4);
     Joined x;
-    if (!join_partials(lds, part, (int64_t)A.groups * (KVQ_PART_BYTES / 4), A.splits + 1, pair, x)) return;
+    if (!join_partials(lds, part, (int64_t)A.groups * (KVQ_PART_BYTES / 4), A.splits, pair, x)) return;
     const int row = row0 + n;
     if (row >= A.rows) return;
     const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D;
@@ -764,11 +788,12 @@ __global__ __launch_bounds__(512) void kvq_tree_merge_kernel(const TreeArgs A) {
 
 // ---- host side
 
-constexpr int kMostSplits = KVQ_MOST_PARTS - 1;
-constexpr int kLeastTiles = 8;  // of a range: two a wavefront of the kernel for few rows
+constexpr int kMostSplits = KVQ_MOST_PARTS;
+constexpr int kNodeTiles = 4;   // what the nodes cost beside their tiles, in tiles: their queries and their layout
+constexpr int kLeastTiles = 8;  // of a range: two a wavefront of the kernel for few rows, or four iterations of the other
 struct TreePlan {
     bool many;
-    int groups, wt, blocks, splits;  // groups of 16 rows in a block
+    int groups, wt, blocks, splits, per, node_tiles;  // groups of 16 rows in a block
     uint64_t bytes;
 };
 // workspace: bytes there are for partial results
@@ -777,7 +802,9 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
     const int rows = c->gqa * nodes;
     p.many = rows > 32;
     if (p.many) {
-        p.wt = rows <= 64 ? 2 : 1;
+        // pairs where rows are few or there is so little to do that the length of the chain counts: 112 rows x 282 tiles x 4 units 27.4 us
+        // and 24.7 in pairs, 256 x 128 x 2 21.4 and 18.7; 200 x 938 x 8 70 and 78, 448 x 256 x 16 77 and 83
+        p.wt = rows <= 64 || (int64_t)c->units * ((rows + 127) / 128) * n_tiles <= 4096 ? 2 : 1;
         p.groups = 8 / p.wt;
         p.blocks = (rows + 16 * p.groups - 1) / (16 * p.groups);
     } else {
@@ -787,9 +814,17 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
     const int64_t wgs = (int64_t)c->units * p.blocks;
     const int64_t want = std::max<int64_t>(1, (p.many && !c->int16() ? 3 : 2) * c->target_workgroups / wgs);
     const uint64_t one = (uint64_t)wgs * p.groups * KVQ_PART_BYTES;  // a range's partial results
-    const int64_t room = (int64_t)std::min<uint64_t>(workspace / one, kMostSplits + 1) - 1;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(n_tiles / kLeastTiles, room)));
-    p.bytes = p.splits > 1 ? one * (uint64_t)(p.splits + 1) : 0;
+    const int64_t room = (int64_t)std::min<uint64_t>(workspace / one, kMostSplits);
+    p.node_tiles = ((nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS + kNodeTiles + kLeastTiles - 1) / kLeastTiles * kLeastTiles;
+    // half as many tiles a range as long as the ranges are not too many to be joined: 40 rows x 64 tiles x 8 units 17.4 us in 8 and 14.7 in
+    // 16, 16 x 128 x 2 11.5 in 16 and 10.3 in 32; 7 x 282 x 4 14.1 in 35 and 15.7 in 65
+    const int64_t tiles = n_tiles + p.node_tiles, cut = std::max<int64_t>(tiles / kLeastTiles, std::min<int64_t>(2 * tiles / kLeastTiles, 32));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(cut, room)));
+    if (n_tiles < kLeastTiles) p.splits = 1;
+    const int round = p.many ? 1 : 3;  // (in whole iterations: two tiles, or one a wavefront)
+    p.per = ((int)((tiles + p.splits - 1) / p.splits) + round) & ~round;
+    p.splits = p.splits > 1 ? (int)((tiles + p.per - 1) / p.per) : 1;
+    p.bytes = p.splits > 1 ? one * (uint64_t)p.splits : 0;
     return p;
 }
 bool nodes_ok(const kvq_cache* c, int nodes) { return c && nodes >= 1 && nodes <= KVQ_MAX_TREE_NODES; }
@@ -838,6 +873,8 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
     A.rows = c->gqa * n_nodes;
     A.blocks = plan.blocks;
     A.splits = plan.splits;
+    A.per = plan.per;
+    A.node_tiles = plan.node_tiles;
     A.out_fp32 = out_is_fp32 ? 1 : 0;
     const float scale = softmax_scale != 0.f ? softmax_scale : 1.0f / std::sqrt((float)KVQ_D);
     A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
@@ -848,7 +885,7 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
                                                 {{}, {kvq_tree_shared_kernel<2, false>, kvq_tree_shared_kernel<2, true>}}};
     const hipStream_t s = kvq_host::as_stream(hip_stream);
     const unsigned row_blocks = (unsigned)(c->units * plan.blocks);
-    hipLaunchKernelGGL(kernels[plan.many][plan.groups > 1][c->int16()], dim3(row_blocks * (unsigned)(plan.splits > 1 ? plan.splits + 1 : 1)),
+    hipLaunchKernelGGL(kernels[plan.many][plan.groups > 1][c->int16()], dim3(row_blocks * (unsigned)plan.splits),
                        dim3(256), 0, s, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (plan.splits > 1) {
