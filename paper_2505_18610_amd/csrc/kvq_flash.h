@@ -164,29 +164,49 @@ __device__ inline void watch_nonfinite(half8 v, uint32_t& seen) {
     seen = __builtin_bit_cast(uint32_t, acc) & 0x7fff7fffu;
 }
 
-// The products of a V operand that holds infinities or NaNs: a key that a row does not see must not reach it, not even as zero times
-// infinity.  The finite values are taken as ever; three more products count the infinities of either sign and the NaNs among the
-// keys that the row sees (`seen`: 1 for these, 0 for the others, in the order of p), and what is counted decides.  Slow, and rare.
-__device__ inline float4v mfma_nonfinite(half8 v, half8 p, half8 seen, float4v o) {
-    half8 finite, kind[3];
+// Infinite and NaN values of V: a key that a row does not see must not reach it, not even as zero times infinity.  Where there are any they
+// are taken as zeros, and their number among the keys that each row sees is counted apart, by products: infinities of either sign
+// and NaNs.  What they add to a row is added behind everything else, to what has been stored: nothing takes an infinity or a NaN out
+// of a sum again.  Slow, and rare.
+__device__ inline u32x4 finite_only(u32x4 v) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const _Float16 x = v[e];
-        const uint16_t w = __builtin_bit_cast(uint16_t, x), size = w & 0x7fffu;
-        finite[e] = size < 0x7c00u ? x : (_Float16)0.f;
-        kind[0][e] = w == 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
-        kind[1][e] = w == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
-        kind[2][e] = size > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+    for (int e = 0; e < 4; ++e) {
+        uint32_t w = v[e];
+        if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
+        if ((w & 0x7c000000u) == 0x7c000000u) w &= 0x0000ffffu;
+        v[e] = w;
     }
-    o = mma(finite, p, o);
-    const float values[3] = {INFINITY, -INFINITY, __builtin_nanf("")};
+    return v;
+}
+struct NonfiniteCount {
+    float4v count[3] = {};
+    // v: the lane's eight values of a V operand; sees: 1 for the tokens that row n sees, 0 for the others
+    __device__ void add(const uint16_t (&v)[8], half8 sees) {
+        half8 kind[3];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        const float4v count = mma(kind[k], seen, float4v{0.f, 0.f, 0.f, 0.f});
+        for (int e = 0; e < 8; ++e) {
+            kind[0][e] = v[e] == 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+            kind[1][e] = v[e] == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
+            kind[2][e] = (v[e] & 0x7fffu) > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += count[i] > 0.f ? values[k] : 0.f;
+        for (int c = 0; c < 3; ++c) count[c] = mma(kind[c], sees, count[c]);
     }
-    return o;
+    __device__ float4v sum() const {
+        float4v x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = (count[0][i] > 0.f ? INFINITY : 0.f) + (count[1][i] > 0.f ? -INFINITY : 0.f) + (count[2][i] > 0.f ? __builtin_nanf("") : 0.f);
+        return x;
+    }
+};
+// x to four consecutive values of an output
+__device__ inline void add_to_out4(void* out, int fp32, int64_t at, float4v x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (fp32) static_cast<float*>(out)[at + i] += x[i];
+        else static_cast<_Float16*>(out)[at + i] = (_Float16)((float)static_cast<_Float16*>(out)[at + i] + x[i]);
+    }
 }
 
 // Joins the states of two wavefronts that saw different tokens of the same rows: x of the other one.

@@ -72,6 +72,35 @@ __device__ inline Row row_of(const PromptArgs& A, const PromptSeq& S, int block,
     return Row{i < S.nq ? h : -1, i};
 }
 
+// What infinite and NaN values of the tiles t0 .. t1 - 1 add to a row that sees them, to what the same lanes have stored: a partial result or an output.
+__device__ inline void add_nonfinite(const PromptArgs& A, const PromptSeq& S, int kv, Row row, int t0, int t1, float* part, int lane) {
+    const int j = lane >> 4, n = lane & 15;
+    const int limit = row.head >= 0 ? min(t1 * KVQ_TILE_TOKENS, row.query + 1 + S.nk - S.nq) : 0;
+    const uint16_t* const v = reinterpret_cast<const uint16_t*>(A.v) + (int64_t)S.k0 * A.v_ts + (int64_t)kv * A.v_hs;
+#pragma unroll 1
+    for (int nt = 0; nt < 8; ++nt) {
+        NonfiniteCount found;
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t) {
+            uint16_t w[8];
+            half8 sees;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int key = t * KVQ_TILE_TOKENS + 8 * j + e;
+                w[e] = key < S.nk ? v[(int64_t)key * A.v_ts + 16 * nt + n] : (uint16_t)0;
+                sees[e] = key < limit ? (_Float16)1.f : (_Float16)0.f;
+            }
+            found.add(w, sees);
+        }
+        if (part) {
+            reinterpret_cast<float4v*>(part)[nt * 64 + lane] += found.sum();
+        } else if (row.head >= 0) {
+            const int64_t at = (S.q0 + row.query) * A.o_ts + (int64_t)(kv * A.gqa + row.head) * A.o_hs;
+            add_to_out4(A.out, A.out_fp32, at + 16 * nt + 4 * j, found.sum());
+        }
+    }
+}
+
 // One workgroup: WM * 16 R rows of one KV head against a range of keys; WT wavefronts share rows and take the tiles in turn.  An
 // iteration loads NT tiles (K and V, 16 KiB each) into one half of LDS while the other is computed on.
 template <int R, int WM, int WT, int NT>
@@ -118,9 +147,11 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
             const int per_head = S.blocks / A.gqa, ib = per_head - 1 - it.block / A.gqa;
             last = max(0, min(S.nq, (ib + 1) * RB) + S.nk - S.nq);
         }
-        tiles = (last + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
+        // (the compiler does not see that this is the same in all lanes; without it every load of the loop was issued in a loop of its
+        // own over the lanes' descriptors, and the accumulators were copied once an iteration)
+        tiles = __builtin_amdgcn_readfirstlane((last + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS);
     }
-    const int per = (tiles + it.splits - 1) / it.splits, t0 = min(tiles, it.split * per), t1 = min(tiles, t0 + per);
+    const int per = (tiles + it.splits - 1) / it.splits, t0 = __builtin_amdgcn_readfirstlane(min(tiles, it.split * per)), t1 = min(tiles, t0 + per);
 
     State<R> st;
     st.clear();
@@ -139,9 +170,9 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
     const int k_off = k_token * k_row + k_chunk * 16, v_off = v_token * v_row + v_chunk * 16;
     u32x4 kr[2 * NT], vr[2 * NT];
     const auto load = [&](int t) {
-        const int tok = t * KVQ_TILE_TOKENS;
+        const int tok = t * KVQ_TILE_TOKENS, behind = __builtin_amdgcn_readfirstlane(S.nk - 1 - tok);
         const auto buffer = [&](const uint8_t* base, int row) {
-            const int64_t bytes = (int64_t)(S.nk - 1 - tok) * row + 2 * KVQ_D;
+            const int64_t bytes = (int64_t)behind * row + 2 * KVQ_D;
             return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + (int64_t)tok * row), 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
         };
         const __amdgpu_buffer_rsrc_t kb = buffer(kp, k_row), vb = buffer(vp, v_row);
@@ -160,9 +191,8 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         }
     };
 
-    // The pass over the tiles.  APART: for a range in which a masked tile holds an infinite or NaN value, every product of V keeps what
-    // a row does not see from it; such a range is taken a second time this way (as a branch inside one pass it costs all the others
-    // sixty registers).
+    // The pass over the tiles.  APART: a range in which a masked tile holds an infinite or NaN value of V is taken a second time, with zeros in
+    // the place of such values (as a branch inside one pass it costs all the others sixty registers).
     const auto pass = [&](auto apart) {
         constexpr bool APART = decltype(apart)::value;
         uint32_t nonfinite = 0;
@@ -172,11 +202,23 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         }
         __syncthreads();
         int buf = 0;
-        for (int t = t0; t < t1; t += NT, buf ^= 1) {
+        // the tiles that this wavefront's rows see; behind them it only loads (in a loop of its own: with the products under a condition in
+        // one loop the accumulators were copied once an iteration)
+        int t = t0;
+        const auto next = [&](bool more) {
+            if (more) {
+                if (APART) load(t + NT);  // (here it need not be on its way meanwhile, and there are no registers for it)
+                store(buf ^ 1);
+            }
+            __syncthreads();
+            buf ^= 1;
+            t += NT;
+        };
+        for (const int end = min(t1, (most + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS) - wt * TT; t < end;) {
             const bool more = t + NT < t1;
-            if (more) load(t + NT);
-            const int first = t + wt * TT, tok = first * KVQ_TILE_TOKENS;  // this wavefront's tiles
-            if (tok < most && first < t1) {
+            if (!APART && more) load(t + NT);
+            const int tok = (t + wt * TT) * KVQ_TILE_TOKENS;  // of this wavefront's tiles
+            {
                 const uint8_t* const kt = lds + buf * STAGE + wt * TT * (2 * KVQ_FLASH_TILE_BYTES);
                 const uint8_t* const vt = kt + KVQ_FLASH_TILE_BYTES;
                 float4v s[R][TT][2];
@@ -230,20 +272,10 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                 for (int x = 0; x < TT; ++x)
 #pragma unroll
                     for (int nt = 0; nt < 8; ++nt) {
-                        const half8 a = read_v(vt + x * (2 * KVQ_FLASH_TILE_BYTES), nt, lane);
+                        half8 a = read_v(vt + x * (2 * KVQ_FLASH_TILE_BYTES), nt, lane);
+                        if (APART) a = to_half8(finite_only(__builtin_bit_cast(u32x4, a)));
 #pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            if constexpr (APART) {
-                                const int end = min(limit[r], t1 * KVQ_TILE_TOKENS) - tok - x * KVQ_TILE_TOKENS - 8 * j;
-                                half8 seen;
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) seen[i] = i < end ? (_Float16)1.f : (_Float16)0.f;
-                                asm volatile("" ::: "memory");
-                                st.o[r][nt] = mfma_nonfinite(a, to_half8(p[r][x]), seen, st.o[r][nt]);
-                            } else {
-                                st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
-                            }
-                        }
+                        for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
                     }
                 if constexpr (!APART) {
                     __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
@@ -255,12 +287,17 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                     __builtin_amdgcn_sched_group_barrier(0x008, 4 * R, 1);
                 }
             }
-            if (more) store(buf ^ 1);
-            __syncthreads();
+            next(more);
+        }
+        while (t < t1) {
+            const bool more = t + NT < t1;
+            if (!APART && more) load(t + NT);
+            next(more);
         }
         return nonfinite;
     };
-    if (__syncthreads_or((int)pass(std::false_type{}))) {
+    const bool apart = __builtin_amdgcn_readfirstlane(__syncthreads_or((int)pass(std::false_type{}))) != 0;
+    if (apart) {
         st.clear();
         pass(std::true_type{});
     }
@@ -283,6 +320,14 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
 #pragma unroll
         for (int nt = 0; nt < 8; ++nt) store_out4(dst, A.out_fp32, 16 * nt + 4 * j, st.o[r][nt] * inv);
         if (A.lse && j == 0) A.lse[(int64_t)head * A.lse_hs + tok] = fine == 0.f ? -INFINITY : (st.m[r] + __builtin_amdgcn_logf(fine)) * 0.69314718055994530942f;
+    }
+    if (apart) {
+#pragma unroll 1
+        for (int r = 0; r < R; ++r) {
+            const int64_t group = parts_of<RB>(S, it.kv, it.block) + it.split * (RB / 16) + wm * R + r;
+            add_nonfinite(A, S, it.kv, row_of<RB>(A, S, it.block, wm * 16 * R + 16 * r + n), t0, t1,
+                          it.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
+        }
     }
 }
 

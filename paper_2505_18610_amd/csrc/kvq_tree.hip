@@ -348,51 +348,33 @@ __device__ inline void tile_products(State<R>& st, const uint32_t (&p)[R][1][4],
     }
 }
 
-// What infinite and NaN values of the nodes add to a row that sees them, behind everything else: nothing takes an infinity or a NaN out of
-// a sum again, so it is added to what the same lanes have stored, a partial result or an output.  The sums before it had zeros in the
-// place of such values: a key that a row does not see must not reach it, not even as zero times infinity.
+// What infinite and NaN values of the nodes add to a row that sees them, to what the same lanes have stored: a partial result or an output.
 __device__ inline void add_nonfinite(const TreeArgs& A, int unit, int row, float* part, int lane) {
     const int j = lane >> 4, n = lane & 15, at_row = min(row, A.rows - 1);
     const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq + (int64_t)(at_row % A.nodes) * A.words;
     const uint16_t* const v = reinterpret_cast<const uint16_t*>(A.v) + (int64_t)unit * A.nodes * KVQ_D;
 #pragma unroll 1
     for (int nt = 0; nt < 8; ++nt) {
-        float4v count[3] = {};  // infinities of either sign and NaNs among the nodes that the row sees
+        NonfiniteCount found;
 #pragma unroll 1
         for (int node0 = 0; node0 < A.nodes; node0 += KVQ_TILE_TOKENS) {
             const uint32_t word = mask[node0 / KVQ_TILE_TOKENS];
-            half8 kind[3], sees;
+            uint16_t w[8];
+            half8 sees;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int node = node0 + 8 * j + e;
-                const uint16_t w = node < A.nodes ? v[(int64_t)node * KVQ_D + 16 * nt + n] : (uint16_t)0;
-                kind[0][e] = w == 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
-                kind[1][e] = w == 0xfc00u ? (_Float16)1.f : (_Float16)0.f;
-                kind[2][e] = (w & 0x7fffu) > 0x7c00u ? (_Float16)1.f : (_Float16)0.f;
+                w[e] = node < A.nodes ? v[(int64_t)node * KVQ_D + 16 * nt + n] : (uint16_t)0;
                 sees[e] = ((word >> (8 * j + e)) & 1u) ? (_Float16)1.f : (_Float16)0.f;
             }
-#pragma unroll
-            for (int c = 0; c < 3; ++c) count[c] = mma(kind[c], sees, count[c]);
+            found.add(w, sees);
         }
-        float4v add;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            add[i] = (count[0][i] > 0.f ? INFINITY : 0.f) + (count[1][i] > 0.f ? -INFINITY : 0.f) + (count[2][i] > 0.f ? __builtin_nanf("") : 0.f);
-        if (part) {
-            reinterpret_cast<float4v*>(part)[nt * 64 + lane] += add;
-        } else if (row < A.rows) {
-            const int64_t at = ((int64_t)unit * A.rows + row) * KVQ_D + 16 * nt + 4 * j;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (A.out_fp32) static_cast<float*>(A.out)[at + i] += add[i];
-                else static_cast<_Float16*>(A.out)[at + i] = (_Float16)((float)static_cast<_Float16*>(A.out)[at + i] + add[i]);
-            }
-        }
+        if (part) reinterpret_cast<float4v*>(part)[nt * 64 + lane] += found.sum();
+        else if (row < A.rows) add_to_out4(A.out, A.out_fp32, ((int64_t)unit * A.rows + row) * KVQ_D + 16 * nt + 4 * j, found.sum());
     }
 }
 
-
-// ---- many rows: eight wavefronts that share the unpacked tiles
+// ---- many rows: wavefronts that share the unpacked tiles
 
 // One of the operands of a tile on its way to the workgroup's staging area in LDS, past the registers: the lanes' packed strings of K or of V
 // and 512 bytes of metadata (scales, zero points).  Strings of 16 bits are not staged, there is no room for them: they are
@@ -532,14 +514,7 @@ __device__ inline bool lay_out_v(const TreeArgs& A, int unit, int first, uint8_t
     const bool any = __any(bad != 0);
     if (any) {  // what is not finite is added at the very end, to the rows that see it
 #pragma unroll
-        for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t w = vo[nt][e];
-                if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
-                if ((w & 0x7c000000u) == 0x7c000000u) w &= 0x0000ffffu;
-                vo[nt][e] = w;
-            }
+        for (int nt = 0; nt < 8; ++nt) vo[nt] = finite_only(vo[nt]);
     }
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) *reinterpret_cast<u32x4*>(to + (nt * 64 + lane) * 16) = vo[nt];
