@@ -188,7 +188,7 @@ def kvq_append_decode_attention_batch(caches, layer, ks, vs, qs, outs, cos_sins=
 
 def _rows(begin):
     """Host array of row numbers."""
-    return (C.c_int32 * len(begin))(*[int(x) for x in begin])
+    return (C.c_int32 * len(begin))(*map(int, begin))
 
 
 def kvq_prompt_workspace_bytes(n_q_heads, n_kv_heads, q_begin, k_begin=None) -> int:
@@ -197,27 +197,30 @@ def kvq_prompt_workspace_bytes(n_q_heads, n_kv_heads, q_begin, k_begin=None) -> 
                                                          None if k_begin is None else _rows(k_begin), len(q_begin) - 1))
 
 
+def _packed(t, rows, heads):
+    """Token and head stride of a packed tensor [rows or more, heads, 128] (a dimension of one element may carry any stride)."""
+    n, h, d = t.shape
+    token, head, channel = t.stride()
+    assert n >= rows and h == heads and d == 128 and channel == 1
+    return 128 if n == 1 else token, 128 if h == 1 else head
+
+
 def kvq_prompt_attention(q, k, v, out, q_begin, k_begin=None, softmax_scale=0.0, lse=None, workspace=None, stream=None):
     """Causal attention of packed sequences.  q [rows, n_q_heads, 128], k, v [rows, n_kv_heads, 128]: fp16 device tensors of any
     strides (transposed and sliced ones too) whose channels follow one another; out like q, fp16 or fp32.  q_begin, k_begin:
     host sequences of n_seqs + 1 row numbers.  lse: fp32 device tensor [n_q_heads, q_begin[-1]] or None; workspace: uint8 device tensor or None."""
-    q_begin = [int(x) for x in q_begin]
-    k_begin = q_begin if k_begin is None else [int(x) for x in k_begin]
-    assert len(q_begin) == len(k_begin) >= 2
-    for t, rows, heads in ((q, q_begin[-1], q.shape[1]), (k, k_begin[-1], k.shape[1]), (v, k_begin[-1], k.shape[1]),
-                           (out, q_begin[-1], q.shape[1])):
-        assert t.dim() == 3 and t.shape[0] >= rows and t.shape[1] == heads and t.shape[2] == 128 and t.stride(2) == 1
-    assert all(t.dtype.itemsize == 2 for t in (q, k, v))
-    assert lse is None or (tuple(lse.shape) == (q.shape[1], q_begin[-1]) and lse.dtype.itemsize == 4)
-
-    def strides(t):  # a dimension of one element may carry any stride
-        return [128 if t.shape[d] == 1 else t.stride(d) for d in (0, 1)]
-
-    d = _Prompt(q.shape[1], k.shape[1], *strides(q), *strides(k), *strides(v), *strides(out),
-                1 if out.dtype.itemsize == 4 else 0, float(softmax_scale))
+    assert len(q_begin) >= 2 and (k_begin is None or len(k_begin) == len(q_begin))
+    qb = _rows(q_begin)
+    kb = qb if k_begin is None else _rows(k_begin)
+    heads, kv = q.shape[1], k.shape[1]
+    size = out.dtype.itemsize
+    assert q.dtype.itemsize == k.dtype.itemsize == v.dtype.itemsize == 2
+    assert lse is None or (tuple(lse.shape) == (heads, qb[-1]) and lse.dtype.itemsize == 4)
+    d = _Prompt(heads, kv, *_packed(q, qb[-1], heads), *_packed(k, kb[-1], kv), *_packed(v, kb[-1], kv), *_packed(out, qb[-1], heads),
+                size == 4, float(softmax_scale))
     st = load_library().kvq_prompt_attention(
-        C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), _rows(q_begin), _rows(k_begin),
-        len(q_begin) - 1, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+        C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), qb, kb, len(qb) - 1, _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream(stream))
     if st != KVQ_OK:
         raise KvqError(st, "kvq_prompt_attention")
 
@@ -328,13 +331,15 @@ class KvqCache:
         """Drafted tokens over the cache and each other.  q, out [batch, n_q_heads, n, 128], k, v [batch, n_kv_heads, n, 128];
         mask: int32 device tensor [n, words] for every sequence or [batch, n, words], bit j % 32 of word j // 32 of row i: node i
         sees node j.  workspace: uint8 device tensor of kvq_tree_workspace_bytes(n), or None."""
-        c, n = self.cfg, q.shape[2]
-        assert tuple(q.shape) == tuple(out.shape) == (c.batch, c.n_q_heads, n, 128)
-        assert tuple(k.shape) == tuple(v.shape) == (c.batch, c.n_kv_heads, n, 128)
-        assert all(t.dtype.itemsize == 2 for t in (q, k, v)) and mask.dtype.itemsize == 4
-        assert tuple(mask.shape) in ((n, (n + 31) // 32), (c.batch, n, (n + 31) // 32))
-        self._check(self.lib.kvq_tree_attention(self.handle, layer, _ptr(q), _ptr(k), _ptr(v), n, _ptr(mask), int(mask.dim() == 3),
-                                                _ptr(out), 1 if out.dtype.itemsize == 4 else 0, float(softmax_scale), _ptr(workspace),
+        c, shape = self.cfg, q.shape
+        n = shape[2]
+        words = (n + 31) // 32
+        size, mask_shape = out.dtype.itemsize, mask.shape
+        assert shape == out.shape == (c.batch, c.n_q_heads, n, 128) and k.shape == v.shape == (c.batch, c.n_kv_heads, n, 128)
+        assert q.dtype.itemsize == k.dtype.itemsize == v.dtype.itemsize == 2 and mask.dtype.itemsize == 4
+        assert mask_shape == (n, words) or mask_shape == (c.batch, n, words)
+        self._check(self.lib.kvq_tree_attention(self.handle, layer, _ptr(q), _ptr(k), _ptr(v), n, _ptr(mask), len(mask_shape) == 3,
+                                                _ptr(out), size == 4, float(softmax_scale), _ptr(workspace),
                                                 0 if workspace is None else workspace.numel(), _stream(stream)),
                     "kvq_tree_attention")
 
