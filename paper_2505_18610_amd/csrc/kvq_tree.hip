@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/kvq.h"
 #include "kvq_cache.h"
@@ -37,7 +38,6 @@ struct TreeArgs {
     int32_t per;             // tiles of a range
     int32_t node_tiles;      // what the nodes count for, in tiles: they come first in the line that is cut into ranges, in range 0
     int32_t groups;          // of 16 rows in a block
-    int32_t wt;              // many rows: wavefronts that share rows and take an iteration's tiles in turn
     int32_t out_fp32;
     float scale_log2;
     uint32_t flip;
@@ -201,20 +201,20 @@ __device__ inline void expand_tile(const Fetched& f, uint8_t* slot, uint8_t* met
 }
 
 // Query operands in pairs.  For the cache they are multiplied by the block's key factors (fp32 product, rounded to fp16, as for a decode
-// step); against the nodes' own keys they are what they are.
+// step); against the nodes' own keys they are what they are.  The rows of a wavefront's groups are `step` rows apart.
 template <int R>
-__device__ inline void ask_queries(u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, int lane) {  // (all loads first: they are the start of a chain)
+__device__ inline void ask_queries(u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, int step, int lane) {  // (all loads first: they are the start of a chain)
     const int j = lane >> 4, n = lane & 15;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = row0 + 16 * r + n;
+        const int row = row0 + step * r + n;
         const _Float16* src = A.q + ((int64_t)unit * A.rows + min(row, A.rows - 1)) * KVQ_D + 8 * j;
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) w[r][grp] = *reinterpret_cast<const u32x4*>(src + 32 * grp);
     }
 }
 template <int R>
-__device__ inline void set_queries(half8 (&q)[R][4], u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+__device__ inline void set_queries(half8 (&q)[R][4], u32x4 (&w)[R][4], const TreeArgs& A, int unit, int row0, int step, bool factors, int lane) {
     const int j = lane >> 4, n = lane & 15;
     if (factors && A.lambda) {
         const float* lam = A.lambda + (size_t)(unit % A.n_kv) * KVQ_D + 8 * j;
@@ -233,16 +233,16 @@ __device__ inline void set_queries(half8 (&q)[R][4], u32x4 (&w)[R][4], const Tre
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const bool real = row0 + 16 * r + n < A.rows;
+        const bool real = row0 + step * r + n < A.rows;
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) q[r][grp] = to_half8(real ? paired(w[r][grp] ^ A.flip) : u32x4{0, 0, 0, 0});
     }
 }
 template <int R>
-__device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, bool factors, int lane) {
+__device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int unit, int row0, int step, bool factors, int lane) {
     u32x4 w[R][4];
-    ask_queries<R>(w, A, unit, row0, lane);
-    set_queries<R>(q, w, A, unit, row0, factors, lane);
+    ask_queries<R>(w, A, unit, row0, step, lane);
+    set_queries<R>(q, w, A, unit, row0, step, factors, lane);
 }
 // Sums of q over the channels of each group, for the zero points: a high part in lane quarter 0, what it leaves in quarter 1, the B operand
 // of a product with 16 channels whose A operand repeats a token's four zero points.  Queries so large that a sum passes the fp16
@@ -283,8 +283,9 @@ __device__ inline float sum_queries(half8 (&q)[R][4], half4 (&qs)[R], int lane) 
     return grow;
 }
 
-// Scores of one tile of the cache in LDS: sums of codes times queries over the 32 channels of a scale, times it, plus the zero points' part.
-template <int R, bool I16>
+// Scores of one tile of the cache in LDS for the first RR groups of a wavefront: sums of codes times queries over the channels of a scale, times it, plus
+// the zero points' part.  SCALES: groups of channels of a token, 4, 2 or 1.
+template <int RR, bool I16, int SCALES, int R>
 __device__ inline void cache_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4], const half4 (&qs)[R], const uint8_t* slot, const uint8_t* meta,
                                     bool planes, int lane) {
     const int j = lane >> 4, n = lane & 15;
@@ -303,23 +304,30 @@ __device__ inline void cache_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4
             for (int e = 0; e < 8; ++e) scale[e] = pk_mul(scale[e], 0x5c005c00u);
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r][0][sub] = mma16(z, qs[r], zero);
+        for (int r = 0; r < RR; ++r) s[r][0][sub] = mma16(z, qs[r], zero);
 #pragma unroll
-        for (int grp = 0; grp < 4; ++grp) {
-            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16));
-            float4v part[R];
+        for (int g = 0; g < SCALES; ++g) {
+            float4v part[RR];
 #pragma unroll
-            for (int r = 0; r < R; ++r) part[r] = mma(a, q[r][grp], zero);
-            if (I16 && planes) {
-                const half8 b = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_TREE_K_LOW + ((sub * 4 + grp) * 64 + lane) * 16));
+            for (int r = 0; r < RR; ++r) part[r] = zero;
 #pragma unroll
-                for (int r = 0; r < R; ++r) part[r] = mma(b, q[r][grp], part[r]);
+            for (int grp = g * (4 / SCALES); grp < (g + 1) * (4 / SCALES); ++grp) {
+                const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + ((sub * 4 + grp) * 64 + lane) * 16));
+#pragma unroll
+                for (int r = 0; r < RR; ++r) part[r] = mma(a, q[r][grp], part[r]);
+                if (I16 && planes) {
+                    const half8 b = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_TREE_K_LOW + ((sub * 4 + grp) * 64 + lane) * 16));
+#pragma unroll
+                    for (int r = 0; r < RR; ++r) part[r] = mma(b, q[r][grp], part[r]);
+                }
             }
+            constexpr int last = 4 / SCALES - 1;  // (the four scales of a token are equal within a group)
+            const int at = g * (4 / SCALES) + last;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < RR; ++r)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    s[r][0][sub][i] = fmaf(mixf(scale[2 * i + (grp >> 1)], grp & 1), part[r][i], s[r][0][sub][i]);
+                    s[r][0][sub][i] = fmaf(mixf(scale[2 * i + (at >> 1)], at & 1), part[r][i], s[r][0][sub][i]);
         }
     }
 }
@@ -338,13 +346,13 @@ __device__ inline void node_scores(float4v (&s)[R][1][2], const half8 (&q)[R][4]
         }
     }
 }
-template <int R>
+template <int RR, int R>
 __device__ inline void tile_products(State<R>& st, const uint32_t (&p)[R][1][4], const uint8_t* slot, int lane) {
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
         const half8 a = to_half8(*reinterpret_cast<const u32x4*>(slot + KVQ_TREE_V + (nt * 64 + lane) * 16));
 #pragma unroll
-        for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
+        for (int r = 0; r < RR; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
     }
 }
 
@@ -442,7 +450,7 @@ __device__ inline void unpack_raw(const uint8_t* from, uint8_t* to, int lane) {
 // A staged operand into its place in a slot (slot: K operands, V operands, and the low bytes of K in the integer 16-bit tier); meta: where
 // the scales and zero points of K go, ones and zeros for a raw tile.
 template <bool I16>
-__device__ inline void unpack_staged(const Staged& f, const uint8_t* from, uint8_t* slot, uint8_t* meta, int part, int lane) {
+__device__ __attribute__((always_inline)) inline void unpack_staged(const Staged& f, const uint8_t* from, uint8_t* slot, uint8_t* meta, int part, int lane) {
     const uint32_t bits = f.bits;
     if (part == 0) {
         u32x4 m = *reinterpret_cast<const u32x4*>(from + KVQ_TREE_STAGE_META + (lane & 31) * 16);
@@ -527,24 +535,24 @@ __device__ inline void range_of(const TreeArgs& A, int split, int& t0, int& t1) 
     t1 = min(A.n_tiles, max(0, (split + 1) * A.per - A.node_tiles));
 }
 // Masks what lies behind the cache's last token.
-template <int R>
+template <int RR, int R>
 __device__ inline void mask_end(float4v (&s)[R][1][2], int end) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < RR; ++r)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (e >= end) s[r][0][e >> 2][e & 3] = -INFINITY;
 }
 // One tile of nodes that is laid out in a slot, for a wavefront's rows.
 template <int R>
-__device__ inline void take_nodes(State<R>& st, const half8 (&q)[R][4], const TreeArgs& A, const uint32_t* mask, const uint8_t* slot, int row0, int tile,
-                                  int lane) {
+__device__ inline void take_nodes(State<R>& st, const half8 (&q)[R][4], const TreeArgs& A, const uint32_t* mask, const uint8_t* slot, int row0, int step,
+                                  int tile, int lane) {
     const int j = lane >> 4, n = lane & 15;
     float4v s[R][1][2];
     node_scores<R>(s, q, slot, lane);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = min(row0 + 16 * r + n, A.rows - 1);
+        const int row = min(row0 + step * r + n, A.rows - 1);
         const int here = A.nodes - tile * KVQ_TILE_TOKENS;
         uint32_t w = mask[(int64_t)(row % A.nodes) * A.words + tile];
         if (here < KVQ_TILE_TOKENS) w &= (1u << here) - 1u;
@@ -556,17 +564,17 @@ __device__ inline void take_nodes(State<R>& st, const half8 (&q)[R][4], const Tr
     uint32_t p[R][1][4];
 #pragma unroll
     for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], A.scale_log2, false, p[r]);
-    tile_products<R>(st, p, slot, lane);
+    tile_products<R, R>(st, p, slot, lane);
 }
-// A wavefront's results: partial ones beyond one range, else the output.
+// A wavefront's results (its groups of 16 rows `apart` groups apart): partial ones beyond one range, else the output.
 template <int R>
-__device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int unit, int block, int split, int group0, bool nonfinite, int lane) {
+__device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int unit, int block, int split, int group0, int apart, bool nonfinite, int lane) {
     const int j = lane >> 4, n = lane & 15;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = (block * A.groups + group0 + r) * 16 + n;
+        const int row = (block * A.groups + group0 + apart * r) * 16 + n;
         if (A.splits > 1) {
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + r;
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + apart * r;
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
             continue;
         }
@@ -580,16 +588,16 @@ __device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int uni
     if (nonfinite) {
 #pragma unroll 1
         for (int r = 0; r < R; ++r) {
-            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + r;
-            add_nonfinite(A, unit, (block * A.groups + group0 + r) * 16 + n, A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
+            const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + apart * r;
+            add_nonfinite(A, unit, (block * A.groups + group0 + apart * r) * 16 + n, A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
         }
     }
 }
 
-// Many rows: 16 R for each of four wavefronts or, wt == 2, for each of two pairs.  An iteration unpacks two tiles, K and V of each in a
+// Many rows: 16 R for each of four wavefronts or, WT == 2, for each of two pairs, which take an iteration's tiles in turn.  An iteration unpacks two tiles, K and V of each in a
 // wavefront of its own, while the next ones are on their way into the staging area.  Three workgroups fit a compute unit, a wavefront of
 // each on every SIMD, so that one computes where another unpacks or waits at its barrier.
-template <int R, bool I16>
+template <int R, bool I16, int SCALES, int WT>
 __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const TreeArgs A) {
     constexpr int NT = 2, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
     static_assert(2 * KVQ_JOIN_BYTES <= NT * SLOT, "two pairs of wavefronts");
@@ -598,14 +606,15 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
     __shared__ __attribute__((aligned(16))) uint8_t staging[2 * NT * KVQ_TREE_STAGE];
     __shared__ uint32_t widths[NT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int WT = A.wt, wm = WT == 2 ? wave >> 1 : wave, wt = WT == 2 ? wave & 1 : 0;
+    const int wm = wave / WT, wt = wave % WT;
     const int part = wave & 1, own = wave >> 1;  // what this wavefront unpacks
     uint8_t* const slot = lds + own * SLOT;
     uint8_t* const stage = staging + wave * KVQ_TREE_STAGE;
     uint8_t* const meta = lds + NT * SLOT;
     // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
     const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
-    const int row0 = (block * A.groups + wm * R) * 16;  // of this wavefront
+    constexpr int apart = 4 / WT, step = 16 * apart;  // the wavefronts take turns at the groups of rows
+    const int row0 = (block * A.groups + wm) * 16;
     int t0, t1;
     range_of(A, split, t0, t1);
     State<R> st;
@@ -615,11 +624,15 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
         const KvqPageDesc first = entry_of(A, min(t0 + own, t1 - 1));
         KvqPageDesc next = entry_of(A, min(t0 + NT + own, t1 - 1));
         u32x4 w[R][4];
-        ask_queries<R>(w, A, unit, row0, lane);
+        ask_queries<R>(w, A, unit, row0, step, lane);
         Staged f = stage_tile(A, first, unit, min(t0 + own, t1 - 1), part, stage, lane);
-        set_queries<R>(q, w, A, unit, row0, true, lane);
+        set_queries<R>(q, w, A, unit, row0, step, true, lane);
         half4 qs[R];
         const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
+        // rows that do not fill a block leave wavefronts with fewer groups (RR), in a loop of their own (not in pairs, where the length of
+        // the chain counts and not what there is to do)
+        const auto pass = [&](auto groups) {
+        constexpr int RR = decltype(groups)::value;
         for (int t = t0; t < t1; t += NT) {
             wait_staged();
             int l = lane;  // (addresses derived from it are not to be kept over the loop: there are no registers for them)
@@ -639,18 +652,21 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
                 int l = lane;
                 asm volatile("" : "+v"(l));
                 float4v s[R][1][2];
-                cache_scores<R, I16>(s, q, qs, lds + i * SLOT, meta + i * 512, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, l);
+                cache_scores<RR, I16, SCALES, R>(s, q, qs, lds + i * SLOT, meta + i * 512, I16 && __builtin_amdgcn_readfirstlane(widths[i]) == 16, l);
                 if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
                     asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
-                    mask_end<R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
+                    mask_end<RR, R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
                 }
                 uint32_t p[R][1][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
-                tile_products<R>(st, p, lds + i * SLOT, l);
+                for (int r = 0; r < RR; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
+                tile_products<RR, R>(st, p, lds + i * SLOT, l);
             }
             lds_barrier();
         }
+        };
+        if (WT == 2 || row0 + step < A.rows) pass(std::integral_constant<int, R>{});
+        else pass(std::integral_constant<int, 1>{});
     }
     // the nodes among themselves
     bool nonfinite = false;
@@ -662,18 +678,18 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
                 nonfinite |= part == 0 ? lay_out_k(A, unit, (t + own) * KVQ_TILE_TOKENS, slot, lane)
                                        : lay_out_v(A, unit, (t + own) * KVQ_TILE_TOKENS, slot + KVQ_TREE_V, lane);
             __syncthreads();
-            load_queries<R>(q, A, unit, row0, false, lane);  // (here, where they do not take registers from the lines above)
+            load_queries<R>(q, A, unit, row0, step, false, lane);  // (here, where they do not take registers from the lines above)
 #pragma unroll 1
-            for (int i = wt; i < NT && t + i < tiles; i += WT) take_nodes<R>(st, q, A, mask, lds + i * SLOT, row0, t + i, lane);
+            for (int i = wt; i < NT && t + i < tiles; i += WT) take_nodes<R>(st, q, A, mask, lds + i * SLOT, row0, step, t + i, lane);
             __syncthreads();
         }
         nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
     }
-    if (WT == 2) {
+    if constexpr (WT == 2) {
         join_waves<R, 2, 2>(st, lds, wm, wt, lane);
         if (wt > 0) return;
     }
-    store_rows<R>(st, A, unit, block, split, wm * R, nonfinite, lane);
+    store_rows<R>(st, A, unit, block, split, wm, apart, nonfinite, lane);
 }
 
 // Few rows, 16 R: four wavefronts that all have them and take a tile each, unpacked for themselves alone.
@@ -699,8 +715,8 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
         u32x4 w[R][4];
         Fetched f;
         fetch_tile<I16>(f, A, first, unit, t0 + wave, lane_off);
-        ask_queries<R>(w, A, unit, row0, lane);
-        set_queries<R>(q, w, A, unit, row0, true, lane);
+        ask_queries<R>(w, A, unit, row0, 16, lane);
+        set_queries<R>(q, w, A, unit, row0, 16, true, lane);
         half4 qs[R];
         const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
         for (int tile = t0 + wave; tile < t1; tile += 4) {
@@ -712,36 +728,36 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
             }
             wave_lds_sync();
             float4v s[R][1][2];
-            cache_scores<R, I16>(s, q, qs, slot, meta_lds, planes, lane);
+            cache_scores<R, I16, 4, R>(s, q, qs, slot, meta_lds, planes, lane);
             if ((tile + 1) * KVQ_TILE_TOKENS > A.n_tokens) {
                 asm volatile("" ::: "memory");  // keep this a branch: the selects must not run for every tile
-                mask_end<R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
+                mask_end<R, R>(s, A.n_tokens - tile * KVQ_TILE_TOKENS - 8 * (lane >> 4));
             }
             uint32_t p[R][1][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
-            tile_products<R>(st, p, slot, lane);
+            tile_products<R, R>(st, p, slot, lane);
             wave_lds_sync();
         }
     }
     // the nodes among themselves
     bool nonfinite = false;
     if (split == 0) {
-        load_queries<R>(q, A, unit, row0, false, lane);
+        load_queries<R>(q, A, unit, row0, 16, false, lane);
         const uint32_t* const mask = A.mask + (int64_t)(unit / A.n_kv) * A.mask_seq;
         const int tiles = (A.nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
         for (int t = wave; t < tiles; t += 4) {
             lay_out_k(A, unit, t * KVQ_TILE_TOKENS, slot, lane);
             nonfinite |= lay_out_v(A, unit, t * KVQ_TILE_TOKENS, slot + KVQ_TREE_V, lane);
             wave_lds_sync();
-            take_nodes<R>(st, q, A, mask, slot, row0, t, lane);
+            take_nodes<R>(st, q, A, mask, slot, row0, 16, t, lane);
             wave_lds_sync();
         }
         nonfinite = __syncthreads_or(nonfinite ? 1 : 0) != 0;
     }
     join_waves<R, 1, 4>(st, lds, 0, wave, lane);
     if (wave > 0) return;
-    store_rows<R>(st, A, unit, block, split, 0, nonfinite, lane);
+    store_rows<R>(st, A, unit, block, split, 0, 1, nonfinite, lane);
 }
 
 // Joins the ranges of one group of 16 rows, 32 channels a workgroup.
@@ -802,6 +818,16 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
     p.bytes = p.splits > 1 ? one * (uint64_t)p.splits : 0;
     return p;
 }
+using Kernel = void (*)(TreeArgs);
+template <bool I16, int SCALES>
+Kernel kernel_of(const TreePlan& p) {
+    if (p.many) return p.wt == 2 ? kvq_tree_shared_kernel<2, I16, 4, 2> : kvq_tree_shared_kernel<2, I16, SCALES, 1>;
+    return p.groups > 1 ? kvq_tree_kernel<2, I16> : kvq_tree_kernel<1, I16>;
+}
+template <bool I16>
+Kernel kernel_of(const TreePlan& p, int group) {
+    return group == 32 ? kernel_of<I16, 4>(p) : kernel_of<I16, 2>(p);
+}
 bool nodes_ok(const kvq_cache* c, int nodes) { return c && nodes >= 1 && nodes <= KVQ_MAX_TREE_NODES; }
 
 }  // namespace
@@ -855,12 +881,10 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
     A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
     A.flip = scale < 0.f ? 0x80008000u : 0u;
     A.groups = plan.groups;
-    A.wt = plan.wt;
-    void (*const kernels[2][2][2])(TreeArgs) = {{{kvq_tree_kernel<1, false>, kvq_tree_kernel<1, true>}, {kvq_tree_kernel<2, false>, kvq_tree_kernel<2, true>}},
-                                                {{}, {kvq_tree_shared_kernel<2, false>, kvq_tree_shared_kernel<2, true>}}};
     const hipStream_t s = kvq_host::as_stream(hip_stream);
     const unsigned row_blocks = (unsigned)(c->units * plan.blocks);
-    hipLaunchKernelGGL(kernels[plan.many][plan.groups > 1][c->int16()], dim3(row_blocks * (unsigned)plan.splits),
+    const Kernel kernel = c->int16() ? kernel_of<true>(plan, c->cfg.group) : kernel_of<false>(plan, c->cfg.group);
+    hipLaunchKernelGGL(kernel, dim3(row_blocks * (unsigned)plan.splits),
                        dim3(256), 0, s, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (plan.splits > 1) {
