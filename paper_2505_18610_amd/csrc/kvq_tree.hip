@@ -573,6 +573,7 @@ __device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int uni
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = (block * A.groups + group0 + apart * r) * 16 + n;
+        if (group0 + apart * r >= A.groups || row - n >= A.rows) continue;  // (another block's, or nobody's)
         if (A.splits > 1) {
             const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + apart * r;
             store_partial(st, r, A.part + group * (KVQ_PART_BYTES / 4), lane);
@@ -588,22 +589,28 @@ __device__ inline void store_rows(const State<R>& st, const TreeArgs& A, int uni
     if (nonfinite) {
 #pragma unroll 1
         for (int r = 0; r < R; ++r) {
+            if (group0 + apart * r >= A.groups || (block * A.groups + group0 + apart * r) * 16 >= A.rows) continue;
             const int64_t group = ((int64_t)(unit * A.blocks + block) * A.splits + split) * A.groups + group0 + apart * r;
             add_nonfinite(A, unit, (block * A.groups + group0 + apart * r) * 16 + n, A.splits > 1 ? A.part + group * (KVQ_PART_BYTES / 4) : nullptr, lane);
         }
     }
 }
 
-// Many rows: 16 R for each of four wavefronts or, WT == 2, for each of two pairs, which take an iteration's tiles in turn.  An iteration unpacks two tiles, K and V of each in a
-// wavefront of its own, while the next ones are on their way into the staging area.  Three workgroups fit a compute unit, a wavefront of
-// each on every SIMD, so that one computes where another unpacks or waits at its barrier.
-template <int R, bool I16, int SCALES, int WT>
-__global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const TreeArgs A) {
-    constexpr int NT = 2, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
-    static_assert(2 * KVQ_JOIN_BYTES <= NT * SLOT, "two pairs of wavefronts");
+// Many rows: 16 R for each of W wavefronts or, WT == 2, for each of W / 2 pairs, which take an iteration's tiles in turn.  An iteration unpacks
+// W / 2 tiles, K and V of each in a wavefront of its own, while the next ones are on their way into the staging area.  Twelve
+// wavefronts fit a compute unit, three on every SIMD: in three workgroups or, where rows are enough, in one, which unpacks a tile for all of them.
+// What it spends its time on (64 drafted tokens x 40 heads over 4 x 32,768 tokens at all widths, 244 us with the joining kernel, 705 TFLOP/s
+// where an fp16 product of 8,192^3 reaches 1,290; with scales for 64 or 128 channels 219 us): issuing.  A tile of two groups of rows takes 36
+// products, 64 multiply-adds with the scales of K, some 70 instructions of softmax, and unpacking its share of a tile 150; products and vector
+// instructions of the wavefronts on a SIMD hardly overlap, no wavefront waits for memory (8 ns an iteration) and little for barriers.
+// Four wavefronts, three workgroups a compute unit: 288 us.
+template <int R, bool I16, int SCALES, int WT, int W>
+__global__ __launch_bounds__(64 * W, I16 ? 2 : 3) void kvq_tree_shared_kernel(const TreeArgs A) {
+    constexpr int NT = W / 2, SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
+    static_assert((WT == 1 && W % 4 == 0) || (W == 4 && 2 * KVQ_JOIN_BYTES <= NT * SLOT), "two pairs of wavefronts");
     // (the staging area is an object of its own: reads of the others then do not wait for what is on its way into it)
     __shared__ __attribute__((aligned(16))) uint8_t lds[NT * SLOT + NT * 512];
-    __shared__ __attribute__((aligned(16))) uint8_t staging[2 * NT * KVQ_TREE_STAGE];
+    __shared__ __attribute__((aligned(16))) uint8_t staging[W * KVQ_TREE_STAGE];
     __shared__ uint32_t widths[NT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WT, wt = wave % WT;
@@ -613,7 +620,7 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
     uint8_t* const meta = lds + NT * SLOT;
     // neighbouring workgroups are different units (and go to different XCDs); the row blocks of a range follow closely
     const int unit = blockIdx.x % A.units, x = blockIdx.x / A.units, block = x % A.blocks, split = x / A.blocks;
-    constexpr int apart = 4 / WT, step = 16 * apart;  // the wavefronts take turns at the groups of rows
+    constexpr int apart = W / WT, step = 16 * apart;  // the wavefronts take turns at the groups of rows
     const int row0 = (block * A.groups + wm) * 16;
     int t0, t1;
     range_of(A, split, t0, t1);
@@ -665,7 +672,7 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
             lds_barrier();
         }
         };
-        if (WT == 2 || row0 + step < A.rows) pass(std::integral_constant<int, R>{});
+        if (WT == 2 || (wm + apart < A.groups && row0 + step < A.rows)) pass(std::integral_constant<int, R>{});
         else pass(std::integral_constant<int, 1>{});
     }
     // the nodes among themselves
@@ -693,6 +700,8 @@ __global__ __launch_bounds__(256, I16 ? 2 : 3) void kvq_tree_shared_kernel(const
 }
 
 // Few rows, 16 R: four wavefronts that all have them and take a tile each, unpacked for themselves alone.
+// 4 drafted tokens x 8 heads over 4,096 tokens: 7.8 us and 2.9 to join 17 ranges, a chain of trips to memory (arguments, page entry, tile) and of
+// two tiles' work.
 template <int R, bool I16>
 __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeArgs A) {
     constexpr int SLOT = (I16 ? 3 : 2) * KVQ_FLASH_TILE_BYTES;
@@ -784,7 +793,7 @@ constexpr int kNodeTiles = 4;   // what the nodes cost beside their tiles, in ti
 constexpr int kLeastTiles = 8;  // of a range: two a wavefront of the kernel for few rows, or four iterations of the other
 struct TreePlan {
     bool many;
-    int groups, wt, blocks, splits, per, node_tiles;  // groups of 16 rows in a block
+    int waves, groups, wt, blocks, splits, per, node_tiles;  // groups of 16 rows in a block
     uint64_t bytes;
 };
 // workspace: bytes there are for partial results
@@ -796,14 +805,21 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
         // pairs where rows are few or there is so little to do that the length of the chain counts: 112 rows x 282 tiles x 4 units 27.4 us
         // and 24.7 in pairs, 256 x 128 x 2 21.4 and 18.7; 200 x 938 x 8 70 and 78, 448 x 256 x 16 77 and 83
         p.wt = rows <= 64 || (int64_t)c->units * ((rows + 127) / 128) * n_tiles <= 4096 ? 2 : 1;
-        p.groups = 8 / p.wt;
+        // a tile is unpacked once a block: twelve wavefronts where they have enough rows (320 rows x 1,026 tiles x 32 units 288 us with four and
+        // 247 with twelve, 272 x 938 x 32 257 and 216, 256 x 938 x 32 196 and 195, 200 x 4,096 x 8 205 and 212) and iterations
+        // of six tiles (320 x 94 x 32 49 and 52, 288 x 157 x 32 65 and 61)
+        const int groups = (rows + 15) / 16, large = (groups + 23) / 24;
+        const bool twelve = p.wt == 1 && !c->int16() && groups > 16 * large && (int64_t)n_tiles * c->units * large >= 18 * (int64_t)c->target_workgroups;
+        p.waves = twelve ? 12 : 4;
+        p.groups = twelve ? (groups + large - 1) / large : 8 / p.wt;
         p.blocks = (rows + 16 * p.groups - 1) / (16 * p.groups);
     } else {
         p.groups = rows <= 16 ? 1 : 2;
         p.blocks = p.wt = 1;
+        p.waves = 4;
     }
     const int64_t wgs = (int64_t)c->units * p.blocks;
-    const int64_t want = std::max<int64_t>(1, (p.many && !c->int16() ? 3 : 2) * c->target_workgroups / wgs);
+    const int64_t want = std::max<int64_t>(1, (p.many && !c->int16() ? 12 / p.waves : 2) * c->target_workgroups / wgs);
     const uint64_t one = (uint64_t)wgs * p.groups * KVQ_PART_BYTES;  // a range's partial results
     const int64_t room = (int64_t)std::min<uint64_t>(workspace / one, kMostSplits);
     p.node_tiles = ((nodes + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS + kNodeTiles + kLeastTiles - 1) / kLeastTiles * kLeastTiles;
@@ -812,8 +828,8 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
     const int64_t tiles = n_tiles + p.node_tiles, cut = std::max<int64_t>(tiles / kLeastTiles, std::min<int64_t>(2 * tiles / kLeastTiles, 32));
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(cut, room)));
     if (n_tiles < kLeastTiles) p.splits = 1;
-    const int round = p.many ? 1 : 3;  // (in whole iterations: two tiles, or one a wavefront)
-    p.per = ((int)((tiles + p.splits - 1) / p.splits) + round) & ~round;
+    const int round = p.many ? p.waves / 2 : 4;  // (in whole iterations: half a tile a wavefront, or one)
+    p.per = ((int)((tiles + p.splits - 1) / p.splits) + round - 1) / round * round;
     p.splits = p.splits > 1 ? (int)((tiles + p.per - 1) / p.per) : 1;
     p.bytes = p.splits > 1 ? one * (uint64_t)p.splits : 0;
     return p;
@@ -821,7 +837,10 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
 using Kernel = void (*)(TreeArgs);
 template <bool I16, int SCALES>
 Kernel kernel_of(const TreePlan& p) {
-    if (p.many) return p.wt == 2 ? kvq_tree_shared_kernel<2, I16, 4, 2> : kvq_tree_shared_kernel<2, I16, SCALES, 1>;
+    if (p.many && p.wt == 2) return kvq_tree_shared_kernel<2, I16, 4, 2, 4>;
+    if constexpr (!I16)
+        if (p.many && p.waves == 12) return kvq_tree_shared_kernel<2, I16, SCALES, 1, 12>;
+    if (p.many) return kvq_tree_shared_kernel<2, I16, SCALES, 1, 4>;
     return p.groups > 1 ? kvq_tree_kernel<2, I16> : kvq_tree_kernel<1, I16>;
 }
 template <bool I16>
@@ -885,7 +904,7 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev
     const unsigned row_blocks = (unsigned)(c->units * plan.blocks);
     const Kernel kernel = c->int16() ? kernel_of<true>(plan, c->cfg.group) : kernel_of<false>(plan, c->cfg.group);
     hipLaunchKernelGGL(kernel, dim3(row_blocks * (unsigned)plan.splits),
-                       dim3(256), 0, s, A);
+                       dim3(64u * (unsigned)plan.waves), 0, s, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (plan.splits > 1) {
         hipLaunchKernelGGL(kvq_tree_merge_kernel, dim3(row_blocks * (unsigned)plan.groups * 4), dim3(512), 0, s, A);
