@@ -279,7 +279,7 @@ __device__ inline void read_v(const ReadArgs& A, const uint8_t* code, const uint
 }
 // A wavefront takes K or V of one tile of one unit.  Rows are put together in LDS because a lane holds eight channels of a token or eight tokens of
 // a channel, and stores of whole lines are what bounds it: a block of 4 x 32,768 tokens at all widths, 706 MB read and written, 152 us from
-// memory (4.6 TB/s; a copy reaches 5.1).  2,440 tokens of 8 heads 6.6 us, one launch's chain of trips.
+// memory (4.6 TB/s; a copy reaches 5.1).  2,372 tokens of 8 heads 6.5 us, one launch's chain of trips.
 __global__ __launch_bounds__(256) void kvq_read_kernel(const ReadArgs A) {
     __shared__ __attribute__((aligned(16))) float lds[4][KVQ_TILE_TOKENS * KVQ_READ_PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

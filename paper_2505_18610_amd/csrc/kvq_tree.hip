@@ -855,7 +855,10 @@ extern "C" {
 
 uint64_t kvq_tree_workspace_bytes(const kvq_cache_t* c, int32_t n_nodes) {
     if (!nodes_ok(c, n_nodes)) return 0;
-    return plan_tree(c, n_nodes, (c->cfg.max_tokens + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS, UINT64_MAX).bytes;
+    uint64_t most = 0;  // (a shorter cache may be cut otherwise)
+    for (int n_tiles = (c->cfg.max_tokens + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS; n_tiles; n_tiles /= 2)
+        most = std::max(most, plan_tree(c, n_nodes, n_tiles, UINT64_MAX).bytes);
+    return most;
 }
 
 kvq_status_t kvq_tree_attention(kvq_cache_t* c, int32_t layer, const void* q_dev, const void* k_dev, const void* v_dev, int32_t n_nodes,
