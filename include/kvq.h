@@ -114,7 +114,8 @@ void kvq_cache_destroy(kvq_cache_t* cache);
  *   k_dev, v_dev: fp16 [batch, n_kv_heads, n_new, head_dim], contiguous; keys already carry RoPE.
  *   n_new < 2^23 tokens per call (KVQ_E_INVALID beyond; append longer inputs in pieces).
  *   entry_bits: 0 = the policy's entry width (16 while a window is configured or under OLDEST_FIRST, else
- *   the block's current width); 16/8/4/2 = store at exactly that width (state construction).  A width that
+ *   the block's current width or, where kvq_cache_fork or kvq_cache_truncate has ended inside a page, that page's width
+ *   until a call ends with a full page); 16/8/4/2 = store at exactly that width (state construction).  A width that
  *   differs from the partially filled last page's width is KVQ_E_STATE.
  *   Quantized widths use asymmetric min-max per group: Z = min, S = (max - Z)/(2^b - 1) in fp32 rounded to
  *   fp16, code = rne((x - Z)/S) with the stored S, clamped; S == 0 gives code 0.

@@ -141,6 +141,7 @@ struct Layer {
     bool reparam = false;  // keys stored as K / lambda, queries multiplied by lambda (Sec. 3.3)
     bool poisoned = false; // an enqueue failed after the host tables had been updated: unusable until kvq_cache_reset
     std::vector<Page> pages;
+    int resumed = -1;      // the page inside which a fork or a cut has ended; see plan_append
     // the pages as runs of one width, of the state runs_version; see runs_of
     mutable std::vector<Run> runs;
     mutable uint64_t runs_version = ~0ull;
@@ -209,6 +210,8 @@ struct kvq_cache {
 
 namespace kvq_host {
 
+// Whether tokens enter at 16 bits by the policy, whatever the block's width.
+inline bool appends_at_16(const kvq_cache* c) { return c->cfg.policy == KVQ_POLICY_OLDEST_FIRST || c->cfg.window > 0; }
 inline hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
 // kvq_host.cpp
 kvq_status_t upload(kvq_cache* c, void* dst_dev, const void* src, uint64_t bytes, hipStream_t s);

@@ -464,6 +464,7 @@ struct DeferredAppend {
 // the append evicts and the width they go to.
 struct AppendPlan {
     int e = 16, T = 0, n_pages = 0, bcur = 16;
+    bool resumes = false;  // at the width of the page inside which a fork or a cut has ended
     std::vector<int> evicted;
 };
 
@@ -474,7 +475,10 @@ kvq_status_t plan_append(const kvq_cache_t* c, int32_t layer, int32_t n_new, int
     if (L.poisoned) return KVQ_E_STATE;
     if ((int64_t)L.T + n_new > cfg.max_tokens) return KVQ_E_STATE;
     int e = entry_bits;
-    if (e == 0) e = (cfg.policy == KVQ_POLICY_OLDEST_FIRST || cfg.window > 0) ? 16 : current_bits(c, L);
+    // A page that a fork or a cut has left partly filled may be wider than the block's current width: it is filled as it is, with all
+    // tokens of the call (a launch stores one width), and so is the page inside which such a call ends.
+    pl.resumes = e == 0 && !appends_at_16(c) && L.T % P != 0 && L.resumed == L.T / P;
+    if (e == 0) e = appends_at_16(c) ? 16 : pl.resumes ? L.pages.back().bits : current_bits(c, L);
     if (L.T % P != 0 && L.pages.back().bits != e) return KVQ_E_STATE;
     const bool evict = entry_bits == 0 && cfg.policy == KVQ_POLICY_PAPER && cfg.window > 0;
     pl.e = e;
@@ -563,6 +567,7 @@ kvq_status_t commit_append(kvq_cache_t* c, int32_t layer, const AppendPlan& pl, 
     for (const Page& p : bl.fresh) L.pages.push_back(p);
     for (size_t i = (size_t)(t_old / P); i < L.pages.size(); ++i) L.pages[i].n = std::min(P, T - (int)i * P);
     L.T = T;
+    if (pl.resumes) L.resumed = T % P ? T / P : -1;
     if (L.runs_version == L.version && !L.runs.empty() && L.runs.back().bits == e) {  // new pages have the width e
         L.runs.back().page_end = (int)L.pages.size();
         L.runs_version = L.version + 1;
@@ -657,8 +662,7 @@ kvq_status_t kvq_progressive_requant(kvq_cache_t* c, int32_t layer, int32_t segm
         if (sg.bits == 2) return KVQ_E_STATE;
         // A run that ends in the partly filled last page: lowering it would leave that page at a width other than the
         // one the policy appends at (16 bits under OLDEST_FIRST or with a window), and no token could follow.
-        if (sg.token_end == L.T && L.T % P != 0 && (cfg.policy == KVQ_POLICY_OLDEST_FIRST || cfg.window > 0))
-            return KVQ_E_STATE;
+        if (sg.token_end == L.T && L.T % P != 0 && appends_at_16(c)) return KVQ_E_STATE;
         std::vector<Lowering> low;
         for (int i = sg.token_begin / P; i < (sg.token_end + P - 1) / P; ++i) low.push_back(Lowering{i, sg.bits, sg.bits / 2});
         st = run_lowerings(c, layer, low, s);
@@ -1420,6 +1424,7 @@ void kvq_host::empty_block(kvq_cache* c, Layer& L) {
     }
     L.pages.clear();
     L.T = 0;
+    L.resumed = -1;
     L.version++;
     L.plan_tiles = -1;
     L.poisoned = false;

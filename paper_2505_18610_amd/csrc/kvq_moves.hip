@@ -321,7 +321,7 @@ void release_pages(kvq_cache* c, const std::vector<Page>& pages, size_t from, si
 // append at: no token could follow.
 bool cut_strands_page(const kvq_cache* c, const Layer& L, int n) {
     if (n == 0 || n >= L.T || n % c->cfg.page_tokens == 0) return false;
-    return (c->cfg.policy == KVQ_POLICY_OLDEST_FIRST || c->cfg.window > 0) && L.pages[(size_t)(n / c->cfg.page_tokens)].bits != 16;
+    return kvq_host::appends_at_16(c) && L.pages[(size_t)(n / c->cfg.page_tokens)].bits != 16;
 }
 hipError_t clear_tail(const kvq_cache* c, const Page& p, int n, hipStream_t s) {
     const int in_page = n % c->cfg.page_tokens;  // (not 0)
@@ -334,6 +334,7 @@ void set_pages(kvq_cache* c, Layer& L, int n) {  // the block's pages hold n tok
     const int P = c->cfg.page_tokens;
     for (size_t i = 0; i < L.pages.size(); ++i) L.pages[i].n = std::min(P, n - (int)i * P);
     L.T = n;
+    L.resumed = n % P ? n / P : -1;
     L.version++;
     L.plan_tiles = -1;
 }
