@@ -277,8 +277,9 @@ kvq_status_t kvq_tree_attention(kvq_cache_t* cache, int32_t layer, const void* q
  *   that is not) and may differ in everything else.  dst may be src: the sequences change places inside the cache, through fresh
  *   pages.  Pages of dst's old block are written over where the widths agree; the others are taken from the arena before anything
  *   changes, beside the old block (KVQ_E_OOM: empty dst's block first if it need not stay).  KVQ_E_BUDGET if dst's block would
- *   exceed its budget, KVQ_E_STATE if n_tokens exceeds what src holds or dst's max_tokens, or if fewer tokens than src holds would
- *   end inside a page below 16 bits while dst's policy appends at 16.  On these dst is unchanged.
+ *   exceed its budget, KVQ_E_STATE if n_tokens exceeds what src holds or dst's max_tokens, or if they end inside a page below 16 bits
+ *   while dst's policy appends at 16, so that no token could follow (all of a block that none can follow in src either may be
+ *   forked).  On these dst is unchanged.
  *   Enqueues kernels on the stream, which both caches' calls are issued on; not for capture. */
 kvq_status_t kvq_cache_fork(kvq_cache_t* dst, kvq_cache_t* src, int32_t layer, const int32_t* seq_map_dev, int32_t n_tokens,
                             void* hip_stream);

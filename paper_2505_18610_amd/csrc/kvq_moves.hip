@@ -317,11 +317,11 @@ void release_pages(kvq_cache* c, const std::vector<Page>& pages, size_t from, si
         if (c->has_meta(pages[i].bits)) c->buddy.release(pages[i].meta_unit, 0);
     }
 }
-// Whether a cut of the block's tokens to n would leave cache c with a last page that is partly filled at a width that c's policy does not
-// append at: no token could follow.
-bool cut_strands_page(const kvq_cache* c, const Layer& L, int n) {
-    if (n == 0 || n >= L.T || n % c->cfg.page_tokens == 0) return false;
-    return kvq_host::appends_at_16(c) && L.pages[(size_t)(n / c->cfg.page_tokens)].bits != 16;
+// Whether the first n tokens of a block of `from` would leave cache c with a last page that is partly filled below 16 bits while c's policy
+// appends at 16: no token could follow.  (A copy of all of a block that no token can follow either is what was asked for.)
+bool strands_page(const kvq_cache* c, const kvq_cache* from, const Layer& L, int n) {
+    if (n % c->cfg.page_tokens == 0 || !kvq_host::appends_at_16(c) || L.pages[(size_t)(n / c->cfg.page_tokens)].bits == 16) return false;
+    return n < L.T || !kvq_host::appends_at_16(from);
 }
 hipError_t clear_tail(const kvq_cache* c, const Page& p, int n, hipStream_t s) {
     const int in_page = n % c->cfg.page_tokens;  // (not 0)
@@ -349,7 +349,7 @@ kvq_status_t fork_impl(kvq_cache* dst, kvq_cache* src, int32_t layer, const int3
     Layer &S = src->layers[(size_t)layer], &D = dst->layers[(size_t)layer];
     if (S.poisoned || D.poisoned) return KVQ_E_STATE;
     const int held = S.T, n = n_tokens < 0 ? held : n_tokens, P = a.page_tokens;
-    if (n > held || n > b.max_tokens || cut_strands_page(dst, S, n)) return KVQ_E_STATE;
+    if (n > held || n > b.max_tokens || strands_page(dst, src, S, n)) return KVQ_E_STATE;
     const size_t n_pages = (size_t)((n + P - 1) / P);
     uint64_t bytes = 0;
     for (size_t i = 0; i < n_pages; ++i)
@@ -466,7 +466,7 @@ kvq_status_t kvq_cache_fork(kvq_cache_t* dst, kvq_cache_t* src, int32_t layer, c
 kvq_status_t kvq_cache_truncate(kvq_cache_t* c, int32_t layer, int32_t n_tokens, void* hip_stream) {
     if (!c || layer < 0 || layer >= c->cfg.n_layers || n_tokens < 0) return KVQ_E_INVALID;
     Layer& L = c->layers[(size_t)layer];
-    if (L.poisoned || n_tokens > L.T || cut_strands_page(c, L, n_tokens)) return KVQ_E_STATE;
+    if (L.poisoned || n_tokens > L.T || strands_page(c, c, L, n_tokens)) return KVQ_E_STATE;
     if (n_tokens == L.T) return KVQ_OK;
     const int P = c->cfg.page_tokens;
     const size_t n_pages = (size_t)((n_tokens + P - 1) / P);

@@ -84,3 +84,24 @@ def test_emptied_blocks_forget():
     for n, bits in ((128, 2), (22, 8)):
         assert append(c, n, bits) == kq.KVQ_OK
     assert append(c, 1) == kq.KVQ_E_STATE  # page 2 is not the one that was cut
+
+
+@pytest.mark.parametrize("kind", [dict(policy=kq.KVQ_POLICY_OLDEST_FIRST), dict(window=64)])
+@pytest.mark.parametrize("n", [100, 128])
+def test_a_whole_block_into_a_cache_that_appends_at_16(kind, n):
+    """100 tokens end inside a page of 8 bits, in which the source goes on and the other cache could not."""
+    s, d = make(tiers=[(n, 16)]), make(tiers=[(10, 16)], **kind)
+    s.kvq_progressive_requant(0)
+    before = d.kvq_cache_describe(0), d.kvq_cache_arena_free_bytes()
+    if n % 64:
+        for m in (-1, n, 70):
+            assert fork(d, s, n=m) == kq.KVQ_E_STATE
+        assert (d.kvq_cache_describe(0), d.kvq_cache_arena_free_bytes()) == before
+        assert fork(d, s, n=64) == kq.KVQ_OK and append(d, 1) == kq.KVQ_OK and widths(d) == [8] * 64 + [16]
+    else:
+        assert fork(d, s) == kq.KVQ_OK and append(d, 1) == kq.KVQ_OK and widths(d) == [8] * n + [16]
+    assert append(s, 1) == kq.KVQ_OK
+    # a block that no such append follows where it is may be copied whole: what is left of it is to be read
+    s = make(tiers=[(100, 8)], **kind)
+    assert append(s, 1) == kq.KVQ_E_STATE
+    assert fork(make(**kind), s) == kq.KVQ_OK and fork(s, s, m=A) == kq.KVQ_OK
