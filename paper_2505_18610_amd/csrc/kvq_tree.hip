@@ -794,7 +794,8 @@ constexpr int kLeastTiles = 8;  // of a range: two a wavefront of the kernel for
 struct TreePlan {
     bool many;
     int waves, groups, wt, blocks, splits, per, node_tiles;  // groups of 16 rows in a block
-    uint64_t bytes;
+    uint64_t bytes;  // of the partial results, no more than `most`: those of as many ranges as this kernel may take for a cache that is not longer
+    uint64_t most;
 };
 // workspace: bytes there are for partial results
 TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspace) {
@@ -828,6 +829,7 @@ TreePlan plan_tree(const kvq_cache* c, int nodes, int n_tiles, uint64_t workspac
     const int64_t tiles = n_tiles + p.node_tiles, cut = std::max<int64_t>(tiles / kLeastTiles, std::min<int64_t>(2 * tiles / kLeastTiles, 32));
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::min<int64_t>(cut, room)));
     if (n_tiles < kLeastTiles) p.splits = 1;
+    p.most = p.splits > 1 ? one * (uint64_t)p.splits : 0;
     const int round = p.many ? p.waves / 2 : 4;  // (in whole iterations: half a tile a wavefront, or one)
     p.per = ((int)((tiles + p.splits - 1) / p.splits) + round - 1) / round * round;
     p.splits = p.splits > 1 ? (int)((tiles + p.per - 1) / p.per) : 1;
@@ -855,9 +857,21 @@ extern "C" {
 
 uint64_t kvq_tree_workspace_bytes(const kvq_cache_t* c, int32_t n_nodes) {
     if (!nodes_ok(c, n_nodes)) return 0;
-    uint64_t most = 0;  // (a shorter cache may be cut otherwise)
-    for (int n_tiles = (c->cfg.max_tokens + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS; n_tiles; n_tiles /= 2)
-        most = std::max(most, plan_tree(c, n_nodes, n_tiles, UINT64_MAX).bytes);
+    // A shorter cache may take another kernel, and fewer tiles may be cut into more ranges, which are of whole iterations.  Before that rounding
+    // ranges only become more with the tiles, so the longest cache of each kernel decides; kernels change at no more than two lengths.
+    const auto plan = [&](int n_tiles) { return plan_tree(c, n_nodes, n_tiles, UINT64_MAX); };
+    const auto same = [](const TreePlan& a, const TreePlan& b) { return a.wt == b.wt && a.waves == b.waves && a.groups == b.groups; };
+    uint64_t most = 0;
+    for (int n_tiles = (c->cfg.max_tokens + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS; n_tiles > 0;) {
+        const TreePlan p = plan(n_tiles);
+        most = std::max(most, p.most);
+        int shorter = 0, longer = n_tiles;  // the longest cache that takes another kernel, 0: none
+        while (longer - shorter > 1) {
+            const int middle = shorter + (longer - shorter) / 2;
+            (same(plan(middle), p) ? longer : shorter) = middle;
+        }
+        n_tiles = shorter;
+    }
     return most;
 }
 
