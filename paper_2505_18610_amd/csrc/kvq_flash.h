@@ -7,10 +7,13 @@
 // after exponentiation are the B operand of the second product as they stand: nothing crosses lanes between the products.  A
 // wavefront carries R groups of 16 rows, so an operand read from LDS serves R products.
 //
-// Statistics, in 32 bits: a reference per row in log2 units, which follows the row's maximum when that is more than 2^8 above it (a
-// rescaling of the accumulators then; with every new maximum 38 % of the tiles of 128 had one, 20 instructions a tile and group of
-// rows), and the sum of the probabilities as rounded to fp16 for the second product, so that a row that one key dominates gets its
-// values back as they are.  Where the caller asks for the log of the sum it is taken from the unrounded ones beside it.
+// Statistics, in 32 bits: a reference per row in log2 units, which is set 2^KVQ_BELOW below the row's maximum and follows it when that is more
+// than 2^KVQ_FOLLOW above where it was (a rescaling of the accumulators then; with every new maximum 38 % of the tiles of 128 had one, 20
+// instructions a tile and group of rows), and the sum of the probabilities as rounded to fp16 for the second product, so that a row
+// that one key dominates gets its values back as they are.  Where the caller asks for the log of the sum it is taken from the unrounded ones
+// beside it.  Probabilities so lie below 2^(KVQ_BELOW + KVQ_FOLLOW) = 2^15, within fp16, and what the rounding of a small one loses, 2^-25 at
+// most, is 2^-(25 + KVQ_BELOW) of the weight of the row's leading key (with the reference at the maximum 131,072 equal keys 17 nats below
+// a leading one were 44 % too heavy and 18 nats below it lost; 0.1 % and 0.9 % now).  Half a per cent of a prompt's time, 1 % of a tree's.
 #ifndef KVQ_FLASH_H
 #define KVQ_FLASH_H
 
@@ -28,6 +31,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
 #define KVQ_FLASH_TILE_BYTES 8192  // one fp16 K or V tile in LDS
+#define KVQ_BELOW 7.f
+#define KVQ_FOLLOW 8.f
 
 #ifdef KVQ_NO_ARITHMETIC  // the measurement build (build.py) loads tiles and computes on none
 __device__ inline float4v mma(half8, half8, float4v c) { return c; }
@@ -71,7 +76,7 @@ struct State {
     }
 };
 
-// What is subtracted from a score: the maximum, or zero while nothing has been seen (exp2(-inf - -inf) would be NaN).
+// What is subtracted from a score: the reference, or zero while nothing has been seen (exp2(-inf - -inf) would be NaN).
 __device__ inline float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // Probabilities of TT tiles for row group r from raw scores s (before the scale), masked ones at -inf; p in the order of the V
@@ -86,8 +91,8 @@ __device__ inline void softmax_group(State<R>& st, int r, const float4v (&s)[TT]
 #pragma unroll
             for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, s[t][sub][i]);
     lmax *= scale_log2;
-    if (__any(lmax > st.m[r] + 8.f)) {
-        const float m_new = fmaxf(st.m[r], quarters_max(lmax));
+    if (__any(lmax > st.m[r] + (KVQ_BELOW + KVQ_FOLLOW))) {
+        const float m_new = fmaxf(st.m[r], quarters_max(lmax) - KVQ_BELOW);
         const float alpha = __builtin_amdgcn_exp2f(st.m[r] - reference_of(m_new));  // 0 for the first scores
         st.l[r] *= alpha;
         if (FINE) st.fine[r] *= alpha;
