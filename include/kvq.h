@@ -220,7 +220,8 @@ kvq_status_t kvq_append_decode_attention_batch(kvq_cache_t* const* caches, int32
  *   NULL: the same as the queries').  Its n_q queries are the last of its n_k keys: query i sees the keys 0 .. i + n_k - n_q,
  *     out[i, h, :] = softmax_j( q[i, h, :] . k[j, h / g, :] * softmax_scale ) v[j, h / g, :],
  *   so n_q = n_k is a whole prompt, n_q < n_k a chunk behind the keys of earlier ones, n_q = 1 a decode step.  A query that sees no
- *   key (n_k < n_q) gets zeros and lse = -inf.  Keys that a query does not see do not reach it, whatever they hold.
+ *   key (n_k < n_q) gets zeros and lse = -inf.  Keys that a query does not see do not reach it, whatever they hold; an infinite or
+ *   NaN value that it sees does, however little it weighs.
  *   q_dev, out_dev: row (t, h) at t * *_token_stride + h * *_head_stride elements, 128 consecutive ones; k_dev, v_dev the same
  *   with KV heads.  Strides are multiples of 8 and not negative (a head stride of 0 in inputs: broadcast), addresses of
  *   16 bytes; the token strides of k and v are 128 .. 2^22 - 1.  Output fp16, or

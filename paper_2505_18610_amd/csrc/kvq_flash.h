@@ -308,14 +308,16 @@ __device__ inline bool join_partials(JoinLds& lds, const float* part, int64_t st
     x.m = -INFINITY;
     for (int s = 0; s < n_parts; ++s) x.m = fmaxf(x.m, lds.w[s][n]);
     const float ref = reference_of(x.m);
+    // (never zero: an infinity among the values that a row sees stays one, whatever its range weighs; of finite sums 2^-126 leaves nothing)
+    const auto weight = [&](int s) { return fmaxf(__builtin_amdgcn_exp2f(lds.w[s][n] - ref), 0x1p-126f); };
     x.o = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int s = slice + 4 * k;
-        if (s < n_parts) x.o += o[k] * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+        if (s < n_parts) x.o += o[k] * weight(s);
     }
     for (int s = slice + 32; s < n_parts; s += 4)
-        x.o += *reinterpret_cast<const float4v*>(part + s * step + (x.nt * 64 + lane) * 4) * __builtin_amdgcn_exp2f(lds.w[s][n] - ref);
+        x.o += *reinterpret_cast<const float4v*>(part + s * step + (x.nt * 64 + lane) * 4) * weight(s);
     if (slice) lds.o[wave - 2][lane] = x.o;
     __syncthreads();
     if (slice) return false;

@@ -195,11 +195,12 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
         }
     };
 
-    // The pass over the tiles.  APART: a range in which a masked tile holds an infinite or NaN value of V is taken a second time, with zeros in
-    // the place of such values (as a branch inside one pass it costs all the others sixty registers).
+    // The pass over the tiles; returns whether every sum of values is finite.  APART: a range with a sum that is not is taken a second time, with
+    // zeros in the place of infinite and NaN values of V (as a branch inside one pass it costs all the others sixty registers).  Such a value
+    // reaches the sums of all rows of its tile, as zero times infinity those of rows that do not see it or whose weight for it
+    // is rounded to zero.
     const auto pass = [&](auto apart) {
         constexpr bool APART = decltype(apart)::value;
-        uint32_t nonfinite = 0;
         if (t0 < t1) {
             load(t0);
             store(0);
@@ -262,12 +263,6 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
                                 for (int i = 0; i < 4; ++i)
                                     if (x * KVQ_TILE_TOKENS + 4 * sub + i >= end) s[r][x][sub][i] = -INFINITY;
                     }
-                    if (!APART) {
-#pragma unroll
-                        for (int x = 0; x < TT; ++x)
-#pragma unroll
-                            for (int nt = 0; nt < 8; ++nt) watch_nonfinite(read_v(vt + x * (2 * KVQ_FLASH_TILE_BYTES), nt, lane), nonfinite);
-                    }
                 }
                 uint32_t p[R][TT][4];
 #pragma unroll
@@ -298,9 +293,18 @@ __global__ __launch_bounds__(KVQ_PROMPT_THREADS, (R <= 2 && NT == 2 ? 2 : 1)) vo
             if (!APART && more) load(t + NT);
             next(more);
         }
-        return nonfinite;
+        float zero = 0.f;  // (times zero a sum is zero, or NaN if it is not finite)
+        if (!APART) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) zero = fmaf(st.o[r][nt][i], 0.f, zero);
+        }
+        return zero == 0.f;
     };
-    const bool apart = __builtin_amdgcn_readfirstlane(__syncthreads_or((int)pass(std::false_type{}))) != 0;
+    const bool apart = __builtin_amdgcn_readfirstlane(__syncthreads_or(pass(std::false_type{}) ? 0 : 1)) != 0;
     if (apart) {
         st.clear();
         pass(std::true_type{});
