@@ -245,42 +245,40 @@ __device__ inline void load_queries(half8 (&q)[R][4], const TreeArgs& A, int uni
     set_queries<R>(q, w, A, unit, row0, step, factors, lane);
 }
 // Sums of q over the channels of each group, for the zero points: a high part in lane quarter 0, what it leaves in quarter 1, the B operand
-// of a product with 16 channels whose A operand repeats a token's four zero points.  Queries so large that a sum passes the fp16
-// range are made smaller by 2^10, all of the wavefront's; returns what the scale grows by.
+// of a product with 16 channels whose A operand repeats a token's four zero points.  A query so large that a sum passes the fp16
+// range is made smaller by 2^10, and its scale, of the lane's row, grows by that (rows have scales of their own: the small components of other
+// queries would become subnormal).
 template <int R>
-__device__ inline float sum_queries(half8 (&q)[R][4], half4 (&qs)[R], int lane) {
+__device__ inline void sum_queries(half8 (&q)[R][4], half4 (&qs)[R], float (&scale)[R], float scale_log2, int lane) {
     const int j = lane >> 4;
     half8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
-    float sum[R][4];
-    bool large = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        float sum[4];
+        bool large = false;
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) {
-            sum[r][grp] = mma(ones, q[r][grp], float4v{0.f, 0.f, 0.f, 0.f})[0];  // (the same for every row of the result)
-            large |= fabsf(sum[r][grp]) >= 65504.f;
+            sum[grp] = mma(ones, q[r][grp], float4v{0.f, 0.f, 0.f, 0.f})[0];  // (the same for every row of the result)
+            large |= fabsf(sum[grp]) >= 65504.f;
         }
-    float grow = 1.f;
-    if (__any(large)) {
-        grow = 1024.f;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
+        scale[r] = scale_log2;
+        if (__any(large)) {
+            const float less = large ? 1.f / 1024.f : 1.f;
+            if (large) scale[r] *= 1024.f;
 #pragma unroll
             for (int grp = 0; grp < 4; ++grp) {
-                sum[r][grp] *= 1.f / 1024.f;
-                q[r][grp] *= (_Float16)(1.f / 1024.f);
+                sum[grp] *= less;
+                q[r][grp] *= (_Float16)less;
             }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
+        }
 #pragma unroll
         for (int grp = 0; grp < 4; ++grp) {
-            const _Float16 high = (_Float16)sum[r][grp], low = (_Float16)(sum[r][grp] - (float)high);
+            const _Float16 high = (_Float16)sum[grp], low = (_Float16)(sum[grp] - (float)high);
             qs[r][grp] = j == 0 ? high : j == 1 ? low : (_Float16)0.f;
         }
-    return grow;
+    }
 }
 
 // Scores of one tile of the cache in LDS for the first RR groups of a wavefront: sums of codes times queries over the channels of a scale, times it, plus
@@ -635,7 +633,8 @@ __global__ __launch_bounds__(64 * W, I16 ? 2 : 3) void kvq_tree_shared_kernel(co
         Staged f = stage_tile(A, first, unit, min(t0 + own, t1 - 1), part, stage, lane);
         set_queries<R>(q, w, A, unit, row0, step, true, lane);
         half4 qs[R];
-        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
+        float scale[R];
+        sum_queries<R>(q, qs, scale, A.scale_log2, lane);
         // rows that do not fill a block leave wavefronts with fewer groups (RR), in a loop of their own (not in pairs, where the length of
         // the chain counts and not what there is to do)
         const auto pass = [&](auto groups) {
@@ -666,7 +665,7 @@ __global__ __launch_bounds__(64 * W, I16 ? 2 : 3) void kvq_tree_shared_kernel(co
                 }
                 uint32_t p[R][1][4];
 #pragma unroll
-                for (int r = 0; r < RR; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
+                for (int r = 0; r < RR; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale[r], false, p[r]);
                 tile_products<RR, R>(st, p, lds + i * SLOT, l);
             }
             lds_barrier();
@@ -727,7 +726,8 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
         ask_queries<R>(w, A, unit, row0, 16, lane);
         set_queries<R>(q, w, A, unit, row0, 16, true, lane);
         half4 qs[R];
-        const float scale_log2 = A.scale_log2 * sum_queries<R>(q, qs, lane);
+        float scale[R];
+        sum_queries<R>(q, qs, scale, A.scale_log2, lane);
         for (int tile = t0 + wave; tile < t1; tile += 4) {
             expand_tile<I16>(f, slot, meta_lds, lane);
             const bool planes = I16 && f.bits == 16;
@@ -744,7 +744,7 @@ __global__ __launch_bounds__(256, I16 ? 1 : 2) void kvq_tree_kernel(const TreeAr
             }
             uint32_t p[R][1][4];
 #pragma unroll
-            for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale_log2, false, p[r]);
+            for (int r = 0; r < R; ++r) softmax_group<R, 1, true, false>(st, r, s[r], scale[r], false, p[r]);
             tile_products<R, R>(st, p, slot, lane);
             wave_lds_sync();
         }
