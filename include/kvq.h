@@ -292,8 +292,8 @@ kvq_status_t kvq_cache_fork(kvq_cache_t* dst, kvq_cache_t* src, int32_t layer, c
 kvq_status_t kvq_cache_truncate(kvq_cache_t* cache, int32_t layer, int32_t n_tokens, void* hip_stream);
 
 /* Reads tokens back as values: k_out[b, h, t, :] = K_hat, v_out[b, h, t, :] = V_hat of the tokens token_begin .. token_begin +
- * n_tokens - 1, device, [batch, n_kv_heads, n_tokens, 128], fp32 or fp16 (rounded once), 16-byte aligned: code * S + Z in
- * fp32, or the raw value; in a block with factors keys are multiplied by them again, so that they are keys as they were appended.  For
+ * n_tokens - 1, device, [batch, n_kv_heads, n_tokens, 128], fp32 or fp16 (rounded once; what a rounded scale has carried beyond the
+ * largest fp16 value becomes it), 16-byte aligned: code * S + Z in fp32, or the raw value; in a block with factors keys are multiplied by them again, so that they are keys as they were appended.  For
  * instance the prefix of a chunked prompt for kvq_prompt_attention, or what shrinking has left of a sequence.
  * KVQ_E_STATE if the block does not hold the tokens, or on an accounting-only cache.  Enqueues one kernel, may be captured. */
 kvq_status_t kvq_cache_read(kvq_cache_t* cache, int32_t layer, int32_t token_begin, int32_t n_tokens, void* k_out_dev,

@@ -170,6 +170,14 @@ __device__ inline void store8(void* out, int fp32, int64_t at, const float (&x)[
                                           kvq_dev::pack_rn2(x[6], x[7])}, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + at));
     }
 }
+// What a rounded scale (or a key's factor) has carried beyond the largest fp16 value becomes it, as in tree attention: no value that was
+// appended is larger.  Infinities and NaNs stay.
+__device__ inline float within_fp16(float x) { return fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x; }
+__device__ inline float largest(float most, const float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+    return most;
+}
 
 // Values of the eight slots 8 p .. 8 p + 7 of a lane; B: 2, 4, 8, 16 (raw) or 17 (integer 16-bit tier, two byte planes).  s and z of
 // each slot: one pair for K, a token each for V.
@@ -209,8 +217,16 @@ __device__ inline void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-__device__ inline void store_rows(const ReadArgs& A, void* out, int unit, int tile, int half, const float* lds, int lane) {
+// most: the largest size among the lane's values (looked at once for all rows: every value on its own cost a block of 4 x 32,768 tokens 8 %).
+__device__ inline void store_rows(const ReadArgs& A, void* out, int unit, int tile, int half, float* lds, float most, int lane) {
     const int64_t rows = A.n_tokens - A.begin;
+    if (!A.fp32 && __any(most > 65504.f)) {
+        wave_sync();
+        for (int i = lane; i < KVQ_TILE_TOKENS * 64; i += 64) {
+            float* const x = lds + (i >> 6) * KVQ_READ_PITCH + (i & 63);
+            *x = within_fp16(*x);
+        }
+    }
     wave_sync();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -228,6 +244,7 @@ __device__ inline void read_k(const ReadArgs& A, const uint8_t* code, const uint
     const int j = lane >> 4, n = lane & 15;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
+        float most = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int sub = q >> 1, grp = 2 * half + (q & 1);
@@ -244,11 +261,12 @@ __device__ inline void read_k(const ReadArgs& A, const uint8_t* code, const uint
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] *= l[i];
             }
+            most = largest(most, x);
             kvq_dev::f32x4* const to = reinterpret_cast<kvq_dev::f32x4*>(lds + t * KVQ_READ_PITCH + (channel & 63));
             to[0] = kvq_dev::f32x4{x[0], x[1], x[2], x[3]};
             to[1] = kvq_dev::f32x4{x[4], x[5], x[6], x[7]};
         }
-        store_rows(A, A.k_out, unit, tile, half, lds, lane);
+        store_rows(A, A.k_out, unit, tile, half, lds, most, lane);
     }
 }
 // ... or eight tokens of a channel.
@@ -257,6 +275,7 @@ __device__ inline void read_v(const ReadArgs& A, const uint8_t* code, const uint
     const int j = lane >> 4, n = lane & 15;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
+        float most = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int nt = 4 * half + q;
@@ -271,15 +290,16 @@ __device__ inline void read_v(const ReadArgs& A, const uint8_t* code, const uint
                 }
             }
             piece_values<B>(code, lane, nt, s, z, x);
+            if (B != 16) most = largest(most, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) lds[(8 * j + i) * KVQ_READ_PITCH + 16 * q + n] = x[i];
         }
-        store_rows(A, A.v_out, unit, tile, half, lds, lane);
+        store_rows(A, A.v_out, unit, tile, half, lds, most, lane);
     }
 }
 // A wavefront takes K or V of one tile of one unit.  Rows are put together in LDS because a lane holds eight channels of a token or eight tokens of
-// a channel, and stores of whole lines are what bounds it: a block of 4 x 32,768 tokens at all widths, 706 MB read and written, 152 us from
-// memory (4.6 TB/s; a copy reaches 5.1).  2,372 tokens of 8 heads 6.5 us, one launch's chain of trips.
+// a channel, and stores of whole lines are what bounds it: a block of 4 x 32,768 tokens at all widths, 706 MB read and written, 155 us from
+// memory (4.6 TB/s; a copy reaches 5.1).  2,372 tokens of 8 heads 6.4 us, one launch's chain of trips.
 __global__ __launch_bounds__(256) void kvq_read_kernel(const ReadArgs A) {
     __shared__ __attribute__((aligned(16))) float lds[4][KVQ_TILE_TOKENS * KVQ_READ_PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
