@@ -331,6 +331,8 @@ __global__ __launch_bounds__(256) void kvq_read_kernel(const ReadArgs A) {
 
 // ----------------------------------------------------------------------------------------------------------- host side
 
+constexpr int64_t kMostWorkgroups = ((1ll << 32) - 1) / 256;  // of 256 threads: a launch has less than 2^32
+
 void release_pages(kvq_cache* c, const std::vector<Page>& pages, size_t from, size_t to) {
     for (size_t i = from; i < to; ++i) {
         c->buddy.release(pages[i].code_unit, order_of_bits(pages[i].bits));
@@ -442,8 +444,8 @@ kvq_status_t fork_impl(kvq_cache* dst, kvq_cache* src, int32_t layer, const int3
     A.last_tiles = (n - (int)(n_pages - 1) * P + KVQ_TILE_TOKENS - 1) / KVQ_TILE_TOKENS;
     A.groups = (src->tpp + KVQ_FORK_TILES - 1) / KVQ_FORK_TILES;
     A.in_place = src == dst ? 1 : 0;
-    const int64_t per_page = (int64_t)A.groups * dst->units;
-    const int most = (int)std::max<int64_t>(1, std::min<int64_t>(KVQ_FORK_ARG_PAGES, (1 << 30) / per_page));
+    const int64_t per_page = (int64_t)A.groups * dst->units;  // (at most 256 x 65,535 workgroups)
+    const int most = (int)std::min<int64_t>(KVQ_FORK_ARG_PAGES, kMostWorkgroups / per_page);
     const bool stream = bytes > KVQ_FORK_STREAM_BYTES;
     hipError_t e = hipSuccess;
     for (int at = 0; at < A.n_pages && e == hipSuccess; at += most) {
@@ -527,7 +529,7 @@ kvq_status_t kvq_cache_read(kvq_cache_t* c, int32_t layer, int32_t token_begin, 
     A.fp32 = out_is_fp32 ? 1 : 0;
     A.items = (int64_t)c->units * A.n_tiles;
     const int64_t wgs = (A.items + 1) / 2;
-    if (wgs > (1ll << 31) - 1) return KVQ_E_INVALID;
+    if (wgs > kMostWorkgroups) return KVQ_E_INVALID;
     hipLaunchKernelGGL(kvq_read_kernel, dim3((unsigned)wgs), dim3(256), 0, as_stream(hip_stream), A);
     return hipGetLastError() == hipSuccess ? KVQ_OK : KVQ_E_HIP;
 }
