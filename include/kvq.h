@@ -224,8 +224,8 @@ kvq_status_t kvq_append_decode_attention_batch(kvq_cache_t* const* caches, int32
  *   NaN value that it sees does, however little it weighs.
  *   q_dev, out_dev: row (t, h) at t * *_token_stride + h * *_head_stride elements, 128 consecutive ones; k_dev, v_dev the same
  *   with KV heads.  Strides are multiples of 8 and not negative (a head stride of 0 in inputs: broadcast), addresses of
- *   16 bytes; the token strides of k and v are 128 .. 2^22 - 1.  Output fp16, or
- *   fp32 with out_is_fp32.
+ *   16 bytes; the token strides of k and v are 128 .. 2^22 - 1; rows of the output share no element (KVQ_E_INVALID).  Output fp16,
+ *   or fp32 with out_is_fp32.
  *   lse_dev: NULL, or fp32 [n_q_heads][q_begin_host[n_seqs]]: log of the sum of exponentials of every row's scaled scores.
  *   softmax_scale 0 means 1 / sqrt(128).
  *   workspace_dev: kvq_prompt_workspace_bytes() bytes, 16-byte aligned, for launches of few rows over many keys, which are cut into

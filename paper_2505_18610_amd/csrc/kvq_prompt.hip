@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstdlib>
 #include <type_traits>
 
 #include "../../include/kvq.h"
@@ -501,6 +502,14 @@ bool lengths_ok(const int32_t* qb, const int32_t* kb, int n_seqs) {
     }
     return true;
 }
+// Whether no two of the rows t * token + h * head, 128 long each, share an element (0 <= t < n, 0 <= h < heads; strides of 128 or more).
+bool rows_apart(int64_t token, int64_t head, int64_t n, int64_t heads) {
+    if (n <= 1 || heads <= 1 || token >= (heads - 1) * head + KVQ_D || head >= (n - 1) * token + KVQ_D) return true;
+    for (int64_t h = 1; h < heads; ++h)  // the tokens that h heads on comes next to
+        for (int64_t t = h * head / token, k = 0; k < 2; ++k, ++t)
+            if (t < n && std::abs(h * head - t * token) < KVQ_D) return false;
+    return true;
+}
 bool heads_ok(int n_q, int n_kv) { return n_kv >= 1 && n_kv <= 65535 && n_q >= 1 && n_q % n_kv == 0 && n_q / n_kv <= KVQ_MAX_GQA; }
 
 }  // namespace
@@ -538,6 +547,7 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* d, const void* q_dev, cons
     for (int64_t s : {d->k_token_stride, d->v_token_stride})
         if (s < KVQ_D || s >= (1ll << 22)) return KVQ_E_INVALID;
     if (d->out_token_stride < KVQ_D || (d->n_q_heads > 1 && d->out_head_stride < KVQ_D)) return KVQ_E_INVALID;
+    if (!rows_apart(d->out_token_stride, d->out_head_stride, q_begin_host[n_seqs] - q_begin_host[0], d->n_q_heads)) return KVQ_E_INVALID;
 
     PromptArgs A{};
     A.q = static_cast<const _Float16*>(q_dev);
