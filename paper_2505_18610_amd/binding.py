@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 
 import numpy as np
 
@@ -186,6 +187,25 @@ def kvq_append_decode_attention_batch(caches, layer, ks, vs, qs, outs, cos_sins=
         raise KvqError(st, "kvq_append_decode_attention_batch")
 
 
+# (a tensor is at hand where these are asked, so torch has been imported)
+def _half(*tensors):
+    """fp16 tensors on a device: other types of two bytes, and host memory, are not told by an address."""
+    half = sys.modules["torch"].float16
+    return all(t.dtype == half and t.is_cuda for t in tensors)
+
+
+def _is_fp32(out):
+    """1 for an fp32 output, 0 for an fp16 one."""
+    torch = sys.modules["torch"]
+    assert out.dtype in (torch.float16, torch.float32) and out.is_cuda
+    return 1 if out.dtype == torch.float32 else 0
+
+
+def _is_int32(t):
+    torch = sys.modules["torch"]
+    return t.dtype in (torch.int32, torch.uint32) and t.is_cuda
+
+
 def _rows(begin):
     """Host array of row numbers."""
     return (C.c_int32 * len(begin))(*map(int, begin))
@@ -213,11 +233,10 @@ def kvq_prompt_attention(q, k, v, out, q_begin, k_begin=None, softmax_scale=0.0,
     qb = _rows(q_begin)
     kb = qb if k_begin is None else _rows(k_begin)
     heads, kv = q.shape[1], k.shape[1]
-    size = out.dtype.itemsize
-    assert q.dtype.itemsize == k.dtype.itemsize == v.dtype.itemsize == 2
-    assert lse is None or (tuple(lse.shape) == (heads, qb[-1]) and lse.dtype.itemsize == 4)
+    assert _half(q, k, v) and (lse is None or (tuple(lse.shape) == (heads, qb[-1]) and _is_fp32(lse)))
+    assert workspace is None or workspace.is_cuda
     d = _Prompt(heads, kv, *_packed(q, qb[-1], heads), *_packed(k, kb[-1], kv), *_packed(v, kb[-1], kv), *_packed(out, qb[-1], heads),
-                size == 4, float(softmax_scale))
+                _is_fp32(out), float(softmax_scale))
     st = load_library().kvq_prompt_attention(
         C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), qb, kb, len(qb) - 1, _ptr(workspace),
         0 if workspace is None else workspace.numel(), _stream(stream))
@@ -228,7 +247,7 @@ def kvq_prompt_attention(q, k, v, out, q_begin, k_begin=None, softmax_scale=0.0,
 def kvq_cache_fork(dst, src, layer, seq_map=None, n_tokens=-1, stream=None):
     """Block `layer` of dst takes the first n_tokens (-1: all) of src's; seq_map: int32 device tensor [dst batch], the sequence of
     src that each of dst's continues, or None.  dst may be src."""
-    assert seq_map is None or (tuple(seq_map.shape) == (dst.cfg.batch,) and seq_map.dtype.itemsize == 4)
+    assert seq_map is None or (tuple(seq_map.shape) == (dst.cfg.batch,) and _is_int32(seq_map))
     st = load_library().kvq_cache_fork(dst.handle, src.handle, layer, _ptr(seq_map), n_tokens, _stream(stream))
     if st != KVQ_OK:
         raise KvqError(st, "kvq_cache_fork")
@@ -334,12 +353,12 @@ class KvqCache:
         c, shape = self.cfg, q.shape
         n = shape[2]
         words = (n + 31) // 32
-        size, mask_shape = out.dtype.itemsize, mask.shape
+        mask_shape = mask.shape
         assert shape == out.shape == (c.batch, c.n_q_heads, n, 128) and k.shape == v.shape == (c.batch, c.n_kv_heads, n, 128)
-        assert q.dtype.itemsize == k.dtype.itemsize == v.dtype.itemsize == 2 and mask.dtype.itemsize == 4
+        assert _half(q, k, v) and _is_int32(mask) and (workspace is None or workspace.is_cuda)
         assert mask_shape == (n, words) or mask_shape == (c.batch, n, words)
         self._check(self.lib.kvq_tree_attention(self.handle, layer, _ptr(q), _ptr(k), _ptr(v), n, _ptr(mask), len(mask_shape) == 3,
-                                                _ptr(out), size == 4, float(softmax_scale), _ptr(workspace),
+                                                _ptr(out), _is_fp32(out), float(softmax_scale), _ptr(workspace),
                                                 0 if workspace is None else workspace.numel(), _stream(stream)),
                     "kvq_tree_attention")
 
@@ -350,9 +369,9 @@ class KvqCache:
         """Tokens token_begin, ... into k_out, v_out: fp16 or fp32 device tensors [batch, n_kv_heads, n, 128]."""
         c = self.cfg
         assert k_out.shape == v_out.shape and k_out.dtype == v_out.dtype and k_out.dim() == 4
-        assert (k_out.shape[0], k_out.shape[1], k_out.shape[3]) == (c.batch, c.n_kv_heads, 128)
+        assert (k_out.shape[0], k_out.shape[1], k_out.shape[3]) == (c.batch, c.n_kv_heads, 128) and v_out.is_cuda
         self._check(self.lib.kvq_cache_read(self.handle, layer, token_begin, k_out.shape[2], _ptr(k_out), _ptr(v_out),
-                                            1 if k_out.dtype.itemsize == 4 else 0, _stream(stream)), "kvq_cache_read")
+                                            _is_fp32(k_out), _stream(stream)), "kvq_cache_read")
 
     def kvq_cache_describe(self, layer):
         """Returns (segments [(token_begin, token_end, bits)], bytes_used, n_tokens, current_bits)."""
