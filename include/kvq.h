@@ -216,7 +216,7 @@ kvq_status_t kvq_append_decode_attention_batch(kvq_cache_t* const* caches, int32
 /* Causal attention of whole prompts, or of chunks of them, over fp16 keys and values: packed sequences of different
  * lengths, grouped heads.  Needs no cache; the keys and values are those that kvq_quantize_append takes next.
  *   Sequence i has the query rows q_begin_host[i] .. q_begin_host[i + 1] - 1 and the key and value rows k_begin_host[i] ..
- *   k_begin_host[i + 1] - 1 (host arrays of n_seqs + 1 non-decreasing row numbers, read during the call; k_begin_host ==
+ *   k_begin_host[i + 1] - 1 (host arrays of n_seqs + 1 non-decreasing row numbers below 2^31 - 4,096, read during the call; k_begin_host ==
  *   NULL: the same as the queries').  Its n_q queries are the last of its n_k keys: query i sees the keys 0 .. i + n_k - n_q,
  *     out[i, h, :] = softmax_j( q[i, h, :] . k[j, h / g, :] * softmax_scale ) v[j, h / g, :],
  *   so n_q = n_k is a whole prompt, n_q < n_k a chunk behind the keys of earlier ones, n_q = 1 a decode step.  A query that sees no

@@ -496,7 +496,7 @@ int64_t plan_prompt(PromptArgs& A, const int32_t* qb, const int32_t* kb, int n_s
 bool lengths_ok(const int32_t* qb, const int32_t* kb, int n_seqs) {
     if (!qb || n_seqs < 1 || n_seqs > (1 << 20)) return false;
     for (const int32_t* b : {qb, kb}) {
-        if (b[0] < 0) return false;
+        if (b[0] < 0 || b[n_seqs] > INT32_MAX - 4096) return false;  // (rounded up to tiles and blocks they stay below 2^31)
         for (int i = 0; i < n_seqs; ++i)
             if (b[i + 1] < b[i]) return false;
     }
