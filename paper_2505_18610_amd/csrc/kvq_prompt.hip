@@ -377,6 +377,7 @@ constexpr int kNumVariants = 4;
 constexpr int kLeastTiles = 8;          // of a range of keys
 constexpr int kMostSplits = KVQ_MOST_PARTS;
 constexpr int kJoinTiles = 48;
+constexpr int64_t kMostItems = (1 << 30) / KVQ_MOST_PARTS;  // row blocks x KV heads of a launch
 
 int variant_of(int gqa, int nq) {
     const int64_t rows = (int64_t)gqa * nq;
@@ -465,7 +466,7 @@ int64_t plan_prompt(PromptArgs& A, const int32_t* qb, const int32_t* kb, int n_s
                 items += (int64_t)A.n_kv * A.seq[A.n_seqs++].blocks;
             }
             if (!A.n_seqs) continue;
-            if (items > (1 << 30) / kMostSplits) return -1;
+            if (items > kMostItems) return -1;
             // the longest first: what starts last ends last
             std::sort(A.seq, A.seq + A.n_seqs, [](const PromptSeq& a, const PromptSeq& b) { return a.nk != b.nk ? a.nk > b.nk : a.q0 < b.q0; });
             cut_blocks(A, items, kVariants[v].slots);
@@ -567,6 +568,13 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* d, const void* q_dev, cons
     const float scale = d->softmax_scale != 0.f ? d->softmax_scale : 1.0f / std::sqrt((float)KVQ_D);
     A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
     A.flip = scale < 0.f ? 0x80008000u : 0u;
+    // nothing is enqueued of a call whose last launches would be too large
+    int64_t items = 0;
+    for (int i = 0; i < n_seqs; ++i) {
+        const int nq = q_begin_host[i + 1] - q_begin_host[i];
+        if (nq) items += (int64_t)A.n_kv * describe(variant_of(A.gqa, nq), A.gqa, 0, nq, 0, 0).blocks;
+    }
+    if (items > kMostItems && plan_prompt(A, q_begin_host, k_begin_host, n_seqs, 0, [](int, const PromptArgs&, int, int) { return true; }) < 0) return KVQ_E_INVALID;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int64_t got = plan_prompt(A, q_begin_host, k_begin_host, n_seqs, workspace_dev ? (int64_t)std::min<uint64_t>(workspace_bytes, INT64_MAX) : 0,
                                     [&](int v, const PromptArgs& args, int wgs, int merges) {

@@ -21,3 +21,11 @@ def test_rows_just_below():
     top = LAST - 4096
     assert kq.kvq_prompt_workspace_bytes(8, 2, [0, 4], [0, top]) > 0
     assert kq.kvq_prompt_workspace_bytes(8, 2, [0, 4], [0, top]) == kq.kvq_prompt_workspace_bytes(8, 2, [top - 4, top], [0, top])
+
+
+@pytest.mark.skipif(os.path.exists("/dev/kfd"), reason="an accepted call would be launched")
+def test_a_call_that_is_too_large_enqueues_nothing():
+    """The first sequence has a launch of its own, in front of the second's, which has more row blocks than a launch takes."""
+    qb, kb = (0, 1, LAST - 5000), (0, 200, 300)
+    assert call(n_q=64, n_kv=64, qb=qb, kb=kb) == kq.KVQ_E_INVALID
+    assert call(n_q=64, n_kv=64, qb=qb[:2], kb=kb[:2]) not in (kq.KVQ_OK, kq.KVQ_E_INVALID)  # (there is no device)
