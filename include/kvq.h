@@ -260,8 +260,10 @@ kvq_status_t kvq_prompt_attention(const kvq_prompt_t* prompt, const void* q_dev,
  *   each sequence, one after the other.  softmax_scale 0 means 1 / sqrt(128).
  *   workspace_dev: kvq_tree_workspace_bytes() bytes for the results of ranges of the cache, 16-byte aligned; with less, or NULL,
  *   the cache is cut into fewer ranges or none, which is slower.  It may be reused by the next call on the stream.
- * Cached values are formed as code * S + Z and rounded to fp16; fp32 accumulation.  Enqueues kernels only and may be captured
- * (the cache must not change between capture and replay).  Sums run in a fixed order.  KVQ_E_STATE on an accounting-only cache. */
+ * V_hat is formed as code * S + Z and rounded to fp16 (what a rounded scale has carried beyond the largest fp16 value becomes
+ * it); keys enter as their codes, S and Z are applied in fp32; weights are rounded to fp16; fp32 accumulation.  Enqueues kernels only and may be
+ * captured (the cache must not change between capture and replay).  Sums run in a fixed order.  KVQ_E_STATE on an accounting-only
+ * cache. */
 uint64_t kvq_tree_workspace_bytes(const kvq_cache_t* cache, int32_t n_nodes);
 kvq_status_t kvq_tree_attention(kvq_cache_t* cache, int32_t layer, const void* q_dev, const void* k_dev, const void* v_dev,
                                 int32_t n_nodes, const uint32_t* mask_dev, int32_t mask_per_sequence, void* out_dev,

@@ -104,8 +104,8 @@ __device__ inline void add_nonfinite(const PromptArgs& A, const PromptSeq& S, in
 
 // One workgroup: WM * 16 R rows of one KV head against a range of keys; WT wavefronts share rows and take the tiles in turn.  An
 // iteration loads NT tiles (K and V, 16 KiB each) into one half of LDS while the other is computed on.
-// 32 rows a wavefront, so that an operand read from LDS serves two products, two workgroups a compute unit.  32,768 tokens x 64 heads: 16.8 to
-// 18.2 ms on different cards, 970 to 1,050 TFLOP/s where an fp16 product of 8,192^3 reaches 1,290.  Matrix cores 46 % busy, vector ALUs
+// 32 rows a wavefront, so that an operand read from LDS serves two products, two workgroups a compute unit.  32,768 tokens x 64 heads: 16.9 to
+// 18.7 ms on different cards, 940 to 1,040 TFLOP/s where an fp16 product of 8,192^3 reaches 1,290.  Matrix cores 47 % busy, vector ALUs
 // 31 %, at the 2.0 GHz to which the card lowers its clock under this load; exponentials put beside products, a third wavefront a SIMD and
 // wavefront priorities each changed that by 2 % or less.
 template <int R, int WM, int WT, int NT>
