@@ -318,6 +318,86 @@ kvq_status_t kvq_cache_export_segment(kvq_cache_t* cache, int32_t layer, int32_t
                                       void* codes_host, void* scales_host, void* zeros_host,
                                       void* hip_stream);
 
+/* ---- The paged cache of 8-bit floating point: one attention block's keys and values as e4m3 codes in pages that the caller deals out.
+ * It stands beside kvq_cache_t for serving loops in which everything that changes from step to step lies on the device: page tables,
+ * lengths and row numbers are device arrays, calls enqueue kernels only, and a captured step replays while the sequences grow, come
+ * and go.  Sequences may share pages that none of them appends to.
+ *
+ * A page holds page_tokens tokens of every KV head.  Codes of 32 tokens of a head are a K tile and a V tile of 4,096 bytes:
+ *   codes_dev[n_pages][n_kv_heads][page_tokens / 32][2][4096]; with lane = 16 j + n,
+ *   K, bytes [sub 2][gh 2][j 4][nh 4][nl 4][gl 2][i 8]: token 8 nh + 4 sub + nl, channel 64 gh + 32 gl + 8 j + i
+ *   V, bytes [th 4][j 4][n 16][tl 2][i 8]:              token 8 j + i,           channel 32 th + 16 tl + n
+ * A page has one scale for each head and kind, 2^e: words_dev[n_pages][n_kv_heads][2] (K, V) holds e + 64 in its low byte, and 0x100
+ * where a NaN has been appended.  A value stands for code * 2^e.
+ *
+ * What no page, row or token is named by does not exist, and nothing is read or written for it: rows of a sequence beyond max_rows or
+ * n_rows, tokens beyond the table (lengths count as table_pages * page_tokens at most, negative ones as 0), table entries outside
+ * 0 .. n_pages - 1 (a page that has been given up: attention passes over its tokens).  Rows that belong to no sequence are left as they were. */
+typedef struct {
+    void* codes_dev;       /* 16-byte aligned */
+    int32_t* words_dev;    /* 8-byte aligned */
+    int32_t n_pages, n_kv_heads;
+    int32_t page_tokens;   /* 32, 64, 128 or 256 */
+} kvq_paged8_t;
+
+/* The sequences of a call.  Rows (of new tokens, queries, values to read) are packed: sequence s has rows row_begin_dev[s] ..
+ * row_begin_dev[s + 1] - 1, which are its last tokens, lengths_dev[s] - rows .. lengths_dev[s] - 1; row_begin_dev == NULL: row s alone.
+ * lengths_dev[s] counts the tokens of the call's rows, so that one batch serves an append and the attention behind it. */
+typedef struct {
+    const int32_t* table_dev;      /* [n_seqs][table_stride], the first table_pages entries of a row name its pages */
+    const int32_t* lengths_dev;    /* [n_seqs] */
+    const int32_t* row_begin_dev;  /* [n_seqs + 1] or NULL */
+    int64_t table_stride;
+    int32_t n_seqs;                /* 0 .. 4096 */
+    int32_t table_pages;
+    int32_t n_rows;                /* rows that the packed tensors of the call have */
+    int32_t max_rows;              /* no sequence has more (what it has more does not exist); 1 without row_begin_dev */
+} kvq_paged8_batch_t;
+
+/* Packed rows [n_rows][heads][128]: strides in elements, 16-byte aligned rows; rows that are written share no memory. */
+typedef struct {
+    const void* data_dev;
+    int64_t row_stride, head_stride;
+} kvq_paged8_rows_t;
+
+/* Appends the rows' keys and values (fp16) to the sequences' pages.  cos_sin_dev: fp32 [n_rows][2 pair], cosines then sines of a
+ * row's angles, 16-byte aligned: channel i of every run of 2 pair channels is rotated with channel i + pair on the way, pair = 64 or, for two
+ * maps of 64 channels each, 32 (each product and sum a separate fp32 operation); NULL: keys are ready, pair is not looked at.
+ *   e of a page, head and kind: the smallest e >= -40 with |x| <= 448 2^e for all finite x (fp32, rotated) appended to it; never lowered while
+ *   the page is filled, and taken afresh when its first token is appended.  Where it rises, the codes that the page holds are
+ *   rounded again.  code = e4m3(x 2^-e), to nearest even.  What is not finite is stored as NaN.
+ * Slots of a tile behind the last token that has been appended to it are zero.  Two sequences of a call must not append to one page. */
+kvq_status_t kvq_paged8_append(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* k_dev,
+                               const kvq_paged8_rows_t* v_dev, const float* cos_sin_dev, int32_t pair, void* hip_stream);
+
+/* The rows' tokens as values, fp16 (magnitudes beyond 65,504 become it) or fp32. */
+kvq_status_t kvq_paged8_read(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* k_out_dev,
+                             const kvq_paged8_rows_t* v_out_dev, int32_t out_is_fp32, void* hip_stream);
+
+/* Bytes of workspace that attention of this batch needs; 0 on invalid arguments.  It depends on n_seqs, table_pages, max_rows, n_rows, the
+ * page size and the heads only.  The workspace is filled with zeros once, before its first use; every call leaves what it counts with
+ * at zero.  Calls that may overlap in time need workspaces of their own; others may share one, whatever their batches. */
+uint64_t kvq_paged8_workspace_bytes(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, int32_t n_q_heads, int32_t two_maps);
+
+/* Attention of the rows over their sequences' cached tokens up to and with their own:
+ *   out[r, h, :] = softmax_t(q[r, h, :] . K_hat[t, h / g, :] * softmax_scale) V_hat[t, h / g, :],  g = n_q_heads / n_kv_heads <= 16
+ *   over t <= lengths[s] - rows(s) + i for the i-th row of sequence s; a row that sees nothing gives zeros.
+ *   q_dev: fp16; out_dev: fp16 or fp32; softmax_scale 0 means 1 / sqrt(128).  lse_dev: fp32 [n_q_heads][n_rows] or NULL, the natural
+ *   logarithms of the sums of exponentials (-inf where nothing is seen).  Sums and statistics are held in fp32, probabilities are rounded
+ *   to fp16 for the product with V_hat.  Equal calls give equal bits. */
+kvq_status_t kvq_paged8_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,
+                                  const kvq_paged8_rows_t* out_dev, int32_t n_q_heads, int32_t out_is_fp32, float softmax_scale,
+                                  float* lse_dev, void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
+
+/* Differential attention: the same with the difference of two softmax maps, over the first and the second 64 channels of queries and keys:
+ *   o = (softmax(q1 . K1_hat * softmax_scale) - lambda[h] softmax(q2 . K2_hat * softmax_scale)) V_hat;  softmax_scale 0 means 1 / sqrt(64)
+ *   out = out_scale o, or with a norm out_scale o / sqrt(mean_c(o_c^2) + norm_eps) norm_weight
+ *   lambda_dev: fp32 [n_q_heads]; norm_weight_dev: fp32 [128], 16-byte aligned, or NULL. */
+kvq_status_t kvq_paged8_diff_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,
+                                       const float* lambda_dev, const kvq_paged8_rows_t* out_dev, int32_t n_q_heads, int32_t out_is_fp32,
+                                       float softmax_scale, const float* norm_weight_dev, float norm_eps, float out_scale,
+                                       void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);
+
 /* Tuning options (the results do not depend on them beyond floating-point summation order).
  *   KVQ_OPT_SPLITS: number of token-range splits kvq_decode_attention uses per (sequence, KV head),
  *                   1..128; 0 restores the automatic choice.

@@ -38,6 +38,19 @@ class _Prompt(C.Structure):
         ("out_is_fp32", C.c_int32), ("softmax_scale", C.c_float)]
 
 
+class _Paged8(C.Structure):
+    _fields_ = [("codes_dev", C.c_void_p), ("words_dev", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_tokens", C.c_int32)]
+
+
+class _Paged8Batch(C.Structure):
+    _fields_ = [("table_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("row_begin_dev", C.c_void_p), ("table_stride", C.c_int64),
+                ("n_seqs", C.c_int32), ("table_pages", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32)]
+
+
+class _Paged8Rows(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 class _SegmentInfo(C.Structure):
     _fields_ = [("token_begin", C.c_int32), ("token_end", C.c_int32), ("bits", C.c_int32)]
 
@@ -96,6 +109,12 @@ _SIGNATURES = {
     "kvq_cache_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]),
     "kvq_cache_truncate": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
     "kvq_cache_read": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "kvq_paged8_append": (C.c_int, [C.c_void_p] * 5 + [C.c_int32, C.c_void_p]),
+    "kvq_paged8_read": (C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_void_p]),
+    "kvq_paged8_workspace_bytes": (C.c_uint64, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32]),
+    "kvq_paged8_attention": (C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "kvq_paged8_diff_attention": (C.c_int, [C.c_void_p] * 5 + [C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_float, C.c_float,
+                                                                C.c_void_p, C.c_uint64, C.c_void_p]),
     "kvq_status_string": (C.c_char_p, [C.c_int]),
 }
 
@@ -273,6 +292,97 @@ def _stream(stream):
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+class KvqPaged8Batch:
+    """The sequences of calls on a paged cache of 8-bit floating point.  table: int32 device tensor [n_seqs, pages] (rows of any stride),
+    lengths: int32 device tensor [n_seqs], row_begin: int32 device tensor [n_seqs + 1] or None (one row each), max_rows: the most rows of a
+    sequence.  Their contents may change between calls and replays; the tensors themselves are kept."""
+
+    def __init__(self, table, lengths, row_begin=None, max_rows=1):
+        n, pages = table.shape
+        assert all(_is_int32(t) for t in (table, lengths)) and lengths.shape == (n,) and lengths.is_contiguous()
+        assert pages <= 1 or table.stride(1) == 1
+        assert row_begin is None or (_is_int32(row_begin) and row_begin.shape == (n + 1,) and row_begin.is_contiguous())
+        self.table, self.lengths, self.row_begin = table, lengths, row_begin
+        self._c = _Paged8Batch(table.data_ptr(), lengths.data_ptr(), None if row_begin is None else row_begin.data_ptr(),
+                               pages if n <= 1 else table.stride(0), n, pages, 0, max_rows)
+
+    def _of(self, n_rows):
+        self._c.n_rows = n_rows
+        return C.byref(self._c)
+
+
+def _paged8_rows(t, rows, heads):
+    """A packed tensor [rows, heads, 128] (a dimension of one element may carry any stride)."""
+    n, h, d = t.shape
+    row, head, channel = t.stride()
+    assert n == rows and h == heads and d == 128 and channel == 1
+    return C.byref(_Paged8Rows(t.data_ptr(), 128 if n <= 1 else row, 128 if h == 1 else head))
+
+
+class KvqPaged8:
+    """A paged cache of 8-bit floating point over the caller's tensors.  codes: uint8 device tensor
+    [n_pages, n_kv_heads, page_tokens / 32, 2, 4096], words: int32 device tensor [n_pages, n_kv_heads, 2]; both may hold anything at first."""
+
+    def __init__(self, codes, words):
+        self.lib = load_library()
+        pages, kv, tiles, kinds, tile = codes.shape
+        assert (kinds, tile) == (2, 4096) and codes.dtype.itemsize == 1 and codes.is_cuda and codes.is_contiguous()
+        assert tuple(words.shape) == (pages, kv, 2) and _is_int32(words) and words.is_contiguous()
+        self.codes, self.words, self.n_kv_heads = codes, words, kv
+        self._c = _Paged8(codes.data_ptr(), words.data_ptr(), pages, kv, 32 * tiles)
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def _check(st, where):
+        if st != KVQ_OK:
+            raise KvqError(st, where)
+
+    def kvq_paged8_append(self, batch, k, v, cos_sin=None, stream=None):
+        """k, v: fp16 device tensors [rows, n_kv_heads, 128] of any strides whose channels follow one another; cos_sin: fp32 device tensor
+        [rows, 128] (cos 64 | sin 64 of channel pairs i, i + 64) or [rows, 64] (cos 32 | sin 32 of pairs i, i + 32 of both halves), or
+        None for keys that are rotated already."""
+        n, pair = k.shape[0], 0
+        assert _half(k, v)
+        if cos_sin is not None:
+            pair = cos_sin.shape[1] // 2
+            assert cos_sin.shape in ((n, 128), (n, 64)) and _is_fp32(cos_sin)
+        self._check(self.lib.kvq_paged8_append(self._ref, batch._of(n), _paged8_rows(k, n, self.n_kv_heads), _paged8_rows(v, n, self.n_kv_heads),
+                                               _ptr(cos_sin), pair, _stream(stream)), "kvq_paged8_append")
+
+    def kvq_paged8_read(self, batch, k_out, v_out, stream=None):
+        """The rows' tokens into k_out, v_out: fp16 or fp32 device tensors [rows, n_kv_heads, 128]."""
+        n, kv = k_out.shape[0], self.n_kv_heads
+        assert k_out.dtype == v_out.dtype and v_out.is_cuda
+        self._check(self.lib.kvq_paged8_read(self._ref, batch._of(n), _paged8_rows(k_out, n, kv), _paged8_rows(v_out, n, kv), _is_fp32(k_out),
+                                             _stream(stream)), "kvq_paged8_read")
+
+    def kvq_paged8_attention(self, batch, q, out, softmax_scale=0.0, lse=None, workspace=None, stream=None):
+        """q: fp16 device tensor [rows, n_q_heads, 128], out: fp16 or fp32 like it, of any strides; lse: fp32 device tensor
+        [n_q_heads, rows] or None; workspace: uint8 device tensor of kvq_paged8_workspace_bytes, zeros before its first use."""
+        n, heads, _ = q.shape
+        assert _half(q) and (lse is None or (tuple(lse.shape) == (heads, n) and _is_fp32(lse))) and (workspace is None or workspace.is_cuda)
+        self._check(self.lib.kvq_paged8_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _paged8_rows(out, n, heads), heads,
+                                                  _is_fp32(out), softmax_scale, _ptr(lse), _ptr(workspace),
+                                                  0 if workspace is None else workspace.numel(), _stream(stream)), "kvq_paged8_attention")
+
+    def kvq_paged8_diff_attention(self, batch, q, lam, out, norm_weight=None, norm_eps=1e-5, out_scale=1.0, softmax_scale=0.0, workspace=None,
+                                  stream=None):
+        """Differential attention; q, out and workspace as in kvq_paged8_attention.  lam: fp32 device tensor [n_q_heads], norm_weight:
+        fp32 device tensor [128] or None."""
+        n, heads, _ = q.shape
+        assert _half(q) and tuple(lam.shape) == (heads,) and _is_fp32(lam) and (workspace is None or workspace.is_cuda)
+        assert norm_weight is None or (tuple(norm_weight.shape) == (128,) and _is_fp32(norm_weight))
+        self._check(self.lib.kvq_paged8_diff_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _ptr(lam), _paged8_rows(out, n, heads),
+                                                       heads, _is_fp32(out), softmax_scale, _ptr(norm_weight), norm_eps, out_scale,
+                                                       _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
+                    "kvq_paged8_diff_attention")
+
+
+def kvq_paged8_workspace_bytes(cache, batch, n_q_heads, n_rows, two_maps=False) -> int:
+    """Bytes of workspace of kvq_paged8_attention (or, two_maps, kvq_paged8_diff_attention) of n_rows rows."""
+    return int(cache.lib.kvq_paged8_workspace_bytes(cache._ref, batch._of(n_rows), n_q_heads, 1 if two_maps else 0))
 
 
 class KvqCache:

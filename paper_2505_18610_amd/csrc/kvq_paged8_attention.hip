@@ -1,0 +1,445 @@
+// Attention over the paged cache of 8-bit floating point, of single tokens, drafted tokens and chunks of prompts in one ragged call, with
+// one softmax map or with the difference of two (kvq_paged8_attention, kvq_paged8_diff_attention).
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/kvq.h"
+#include "kvq_flash.h"
+#include "kvq_paged8.h"
+#include "kvq_paged8_host.h"
+
+namespace {
+
+using namespace kvq_p8;
+using kvq_flash::half8;
+using kvq_flash::half2v;
+using kvq_flash::float4v;
+using kvq_flash::mma;
+using kvq_flash::State;
+using kvq_flash::quarters_sum;
+using kvq_flash::reference_of;
+using kvq_flash::softmax_group;
+using kvq_flash::to_half8;
+
+#define KVQ_P8_GROUPS 512       // workgroups of a launch over ranges of tiles, at most
+#define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
+#define KVQ_P8_LEAST_SHARE 8    // tiles of a workgroup, at least
+#define KVQ_P8_MOST_PIECES 128  // of a unit
+
+struct AttnArgs {
+    KvqP8 p;
+    const _Float16* q;
+    void* out;
+    float* lse;
+    const float *lambda, *weight;  // two maps: a factor for each head; weights of the norm or NULL
+    uint32_t* counters;
+    float* part;
+    int64_t q_rs, q_hs, o_rs, o_hs, lse_hs;
+    int32_t gqa, maps, out_fp32;   // gqa: query heads of a KV head
+    float scale_log2, eps, out_scale;
+    uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
+};
+
+// A lane's eight codes of one operand, widened: exact but for values below 2^-21, which keep the 2^-25 that fp16 has there.
+__device__ inline half8 widen(uint32_t lo, uint32_t hi, float scale) {
+    const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+    const half2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
+    return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// Values are taken times 1/2 and outputs times 2: a rounded code may stand for up to 2^16, beyond fp16.
+__device__ inline float value_scale(int word) { return ldexpf(0.5f, exponent_of(word)); }
+
+// What NaN codes among a lane's eight of one V operand, of tokens token, token + 1, ..., add to a row that sees those below limit; the codes
+// become zeros.
+__device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
+    half8 nan, sees;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int at = 8 * (e & 3);
+        const bool is = ((w[e >> 2] >> at) & 0x7fu) == 0x7fu;
+        sees[e] = token + e < limit ? (_Float16)1.f : (_Float16)0.f;
+        nan[e] = is ? (_Float16)1.f : (_Float16)0.f;
+        if (is) w[e >> 2] &= ~(0xffu << at);
+    }
+    const float4v count = mma(nan, sees, float4v{0.f, 0.f, 0.f, 0.f});
+    float4v x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = count[i] > 0.f ? __builtin_nanf("") : 0.f;
+    return x;
+}
+
+// A unit: the rows of one block of one KV head of one sequence.  Rows follow one another token by token, of a token head by head, of a head
+// map by map; a block has 16 R of them.
+struct Unit {
+    int kv, block, tiles;
+};
+
+// A range of the tiles of all units a workgroup; units that end in another workgroup's range are joined by the last of theirs to arrive.
+// Eight wavefronts take a range's tiles in turn, every one from memory straight into operand registers: nothing is shared before the end.
+template <int R>
+__global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(const AttnArgs A) {
+    constexpr int RB = 16 * R, W = 8;
+    __shared__ float4v lds_o[W][16][32];     // a wavefront's outputs of 16 rows, chunks of four channels turned by the row
+    __shared__ float4v lds_ml[W][16];        // reference, sum, sum of the unrounded
+    __shared__ u32x4 lds_q[R][4][64];        // queries as operands: registers are for tiles on their way
+    __shared__ int lds_last;
+    const KvqP8& P = A.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
+    const int wg = blockIdx.x, rows_per_token = A.gqa * A.maps;
+
+    const auto blocks_of = [&](const Seq& q) { return (q.rows * rows_per_token + RB - 1) / RB; };
+    const auto tiles_of = [&](const Seq& q) { return max(1, (q.tokens + 31) >> 5); };
+    const auto count = [&](int s) {
+        const Seq q = seq_of(P, s);
+        return blocks_of(q) * tiles_of(q) * P.n_kv;
+    };
+    const Census<decltype(count)> census(count, P.n_seqs);
+    if (census.total == 0) return;
+    int longest;
+    {
+        int most = 0;
+        for (int k = 0; k < census.per; ++k) {
+            const int s = lane * census.per + k;
+            if (s < P.n_seqs) most = max(most, tiles_of(seq_of(P, s)));
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+        longest = __builtin_amdgcn_readfirstlane(most);
+    }
+    const int share = max(max(KVQ_P8_LEAST_SHARE, (census.total + (int)gridDim.x - 1) / (int)gridDim.x), (longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES);
+    int pos = wg * share;
+    if (pos >= census.total) return;
+    const int range_end = min(census.total, pos + share);
+    int first;
+    int s = __builtin_amdgcn_readfirstlane(census.find(pos, first));
+    first = __builtin_amdgcn_readfirstlane(first);
+    Seq seq = seq_of(P, s);
+    while (pos < range_end) {
+        // ---- the piece: tiles t0 .. t1 - 1 of a unit
+        int tiles = tiles_of(seq), blocks = blocks_of(seq);
+        while (pos - first >= tiles * blocks * P.n_kv) {
+            first += tiles * blocks * P.n_kv;
+            seq = seq_of(P, ++s);
+            tiles = tiles_of(seq);
+            blocks = blocks_of(seq);
+        }
+        const int unit = (pos - first) / tiles, t0 = pos - first - unit * tiles, t1 = min(tiles, t0 + range_end - pos);
+        const int kv = unit / blocks, block = unit - kv * blocks;
+
+        int limit[R];
+        int most = 0, least = 0x7fffffff;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int f = block * RB + 16 * r + n, i = f / rows_per_token;
+            const bool real = i < seq.rows;
+            limit[r] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
+            most = max(most, real ? limit[r] : 0);
+            least = min(least, limit[r]);
+        }
+        if (wave < 4) {  // four channel groups of the rows, one a wavefront
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int f = block * RB + 16 * r + n, i = f / rows_per_token, rest = f - i * rows_per_token;
+                const int h = A.maps == 2 ? rest >> 1 : rest, map = A.maps == 2 ? rest & 1 : 0;
+                u32x4 w = {0, 0, 0, 0};
+                if (i < seq.rows && (A.maps == 1 || (wave >> 1) == map)) {
+                    w = *reinterpret_cast<const u32x4*>(A.q + (seq.row0 + i) * A.q_rs + (int64_t)(kv * A.gqa + h) * A.q_hs + 32 * wave + 8 * j);
+                    w ^= A.flip;
+                }
+                lds_q[r][wave][lane] = w;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            most = max(most, __shfl_xor(most, d));
+            least = min(least, __shfl_xor(least, d));
+        }
+        most = __builtin_amdgcn_readfirstlane(most);
+        least = __builtin_amdgcn_readfirstlane(least);
+        const int end = min(t1, (most + 31) >> 5);
+
+        State<R> st;
+        st.clear();
+        for (int from = t0 + wave; from < end; from += 64 * W) {
+            // the pages and scale words of the wavefront's next 64 tiles, one a lane
+            const int mine = from + lane * W;
+            const int page = mine < end ? page_of(P, s, mine >> (P.page_shift - 5)) : -1;
+            u32x2 words = {0, 0};
+            if (page >= 0) words = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)page * P.n_kv + kv) * 2);
+            const int todo = min(64, (end - from + W - 1) / W);
+            u32x4 kc[4], vc[4];
+            const auto at = [&](int k) {
+                const int pg = max(0, __builtin_amdgcn_readlane(page, k));
+                return tile_of(P, pg, kv, (from + k * W) & ((1 << (P.page_shift - 5)) - 1)) + lane * 16;
+            };
+            const auto load_k = [&](const uint8_t* p) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) kc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + c * 1024));
+            };
+            const auto load_v = [&](const uint8_t* p) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) vc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4096 + c * 1024));
+            };
+            load_k(at(0));
+            load_v(at(0));
+            for (int k = 0; k < todo; ++k) {
+                const uint8_t* const next = at(min(k + 1, todo - 1));
+                const int kw = __builtin_amdgcn_readlane(words[0], k), vw = __builtin_amdgcn_readlane(words[1], k);
+                const bool there = __builtin_amdgcn_readlane(page, k) >= 0;
+                const int tok = (from + k * W) * 32;
+                float4v sc[R][1][2];
+                asm volatile("" ::: "memory");  // (queries would be kept in registers)
+#pragma unroll
+                for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) sc[r][0][sub] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int grp = 0; grp < 4; ++grp) {
+                        const u32x4 w = kc[2 * sub + (grp >> 1)];
+                        const half8 a = widen(w[2 * (grp & 1)], w[2 * (grp & 1) + 1], 1.f);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) sc[r][0][sub] = mma(a, to_half8(lds_q[r][grp][lane]), sc[r][0][sub]);
+                    }
+                }
+                load_k(next);
+                if (there) {
+                    if (least < tok + 32) {
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            const int over = limit[r] - tok - 8 * j;
+#pragma unroll
+                            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    if (4 * sub + i >= over) sc[r][0][sub][i] = -INFINITY;
+                        }
+                    }
+                    uint32_t p[R][1][4];
+                    const float factor = A.scale_log2 * ldexpf(1.f, exponent_of(kw));
+#pragma unroll
+                    for (int r = 0; r < R; ++r) softmax_group<R, 1, false, true>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
+                    const float vs = value_scale(vw);
+                    const bool nan = (vw & KVQ_P8_NAN) != 0;
+#pragma unroll
+                    for (int nt = 0; nt < 8; ++nt) {
+                        uint32_t w[2] = {vc[nt >> 1][2 * (nt & 1)], vc[nt >> 1][2 * (nt & 1) + 1]};
+                        if (nan) {
+#pragma unroll
+                            for (int r = 0; r < R; ++r) {
+                                uint32_t x[2] = {w[0], w[1]};
+                                st.o[r][nt] += nan_codes(x, tok + 8 * j, limit[r]);
+                                if (r == R - 1) w[0] = x[0], w[1] = x[1];
+                            }
+                        }
+                        const half8 a = widen(w[0], w[1], vs);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
+                    }
+                }
+                load_v(next);
+            }
+        }
+
+        // ---- the wavefronts' states together, then the pieces of the unit, then the rows of the output
+        // (the thread's index afresh: what follows from it would be kept in registers through the loop above)
+        int fresh = threadIdx.x;
+        asm volatile("" : "+v"(fresh));
+        const int tid = fresh, lane = tid & 63, j = lane >> 4, n = lane & 15;
+        const int global0 = pos - t0, w0 = global0 / share, w1 = (global0 + tiles - 1) / share, pieces = w1 - w0 + 1;
+        const int real_rows = min(RB, seq.rows * rows_per_token - block * RB);
+        const auto slot = [&](int piece) { return A.part + (int64_t)(2 * (w0 + piece) + (piece == 0 ? 1 : 0)) * (R * (KVQ_PART_BYTES / 4)); };
+        const int row = tid >> 5, chunk = tid & 31;
+        float4v o[R];
+        float m[R], l[R], fine[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            __syncthreads();
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt) lds_o[wave][n][(4 * nt + j + n) & 31] = st.o[r][nt];
+            const float sum = quarters_sum(st.l[r]), fine_sum = quarters_sum(st.fine[r]);
+            if (lane < 16) lds_ml[wave][n] = float4v{st.m[r], sum, fine_sum, 0.f};
+            __syncthreads();
+            m[r] = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < W; ++w) m[r] = fmaxf(m[r], lds_ml[w][row][0]);
+            o[r] = float4v{0.f, 0.f, 0.f, 0.f};
+            l[r] = fine[r] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float4v ml = lds_ml[w][row];
+                const float weight = __builtin_amdgcn_exp2f(ml[0] - reference_of(m[r]));
+                o[r] += lds_o[w][row][(chunk + row) & 31] * weight;
+                l[r] += ml[1] * weight;
+                fine[r] += ml[2] * weight;
+            }
+        }
+        bool mine = true;
+        if (pieces > 1) {
+            float* const to = slot(wg - w0);
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(to, 0, R * KVQ_PART_BYTES, 0x00020000);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (16 * r + row >= real_rows) continue;
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[r]), buf, r * KVQ_PART_BYTES + tid * 16, 0, 16);
+                if (chunk == 0)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{m[r], l[r], fine[r], 0.f}), buf,
+                                                           r * KVQ_PART_BYTES + KVQ_PART_O_FLOATS * 4 + row * 16, 0, 16);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) {
+                uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
+                const uint32_t got = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const bool last = got == (uint32_t)pieces - 1u;
+                if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                lds_last = last ? 1 : 0;
+            }
+            __syncthreads();
+            mine = lds_last != 0;
+            asm volatile("" ::: "memory");
+            if (mine) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (16 * r + row >= real_rows) continue;
+                    m[r] = -INFINITY;
+                    l[r] = fine[r] = 0.f;
+                    o[r] = float4v{0.f, 0.f, 0.f, 0.f};
+                    for (int k = 0; k < pieces; ++k) {
+                        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot(k), 0, R * KVQ_PART_BYTES, 0x00020000);
+                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, r * KVQ_PART_BYTES + KVQ_PART_O_FLOATS * 4 + row * 16, 0, 16));
+                        const float4v x = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, r * KVQ_PART_BYTES + tid * 16, 0, 16));
+                        const float m_new = fmaxf(m[r], ml[0]), ref = reference_of(m_new);
+                        const float a = __builtin_amdgcn_exp2f(m[r] - ref), b = __builtin_amdgcn_exp2f(ml[0] - ref);
+                        o[r] = o[r] * a + x * b;
+                        l[r] = l[r] * a + ml[1] * b;
+                        fine[r] = fine[r] * a + ml[2] * b;
+                        m[r] = m_new;
+                    }
+                }
+            }
+        }
+        if (mine) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int f = block * RB + 16 * r + row, i = f / rows_per_token, rest = f - i * rows_per_token;
+                float4v x = o[r] * (2.f * kvq_flash::inverse_of(l[r]));
+                const int h = kv * A.gqa + (A.maps == 2 ? rest >> 1 : rest);
+                const bool real = i < seq.rows;
+                if (A.maps == 2) {
+                    // the second map's row lies 32 lanes on
+                    const float lam = real ? A.lambda[h] : 0.f;
+                    float square = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = x[e] - lam * __shfl_xor(x[e], 32);
+                        square = fmaf(x[e], x[e], square);
+                    }
+                    if (A.weight) {
+#pragma unroll
+                        for (int d = 1; d < 32; d <<= 1) square += __shfl_xor(square, d);
+                        const float mean = square * (1.f / KVQ_D) + A.eps;
+                        x *= mean > 0.f ? 1.f / sqrtf(mean) : mean;  // (nothing but zeros and no eps: zeros; NaN stays)
+                        x *= *reinterpret_cast<const float4v*>(A.weight + 4 * chunk);
+                    }
+                    x *= A.out_scale;
+                }
+                if (!real || (A.maps == 2 && (rest & 1))) continue;
+                const int64_t to = (seq.row0 + i) * A.o_rs + h * A.o_hs;
+                void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
+                kvq_flash::store_out4(dst, A.out_fp32, 4 * chunk, x);
+                if (A.lse && chunk == 0)
+                    A.lse[h * A.lse_hs + seq.row0 + i] = fine[r] == 0.f ? -INFINITY : (m[r] + __builtin_amdgcn_logf(fine[r])) * 0.69314718055994530942f;
+            }
+        }
+        pos += t1 - t0;
+    }
+}
+
+constexpr uint64_t kCounterBytes = (uint64_t)KVQ_P8_GROUPS * KVQ_P8_COUNTER_STRIDE * 4;
+
+bool heads_ok(int32_t n_q, int32_t n_kv) { return n_q >= 1 && n_q % n_kv == 0 && n_q / n_kv <= KVQ_MAX_GQA; }
+
+// The launches of a call: whether rows are few enough for blocks of 16, and how many workgroups.
+struct Plan {
+    int r;
+    int64_t groups;
+    uint64_t bytes;
+};
+bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
+    const int64_t rows = (int64_t)P.max_rows * gqa * maps;
+    plan.r = rows <= 16 ? 1 : 2;
+    const int64_t blocks = (rows + 16 * plan.r - 1) / (16 * plan.r), tiles = (int64_t)P.table_pages << (P.page_shift - 5);
+    const int64_t seqs = P.n_seqs;
+    if (seqs && blocks * tiles > INT32_MAX / 2 / seqs / P.n_kv) return false;
+    const int64_t total = blocks * tiles * seqs * P.n_kv;
+    plan.groups = std::min<int64_t>(KVQ_P8_GROUPS, (total + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
+    plan.bytes = kCounterBytes + (uint64_t)plan.groups * 2 * plan.r * KVQ_PART_BYTES;
+    return true;
+}
+
+kvq_status_t attend(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q, const kvq_paged8_rows_t* out,
+                    int32_t n_q_heads, int32_t out_is_fp32, float softmax_scale, void* workspace, uint64_t bytes, AttnArgs& A, hipStream_t stream) {
+    Plan plan;
+    if (!kvq_p8_args(cache, batch, A.p) || !heads_ok(n_q_heads, cache->n_kv_heads)) return KVQ_E_INVALID;
+    if (!kvq_p8_rows_ok(q, batch, 8) || !kvq_p8_rows_ok(out, batch, out_is_fp32 ? 4 : 8) || !kvq_p8_rows_apart(out, batch, n_q_heads)) return KVQ_E_INVALID;
+    if (!std::isfinite(softmax_scale) || !plan_of(A.p, n_q_heads / cache->n_kv_heads, A.maps, plan)) return KVQ_E_INVALID;
+    if (!A.p.n_seqs || !A.p.n_rows) return KVQ_OK;
+    if (!kvq_p8_aligned(workspace, 16) || bytes < plan.bytes) return KVQ_E_INVALID;
+    A.q = static_cast<const _Float16*>(q->data_dev);
+    A.out = const_cast<void*>(out->data_dev);
+    A.q_rs = q->row_stride; A.q_hs = q->head_stride;
+    A.o_rs = out->row_stride; A.o_hs = out->head_stride;
+    A.lse_hs = A.p.n_rows;
+    A.gqa = n_q_heads / cache->n_kv_heads;
+    A.out_fp32 = out_is_fp32 ? 1 : 0;
+    const float scale = softmax_scale != 0.f ? softmax_scale : 1.0f / std::sqrt((float)(KVQ_D / A.maps));
+    A.scale_log2 = std::fabs(scale) * 1.44269504088896340736f;
+    A.flip = scale < 0.f ? 0x80008000u : 0u;
+    A.counters = static_cast<uint32_t*>(workspace);
+    A.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterBytes);
+    if (plan.r == 1) hipLaunchKernelGGL(kvq_paged8_ranges_kernel<1>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
+    else hipLaunchKernelGGL(kvq_paged8_ranges_kernel<2>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
+    return hipGetLastError() == hipSuccess ? KVQ_OK : KVQ_E_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t kvq_paged8_workspace_bytes(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, int32_t n_q_heads, int32_t two_maps) {
+    KvqP8 P{};
+    Plan plan;
+    if (!kvq_p8_args(cache, batch, P) || !heads_ok(n_q_heads, P.n_kv)) return 0;
+    return plan_of(P, n_q_heads / P.n_kv, two_maps ? 2 : 1, plan) ? plan.bytes : 0;
+}
+
+kvq_status_t kvq_paged8_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,
+                                  const kvq_paged8_rows_t* out_dev, int32_t n_q_heads, int32_t out_is_fp32, float softmax_scale,
+                                  float* lse_dev, void* workspace_dev, uint64_t workspace_bytes, void* hip_stream) {
+    AttnArgs A{};
+    if (reinterpret_cast<uintptr_t>(lse_dev) & 3u) return KVQ_E_INVALID;
+    A.lse = lse_dev;
+    A.maps = 1;
+    return attend(cache, batch, q_dev, out_dev, n_q_heads, out_is_fp32, softmax_scale, workspace_dev, workspace_bytes, A,
+                  static_cast<hipStream_t>(hip_stream));
+}
+
+kvq_status_t kvq_paged8_diff_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,
+                                       const float* lambda_dev, const kvq_paged8_rows_t* out_dev, int32_t n_q_heads, int32_t out_is_fp32,
+                                       float softmax_scale, const float* norm_weight_dev, float norm_eps, float out_scale,
+                                       void* workspace_dev, uint64_t workspace_bytes, void* hip_stream) {
+    AttnArgs A{};
+    if (!kvq_p8_aligned(lambda_dev, 4) || (norm_weight_dev && !kvq_p8_aligned(norm_weight_dev, 16))) return KVQ_E_INVALID;
+    if (!std::isfinite(out_scale) || !std::isfinite(norm_eps) || norm_eps < 0.f) return KVQ_E_INVALID;
+    A.lambda = lambda_dev;
+    A.weight = norm_weight_dev;
+    A.eps = norm_eps;
+    A.out_scale = out_scale;
+    A.maps = 2;
+    return attend(cache, batch, q_dev, out_dev, n_q_heads, out_is_fp32, softmax_scale, workspace_dev, workspace_bytes, A,
+                  static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"
