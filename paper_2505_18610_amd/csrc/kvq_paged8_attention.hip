@@ -25,6 +25,7 @@ using kvq_flash::to_half8;
 #define KVQ_P8_GROUPS 512       // workgroups of a launch over ranges of tiles, at most
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
 #define KVQ_P8_LEAST_SHARE 8    // tiles of a workgroup, at least
+#define KVQ_P8_LEAST_CHUNK 16   // of a workgroup with a chunk
 #define KVQ_P8_MOST_PIECES 128  // of a unit
 
 struct AttnArgs {
@@ -37,6 +38,7 @@ struct AttnArgs {
     float* part;
     int64_t q_rs, q_hs, o_rs, o_hs, lse_hs;
     int32_t gqa, maps, out_fp32;   // gqa: query heads of a KV head
+    int32_t least_rows;            // sequences with more flat rows (of one map) are chunks
     float scale_log2, eps, out_scale;
     uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
 };
@@ -46,6 +48,10 @@ __device__ inline half8 widen(uint32_t lo, uint32_t hi, float scale) {
     const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
     const half2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
     return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// What a raw score times gives its place in the softmax, in log2 units (kept from zero and infinity, which would make NaN of masked scores).
+__device__ inline float score_factor(float scale_log2, int word) {
+    return fminf(fmaxf(ldexpf(scale_log2, exponent_of(word)), 0x1p-126f), 0x1p126f);
 }
 // Values are taken times 1/2 and outputs times 2: a rounded code may stand for up to 2^16, beyond fp16.
 __device__ inline float value_scale(int word) { return ldexpf(0.5f, exponent_of(word)); }
@@ -88,7 +94,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
     const int wg = blockIdx.x, rows_per_token = A.gqa * A.maps;
 
-    const auto blocks_of = [&](const Seq& q) { return (q.rows * rows_per_token + RB - 1) / RB; };
+    const auto blocks_of = [&](const Seq& q) { return q.rows * A.gqa > A.least_rows ? 0 : (q.rows * rows_per_token + RB - 1) / RB; };
     const auto tiles_of = [&](const Seq& q) { return max(1, (q.tokens + 31) >> 5); };
     const auto count = [&](int s) {
         const Seq q = seq_of(P, s);
@@ -217,7 +223,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
                         }
                     }
                     uint32_t p[R][1][4];
-                    const float factor = A.scale_log2 * ldexpf(1.f, exponent_of(kw));
+                    const float factor = score_factor(A.scale_log2, kw);
 #pragma unroll
                     for (int r = 0; r < R; ++r) softmax_group<R, 1, false, true>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
                     const float vs = value_scale(vw);
@@ -357,25 +363,410 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     }
 }
 
+// ---- Sequences with many rows: chunks of prompts
+
+// Probabilities of TT tiles for row group r as kvq_flash.h's softmax_group, the tiles with a factor each.
+template <int R, int TT>
+__device__ inline void softmax_tiles(State<R>& st, int r, const float4v (&s)[TT][2], const float (&factor)[TT], bool fine, uint32_t (&p)[TT][4]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, s[t][sub][i]);
+        top = fmaxf(top, most * factor[t]);
+    }
+    if (__any(top > st.m[r] + (KVQ_BELOW + KVQ_FOLLOW))) {
+        const float m_new = fmaxf(st.m[r], kvq_flash::quarters_max(top) - KVQ_BELOW);
+        const float alpha = __builtin_amdgcn_exp2f(st.m[r] - reference_of(m_new));
+        st.l[r] *= alpha;
+        st.fine[r] *= alpha;
+#pragma unroll
+        for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= alpha;
+        st.m[r] = m_new;
+    }
+    const float ref = reference_of(st.m[r]);
+    const half2v ones = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        float e[2][4];
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[sub][i] = __builtin_amdgcn_exp2f(fmaf(s[t][sub][i], factor[t], -ref));
+        if (fine) {
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.fine[r] += e[sub][i];
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            p[t][v] = kvq_flash::pack2(e[v >> 1][2 * (v & 1)], e[v >> 1][2 * (v & 1) + 1]);
+            const uint32_t two = p[t][v];
+            st.l[r] = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), ones, st.l[r], false);
+        }
+    }
+}
+
+// Where the work of the units lies on one line that workgroups take equal shares of.  A block's length on it is its tiles, by the tokens that its last
+// row sees, and kLead for what a block costs beside them; blocks of a KV head lie one after the other, KV heads, sequences.
+struct Line {
+    int rows, seen0, per_token, blocks;  // flat rows, tokens that the rows of the first token see, flat rows of a token, blocks
+    int length;                          // of all blocks of one KV head
+    static constexpr int kLead = 4;
+    template <int RB>
+    __device__ int at(int b) const {  // where block b begins
+        return (int)(((int64_t)b * seen0 + (int64_t)b * (b + 1) / 2 * RB / per_token) >> 5) + kLead * b;
+    }
+};
+template <int RB>
+__device__ inline Line line_of(const Seq& q, int per_token, int least_rows) {
+    Line x;
+    x.rows = q.rows * per_token;
+    x.seen0 = max(0, q.tokens - q.rows);
+    x.per_token = per_token;
+    x.blocks = x.rows > least_rows ? (x.rows + RB - 1) / RB : 0;
+    x.length = x.blocks ? x.at<RB>(x.blocks) : 0;
+    return x;
+}
+
+// RG groups of 16 rows a wavefront, MAPS states of each; four wavefronts with rows of their own share the tiles: two an iteration, widened to fp16 once on
+// their way into LDS, where the next ones are put while these are computed on.
+template <int RG, int MAPS, int TT>
+__global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
+    constexpr int R = RG * MAPS, RB = 64 * RG, NT = 2, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+    __shared__ int lds_last;
+    const KvqP8& P = A.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
+    const int per_page = P.page_shift - 5;
+
+    const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.least_rows); };
+    const auto count = [&](int s) { return line(seq_of(P, s)).length * P.n_kv; };
+    const Census<decltype(count)> census(count, P.n_seqs);
+    if (census.total == 0) return;
+    const int groups = gridDim.x, share = max(KVQ_P8_LEAST_CHUNK, (census.total + groups - 1) / groups);
+    // neighbours on the line go to one XCD, whose L2 then holds the keys and values that they have in common
+    const int wg = groups % 8 == 0 ? (blockIdx.x & 7) * (groups >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    int pos = wg * share;
+    if (pos >= census.total) return;
+    const int range_end = min(census.total, pos + share);
+    int first;
+    int s = __builtin_amdgcn_readfirstlane(census.find(pos, first));
+    first = __builtin_amdgcn_readfirstlane(first);
+    Seq seq = seq_of(P, s);
+    Line ln = line(seq);
+    while (pos < range_end) {
+        while (pos - first >= ln.length * P.n_kv) {
+            first += ln.length * P.n_kv;
+            seq = seq_of(P, ++s);
+            ln = line(seq);
+        }
+        const int kv = (pos - first) / ln.length, in_head = pos - first - kv * ln.length;
+        int block = 0;
+        for (int step = 1 << 26; step; step >>= 1)
+            if (block + step < ln.blocks && ln.at<RB>(block + step) <= in_head) block += step;
+        const int unit = pos - in_head + ln.at<RB>(block), length = ln.at<RB>(block + 1) - ln.at<RB>(block);  // the unit's place on the line
+        const int unit_end = min(range_end, unit + length);
+
+        int limit[RG];
+        half8 q[RG][4];
+        int most = 0, least = 0x7fffffff;
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            const int f = block * RB + wave * 16 * RG + 16 * g + n, i = f / A.gqa, h = f - i * A.gqa;
+            const bool real = f < ln.rows;
+            limit[g] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
+            most = max(most, real ? limit[g] : 0);
+            least = min(least, limit[g]);
+            const _Float16* const src = A.q + (seq.row0 + (real ? i : 0)) * A.q_rs + (int64_t)(kv * A.gqa + (real ? h : 0)) * A.q_hs + 8 * j;
+#pragma unroll
+            for (int grp = 0; grp < 4; ++grp) {
+                u32x4 w = *reinterpret_cast<const u32x4*>(src + 32 * grp);
+                w ^= A.flip;
+                if (!real) w = u32x4{0, 0, 0, 0};
+                q[g][grp] = to_half8(w);
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            most = max(most, __shfl_xor(most, d));
+            least = min(least, __shfl_xor(least, d));
+        }
+        most = __builtin_amdgcn_readfirstlane(most);
+        least = __builtin_amdgcn_readfirstlane(least);
+        // the block's tiles: those that its last row sees
+        const int last_row = min(ln.rows, (block + 1) * RB) - 1;
+        const int tiles = (max(0, seq.tokens - seq.rows + last_row / A.gqa + 1) + 31) >> 5;
+        const auto tile_at = [&](int x) { return __builtin_amdgcn_readfirstlane((int)((int64_t)(x - unit) * tiles / length)); };
+        const int t0 = tile_at(pos), t1 = tile_at(unit_end);
+
+        State<R> st;
+        st.clear();
+
+        // pages and scale words of 64 tiles, one a lane, and of the 64 behind them
+        int batch = t0, page, page_next;
+        u32x2 words, words_next;
+        const auto pages_from = [&](int t) { return t + lane < t1 ? page_of(P, s, (t + lane) >> per_page) : -1; };
+        const auto words_of = [&](int pg) {
+            u32x2 w = {0, 0};
+            if (pg >= 0) w = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)pg * P.n_kv + kv) * 2);
+            return w;
+        };
+        page = pages_from(batch);
+        page_next = pages_from(batch + 64);
+        words = words_of(page);
+        words_next = u32x2{0, 0};
+
+        struct Tile { int page, kw, vw; } now[NT], next[NT];
+        u32x4 kr[NT], vr[NT];
+        const auto load = [&](int t) {  // a quarter of every tile a wavefront
+            if (t - batch >= 64) {
+                page = page_next;
+                words = words_next;
+                batch += 64;
+                page_next = pages_from(batch + 64);
+            }
+            if (t - batch == 32) words_next = words_of(page_next);
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                next[x].page = __builtin_amdgcn_readlane(page, t - batch + x);
+                next[x].kw = __builtin_amdgcn_readlane(words[0], t - batch + x);
+                next[x].vw = __builtin_amdgcn_readlane(words[1], t - batch + x);
+                const uint8_t* const at = tile_of(P, max(0, next[x].page), kv, (t + x) & ((1 << per_page) - 1)) + wave * 1024 + lane * 16;
+                kr[x] = *reinterpret_cast<const u32x4*>(at);
+                vr[x] = *reinterpret_cast<const u32x4*>(at + 4096);
+            }
+        };
+        const auto store = [&](int buf) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                uint8_t* const kt = lds + buf * STAGE + x * TILE + lane * 16;
+                uint8_t* const vt = kt + KVQ_FLASH_TILE_BYTES;
+                const float vs = value_scale(next[x].vw);
+                u32x4 v = vr[x];
+                if (next[x].page < 0) v = u32x4{0, 0, 0, 0};
+                if (next[x].vw & KVQ_P8_NAN) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+#pragma unroll
+                        for (int b = 0; b < 32; b += 8)
+                            if (((v[d] >> b) & 0x7fu) == 0x7fu) v[d] &= ~(0xffu << b);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // chunk `wave` of the K tile: sub-tile wave / 2, channel groups 2 (wave % 2) + h; of the V tile: channel block 2 wave + h
+                    *reinterpret_cast<half8*>(kt + (4 * (wave >> 1) + 2 * (wave & 1) + h) * 1024) = widen(kr[x][2 * h], kr[x][2 * h + 1], 1.f);
+                    *reinterpret_cast<half8*>(vt + (2 * wave + h) * 1024) = widen(v[2 * h], v[2 * h + 1], vs);
+                }
+            }
+        };
+        if (t0 < t1) {
+            load(t0);
+            store(0);
+        }
+        __syncthreads();
+        int buf = 0;
+        for (int t = t0; t < t1; t += NT) {
+            const bool more = t + NT < t1;
+#pragma unroll
+            for (int x = 0; x < NT; ++x) now[x] = next[x];
+            if (more) load(t + NT);
+            if (t * 32 < most) {  // (behind what its rows see a wavefront only loads)
+#pragma unroll
+                for (int x0 = 0; x0 < NT; x0 += TT) {
+                    const uint8_t* const kt = lds + buf * STAGE + x0 * TILE + lane * 16;
+                    const uint8_t* const vt = kt + KVQ_FLASH_TILE_BYTES;
+                    const int tok = (t + x0) * 32;
+                    float4v sc[R][TT][2];
+#pragma unroll
+                    for (int x = 0; x < TT; ++x)
+#pragma unroll
+                        for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+                            for (int r = 0; r < R; ++r) sc[r][x][sub] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int grp = 0; grp < 4; ++grp) {
+                                const half8 a = to_half8(*reinterpret_cast<const u32x4*>(kt + x * TILE + (sub * 4 + grp) * 1024));
+#pragma unroll
+                                for (int g = 0; g < RG; ++g) {
+                                    float4v& to = sc[MAPS * g + (MAPS == 2 ? grp >> 1 : 0)][x][sub];
+                                    to = mma(a, q[g][grp], to);
+                                }
+                            }
+                        }
+                    bool masked = least < tok + TT * 32;
+                    float factor[TT];
+#pragma unroll
+                    for (int x = 0; x < TT; ++x) {
+                        masked = masked || now[x0 + x].page < 0;
+                        factor[x] = score_factor(A.scale_log2, now[x0 + x].kw);
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int g = 0; g < RG; ++g)
+#pragma unroll
+                            for (int x = 0; x < TT; ++x) {
+                                const int over = (now[x0 + x].page < 0 ? 0 : limit[g] - tok - 32 * x) - 8 * j;
+#pragma unroll
+                                for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+                                    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                                        for (int i = 0; i < 4; ++i)
+                                            if (4 * sub + i >= over) sc[MAPS * g + m][x][sub][i] = -INFINITY;
+                            }
+                    }
+                    uint32_t p[R][TT][4];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) softmax_tiles<R, TT>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
+#pragma unroll
+                    for (int x = 0; x < TT; ++x) {
+                        if ((now[x0 + x].vw & KVQ_P8_NAN) && now[x0 + x].page >= 0) {
+                            const uint8_t* const at = tile_of(P, now[x0 + x].page, kv, (t + x0 + x) & ((1 << per_page) - 1)) + 4096 + lane * 16;
+#pragma unroll
+                            for (int nt = 0; nt < 8; ++nt) {
+                                const u32x2 w = *reinterpret_cast<const u32x2*>(at + (nt >> 1) * 1024 + (nt & 1) * 8);
+#pragma unroll
+                                for (int r = 0; r < R; ++r) {
+                                    uint32_t y[2] = {w[0], w[1]};
+                                    st.o[r][nt] += nan_codes(y, tok + 32 * x + 8 * j, limit[r / MAPS]);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < 8; ++nt) {
+                            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(vt + x * TILE + nt * 1024));
+#pragma unroll
+                            for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
+                        }
+                    }
+                }
+            }
+            if (more) store(buf ^ 1);
+            __syncthreads();
+            buf ^= 1;
+        }
+
+        // ---- the pieces of a unit that lies in several workgroups' shares, joined by the last of them in the order of the line
+        const int w0 = unit / share, w1 = (unit + length - 1) / share, pieces = w1 - w0 + 1;
+        bool mine = true;
+        if (pieces > 1) {
+            constexpr int SLOT = 4 * R * KVQ_PART_BYTES;
+            const auto slot = [&](int k) {
+                return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(A.part) + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * SLOT, 0, SLOT, 0x00020000);
+            };
+            const __amdgpu_buffer_rsrc_t to = slot(wg - w0);
+            const int own_at = wave * R * KVQ_PART_BYTES + lane * 16;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int at = own_at + r * KVQ_PART_BYTES;
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, st.o[r][nt]), to, at + nt * 1024, 0, 16);
+                const float l = quarters_sum(st.l[r]), fine = quarters_sum(st.fine[r]);
+                if (j == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st.m[r], l, fine, 0.f}), to, at + 8192, 0, 16);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
+                const uint32_t got = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const bool last = got == (uint32_t)pieces - 1u;
+                if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                lds_last = last ? 1 : 0;
+            }
+            __syncthreads();
+            mine = lds_last != 0;
+            asm volatile("" ::: "memory");
+            if (mine) {
+                st.clear();
+                for (int k = 0; k < pieces; ++k) {
+                    const __amdgpu_buffer_rsrc_t from = slot(k);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const int at = own_at + r * KVQ_PART_BYTES;
+                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at - j * 256 + 8192, 0, 16));
+                        float a, b;
+                        kvq_flash::join_row<R>(st, r, ml[0], j == 0 ? ml[1] : 0.f, j == 0 ? ml[2] : 0.f, a, b);
+#pragma unroll
+                        for (int nt = 0; nt < 8; ++nt)
+                            st.o[r][nt] = st.o[r][nt] * a + __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + nt * 1024, 0, 16)) * b;
+                    }
+                }
+            }
+        }
+        if (mine) {
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                const int f = block * RB + wave * 16 * RG + 16 * g + n, i = f / A.gqa, h = kv * A.gqa + f - i * A.gqa;
+                const bool real = f < ln.rows;
+                float inv[MAPS], fine = 0.f;
+#pragma unroll
+                for (int m = 0; m < MAPS; ++m) inv[m] = 2.f * kvq_flash::inverse_of(quarters_sum(st.l[MAPS * g + m]));
+                float4v x[8];
+                float square = 0.f;
+                const float lam = MAPS == 2 && real ? A.lambda[h] : 0.f;
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) {
+                    x[nt] = st.o[MAPS * g][nt] * inv[0];
+                    if (MAPS == 2) {
+                        x[nt] = x[nt] - st.o[R - 1 - (MAPS * (RG - 1 - g))][nt] * inv[MAPS - 1] * lam;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) square = fmaf(x[nt][e], x[nt][e], square);
+                    }
+                }
+                if (MAPS == 2) {
+                    float by = A.out_scale;
+                    if (A.weight) {
+                        const float mean = quarters_sum(square) * (1.f / KVQ_D) + A.eps;
+                        by *= mean > 0.f ? 1.f / sqrtf(mean) : mean;
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < 8; ++nt) {
+                        x[nt] *= by;
+                        if (A.weight) x[nt] *= *reinterpret_cast<const float4v*>(A.weight + 16 * nt + 4 * j);
+                    }
+                } else {
+                    fine = quarters_sum(st.fine[g]);
+                }
+                if (!real) continue;
+                const int64_t to = (seq.row0 + i) * A.o_rs + h * A.o_hs;
+                void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) kvq_flash::store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x[nt]);
+                if (MAPS == 1 && A.lse && j == 0)
+                    A.lse[h * A.lse_hs + seq.row0 + i] = fine == 0.f ? -INFINITY : (st.m[g] + __builtin_amdgcn_logf(fine)) * 0.69314718055994530942f;
+            }
+        }
+        pos = unit_end;
+    }
+}
+
 constexpr uint64_t kCounterBytes = (uint64_t)KVQ_P8_GROUPS * KVQ_P8_COUNTER_STRIDE * 4;
 
 bool heads_ok(int32_t n_q, int32_t n_kv) { return n_q >= 1 && n_q % n_kv == 0 && n_q / n_kv <= KVQ_MAX_GQA; }
 
-// The launches of a call: whether rows are few enough for blocks of 16, and how many workgroups.
+// The launches of a call: over ranges of tiles for sequences of few rows, of more where there may be any.  Either uses the workspace from its start.
+constexpr int kFewRows = 64;  // flat rows of one map
 struct Plan {
-    int r;
-    int64_t groups;
+    int r;                  // groups of 16 rows of the first launch
+    int64_t groups, chunk;  // workgroups
     uint64_t bytes;
 };
 bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
-    const int64_t rows = (int64_t)P.max_rows * gqa * maps;
+    const int64_t most = (int64_t)P.max_rows * gqa, rows = std::min<int64_t>(most, kFewRows) * maps;
     plan.r = rows <= 16 ? 1 : 2;
-    const int64_t blocks = (rows + 16 * plan.r - 1) / (16 * plan.r), tiles = (int64_t)P.table_pages << (P.page_shift - 5);
-    const int64_t seqs = P.n_seqs;
-    if (seqs && blocks * tiles > INT32_MAX / 2 / seqs / P.n_kv) return false;
-    const int64_t total = blocks * tiles * seqs * P.n_kv;
+    const int64_t tiles = (int64_t)P.table_pages << (P.page_shift - 5), heads = (int64_t)P.n_seqs * P.n_kv;
+    // blocks of 16 rows bound both: every number on either line stays below 2^30
+    if (heads && (most * maps + 15) / 16 * (tiles + 8 + P.max_rows / 32) > (1 << 30) / heads) return false;
+    const int64_t total = (rows + 16 * plan.r - 1) / (16 * plan.r) * tiles * heads;
     plan.groups = std::min<int64_t>(KVQ_P8_GROUPS, (total + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
-    plan.bytes = kCounterBytes + (uint64_t)plan.groups * 2 * plan.r * KVQ_PART_BYTES;
+    const int64_t line = ((most + 63) / 64) * (tiles + 8 + P.max_rows / 32) * heads;
+    plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
+    plan.bytes = kCounterBytes + 2 * (uint64_t)KVQ_PART_BYTES * std::max<uint64_t>(plan.groups * plan.r, plan.chunk * 4 * (maps == 1 ? 2 : 4));
     return true;
 }
 
@@ -399,8 +790,13 @@ kvq_status_t attend(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, 
     A.flip = scale < 0.f ? 0x80008000u : 0u;
     A.counters = static_cast<uint32_t*>(workspace);
     A.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterBytes);
+    A.least_rows = kFewRows;
     if (plan.r == 1) hipLaunchKernelGGL(kvq_paged8_ranges_kernel<1>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     else hipLaunchKernelGGL(kvq_paged8_ranges_kernel<2>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
+    if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
+    if (!plan.chunk) return KVQ_OK;
+    if (A.maps == 1) hipLaunchKernelGGL((kvq_paged8_chunk_kernel<2, 1, 2>), dim3((unsigned)plan.chunk), dim3(256), 0, stream, A);
+    else hipLaunchKernelGGL((kvq_paged8_chunk_kernel<1, 2, 2>), dim3((unsigned)plan.chunk), dim3(256), 0, stream, A);
     return hipGetLastError() == hipSuccess ? KVQ_OK : KVQ_E_HIP;
 }
 
