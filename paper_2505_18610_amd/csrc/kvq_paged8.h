@@ -61,31 +61,39 @@ __device__ inline uint8_t* tile_of(const KvqP8& P, int page, int kv, int tile) {
 }
 __device__ inline int exponent_of(int word) { return (word & 0xff) - KVQ_P8_BIAS; }
 
-// Things counted by sequence (at most 64 x 64 sequences, the sum below 2^31), by a whole wavefront: how many there are, the most of one
-// sequence, and which sequence the one with a given number belongs to.
+// Sums over the lanes of a wavefront up to and with each lane's own, by data-parallel moves: within rows of 16, then row by row.
+__device__ inline int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+    return x;
+}
+__device__ inline int wave_max(int x) {  // of values of at least zero, in every lane
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Things counted by sequence (at most 64 x 64 sequences, the sum below 2^31), by a whole wavefront: how many
+// there are, and which sequence the one with a given number belongs to.
 template <class Count>
 struct Census {
     const Count& count;
-    int n, per, lane, mine, upto, total, most;
-    __device__ Census(const Count& c, int n_seqs) : count(c), n(n_seqs), per((n_seqs + 63) >> 6), lane(threadIdx.x & 63), mine(0), most(0) {
+    int n, per, lane, mine, upto, total;
+    __device__ Census(const Count& c, int n_seqs) : count(c), n(n_seqs), per((n_seqs + 63) >> 6), lane(threadIdx.x & 63), mine(0) {
         for (int k = 0; k < per; ++k) {
-            const int s = lane * per + k, x = s < n ? count(s) : 0;
-            mine += x;
-            most = max(most, x);
+            const int s = lane * per + k;
+            mine += s < n ? count(s) : 0;
         }
-        upto = scan(mine);
+        upto = wave_scan(mine);
         total = __builtin_amdgcn_readlane(upto, 63);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
-        most = __builtin_amdgcn_readfirstlane(most);
-    }
-    __device__ int scan(int x) const {
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
-        }
-        return x;
     }
     // The sequence of thing p (0 <= p < total) and, in `first`, the number of the sequence's first one.
     __device__ int find(int p, int& first) const {
@@ -94,7 +102,7 @@ struct Census {
             first = before;
             return at;
         }
-        const int s = at * per + lane, x = lane < per && s < n ? count(s) : 0, sum = before + scan(x);
+        const int s = at * per + lane, x = lane < per && s < n ? count(s) : 0, sum = before + wave_scan(x);
         const int k = __builtin_ctzll(__ballot(sum > p));
         first = __builtin_amdgcn_readlane(sum - x, k);
         return at * per + k;

@@ -76,13 +76,83 @@ __device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
 }
 
 // A unit: the rows of one block of one KV head of one sequence.  Rows follow one another token by token, of a token head by head, of a head
-// map by map; a block has 16 R of them.
-struct Unit {
-    int kv, block, tiles;
+// map by map; a block has 16 R of them.  Units of many tiles are cut into pieces of `share` tiles at most, one workgroup each: where the units
+// are few, of the smallest share that leaves no more pieces than the device takes workgroups at a time (a workgroup that came behind them would
+// have the device for itself), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
+struct Piece {
+    int seq, unit, tiles, pieces, piece;
+    int slot;  // of the unit's first piece among those of all units that are cut
+};
+struct Cuts {
+    struct Shape { int tiles, units; };
+    const Shape* all;  // of all sequences, where they are more than lanes
+    Shape mine;
+    int n, per, lane, share;
+
+    // over this lane's sequences
+    template <class F>
+    __device__ int sum(F f) const {
+        if (per == 1) return f(mine);
+        int x = 0;
+        for (int k = 0; k < per; ++k)
+            if (lane * per + k < n) x += f(all[lane * per + k]);
+        return x;
+    }
+    template <class F>
+    __device__ int total(F f) const { return __builtin_amdgcn_readlane(wave_scan(sum(f)), 63); }
+    __device__ int cuts_of(Shape x) const { return (x.tiles + share - 1) / share; }
+
+    __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_) : all(shapes), mine(own), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
+        const int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
+        int longest = 0;
+        sum([&](Shape x) { longest = max(longest, x.units ? x.tiles : 0); return 0; });
+        longest = wave_max(longest);
+        const int wanted = KVQ_P8_GROUPS;
+        int low = max(max(KVQ_P8_LEAST_SHARE, (tiles + wanted - 1) / wanted), (longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES);
+        share = low;
+        if (2 * units > wanted) return;
+        int high = max(low, (tiles + wanted - units - 1) / (wanted - units));  // enough: a unit has at most one piece more than its tiles by the share
+        while (high - low > low >> 4) {
+            share = (low + high) >> 1;
+            if (total([&](Shape x) { return x.units * cuts_of(x); }) <= wanted) high = share;
+            else low = share + 1;
+        }
+        share = high;
+    }
+    // Piece `id`, the same in all lanes.
+    __device__ bool find(int id, Piece& p) const {
+        const auto pieces = [&](Shape x) { return x.units * cuts_of(x); };
+        const auto cut = [&](Shape x) { const int c = cuts_of(x); return c > 1 ? x.units * c : 0; };
+        int x = sum(pieces), y = sum(cut), upto = wave_scan(x), cut_upto = wave_scan(y);
+        uint64_t behind = __ballot(upto > id);
+        if (!behind) return false;
+        int at = __builtin_ctzll(behind);
+        int before = __builtin_amdgcn_readlane(upto - x, at), slots = __builtin_amdgcn_readlane(cut_upto - y, at);
+        Shape s = mine;
+        p.seq = at;
+        if (per > 1) {  // among that lane's sequences, one a lane
+            const int i = at * per + lane;
+            s = lane < per && i < n ? all[i] : Shape{1, 0};
+            x = pieces(s);
+            y = cut(s);
+            upto = before + wave_scan(x);
+            cut_upto = slots + wave_scan(y);
+            at = __builtin_ctzll(__ballot(upto > id));
+            before = __builtin_amdgcn_readlane(upto - x, at);
+            slots = __builtin_amdgcn_readlane(cut_upto - y, at);
+            p.seq = __builtin_amdgcn_readlane(i, at);
+        }
+        p.tiles = __builtin_amdgcn_readlane(s.tiles, at);
+        p.pieces = (p.tiles + share - 1) / share;
+        p.unit = (id - before) / p.pieces;
+        p.piece = id - before - p.unit * p.pieces;
+        p.slot = slots + p.unit * p.pieces;
+        return true;
+    }
 };
 
-// A range of the tiles of all units a workgroup; units that end in another workgroup's range are joined by the last of theirs to arrive.
-// Eight wavefronts take a range's tiles in turn, every one from memory straight into operand registers: nothing is shared before the end.
+// A piece a workgroup; the pieces of a unit are joined by the last of them to arrive.  Eight wavefronts take a piece's tiles in turn, every one
+// from memory straight into operand registers: nothing but the queries is shared before the end.
 template <int R>
 __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(const AttnArgs A) {
     constexpr int RB = 16 * R, W = 8;
@@ -92,170 +162,150 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     __shared__ int lds_last;
     const KvqP8& P = A.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
-    const int wg = blockIdx.x, rows_per_token = A.gqa * A.maps;
+    const int rows_per_token = A.gqa * A.maps;
 
-    const auto blocks_of = [&](const Seq& q) { return q.rows * A.gqa > A.least_rows ? 0 : (q.rows * rows_per_token + RB - 1) / RB; };
-    const auto tiles_of = [&](const Seq& q) { return max(1, (q.tokens + 31) >> 5); };
-    const auto count = [&](int s) {
-        const Seq q = seq_of(P, s);
-        return blocks_of(q) * tiles_of(q) * P.n_kv;
+    // ---- which piece
+    const auto shape = [&](int at) {
+        const Seq q = seq_of(P, at);
+        const int blocks = q.rows * A.gqa > A.least_rows ? 0 : (q.rows * rows_per_token + RB - 1) / RB;
+        return Cuts::Shape{max(1, (q.tokens + 31) >> 5), blocks * P.n_kv};
     };
-    const Census<decltype(count)> census(count, P.n_seqs);
-    if (census.total == 0) return;
-    int longest;
-    {
-        int most = 0;
-        for (int k = 0; k < census.per; ++k) {
-            const int s = lane * census.per + k;
-            if (s < P.n_seqs) most = max(most, tiles_of(seq_of(P, s)));
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
-        longest = __builtin_amdgcn_readfirstlane(most);
+    Cuts::Shape* const shapes = reinterpret_cast<Cuts::Shape*>(lds_o);
+    if (P.n_seqs > 64) {
+        for (int at = threadIdx.x; at < P.n_seqs; at += 512) shapes[at] = shape(at);
+        __syncthreads();
     }
-    const int share = max(max(KVQ_P8_LEAST_SHARE, (census.total + (int)gridDim.x - 1) / (int)gridDim.x), (longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES);
-    int pos = wg * share;
-    if (pos >= census.total) return;
-    const int range_end = min(census.total, pos + share);
-    int first;
-    int s = __builtin_amdgcn_readfirstlane(census.find(pos, first));
-    first = __builtin_amdgcn_readfirstlane(first);
-    Seq seq = seq_of(P, s);
-    while (pos < range_end) {
-        // ---- the piece: tiles t0 .. t1 - 1 of a unit
-        int tiles = tiles_of(seq), blocks = blocks_of(seq);
-        while (pos - first >= tiles * blocks * P.n_kv) {
-            first += tiles * blocks * P.n_kv;
-            seq = seq_of(P, ++s);
-            tiles = tiles_of(seq);
-            blocks = blocks_of(seq);
-        }
-        const int unit = (pos - first) / tiles, t0 = pos - first - unit * tiles, t1 = min(tiles, t0 + range_end - pos);
-        const int kv = unit / blocks, block = unit - kv * blocks;
-
-        int limit[R];
-        int most = 0, least = 0x7fffffff;
+    Cuts cuts(shapes, P.n_seqs, P.n_seqs <= 64 && lane < P.n_seqs ? shape(lane) : Cuts::Shape{1, 0}, lane);
+    Piece pc;
+    if (!cuts.find(blockIdx.x, pc)) return;
+    const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
+    const Seq seq = seq_of(P, s);
+    const int blocks = (seq.rows * rows_per_token + RB - 1) / RB, kv = pc.unit / blocks, block = pc.unit - kv * blocks;
+    // (equal ranges: 33 tiles are 17 and 16, not 32 and 1)
+    const int t0 = (int)((int64_t)tiles * piece / pieces), t1 = (int)((int64_t)tiles * (piece + 1) / pieces);
+    int limit[R];
+    int most = 0, least = 0x7fffffff;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int f = block * RB + 16 * r + n, i = f / rows_per_token;
+        const bool real = i < seq.rows;
+        limit[r] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
+        most = max(most, real ? limit[r] : 0);
+        least = min(least, limit[r]);
+    }
+    if (wave < 4) {  // four channel groups of the rows, one a wavefront
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int f = block * RB + 16 * r + n, i = f / rows_per_token;
-            const bool real = i < seq.rows;
-            limit[r] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
-            most = max(most, real ? limit[r] : 0);
-            least = min(least, limit[r]);
-        }
-        if (wave < 4) {  // four channel groups of the rows, one a wavefront
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int f = block * RB + 16 * r + n, i = f / rows_per_token, rest = f - i * rows_per_token;
-                const int h = A.maps == 2 ? rest >> 1 : rest, map = A.maps == 2 ? rest & 1 : 0;
-                u32x4 w = {0, 0, 0, 0};
-                if (i < seq.rows && (A.maps == 1 || (wave >> 1) == map)) {
-                    w = *reinterpret_cast<const u32x4*>(A.q + (seq.row0 + i) * A.q_rs + (int64_t)(kv * A.gqa + h) * A.q_hs + 32 * wave + 8 * j);
-                    w ^= A.flip;
-                }
-                lds_q[r][wave][lane] = w;
+            const int f = block * RB + 16 * r + n, i = f / rows_per_token, rest = f - i * rows_per_token;
+            const int h = A.maps == 2 ? rest >> 1 : rest, map = A.maps == 2 ? rest & 1 : 0;
+            u32x4 w = {0, 0, 0, 0};
+            if (i < seq.rows && (A.maps == 1 || (wave >> 1) == map)) {
+                w = *reinterpret_cast<const u32x4*>(A.q + (seq.row0 + i) * A.q_rs + (int64_t)(kv * A.gqa + h) * A.q_hs + 32 * wave + 8 * j);
+                w ^= A.flip;
             }
+            lds_q[r][wave][lane] = w;
         }
-        __syncthreads();
+    }
+    __syncthreads();
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
-            most = max(most, __shfl_xor(most, d));
-            least = min(least, __shfl_xor(least, d));
-        }
-        most = __builtin_amdgcn_readfirstlane(most);
-        least = __builtin_amdgcn_readfirstlane(least);
-        const int end = min(t1, (most + 31) >> 5);
+    for (int d = 1; d < 16; d <<= 1) {
+        most = max(most, __shfl_xor(most, d));
+        least = min(least, __shfl_xor(least, d));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+    const int end = min(t1, (most + 31) >> 5);
 
-        State<R> st;
-        st.clear();
-        for (int from = t0 + wave; from < end; from += 64 * W) {
-            // the pages and scale words of the wavefront's next 64 tiles, one a lane
-            const int mine = from + lane * W;
-            const int page = mine < end ? page_of(P, s, mine >> (P.page_shift - 5)) : -1;
-            u32x2 words = {0, 0};
-            if (page >= 0) words = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)page * P.n_kv + kv) * 2);
-            const int todo = min(64, (end - from + W - 1) / W);
-            u32x4 kc[4], vc[4];
-            const auto at = [&](int k) {
-                const int pg = max(0, __builtin_amdgcn_readlane(page, k));
-                return tile_of(P, pg, kv, (from + k * W) & ((1 << (P.page_shift - 5)) - 1)) + lane * 16;
-            };
-            const auto load_k = [&](const uint8_t* p) {
+    State<R> st;
+    st.clear();
+    for (int from = t0 + wave; from < end; from += 64 * W) {
+        // the pages and scale words of the wavefront's next 64 tiles, one a lane
+        const int mine = from + lane * W;
+        const int page = mine < end ? page_of(P, s, mine >> (P.page_shift - 5)) : -1;
+        u32x2 words = {0, 0};
+        if (page >= 0) words = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)page * P.n_kv + kv) * 2);
+        const int todo = min(64, (end - from + W - 1) / W);
+        u32x4 kc[4], vc[4];
+        const auto at = [&](int k) {
+            const int pg = max(0, __builtin_amdgcn_readlane(page, k));
+            return tile_of(P, pg, kv, (from + k * W) & ((1 << (P.page_shift - 5)) - 1)) + lane * 16;
+        };
+        const auto load_k = [&](const uint8_t* p) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) kc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + c * 1024));
-            };
-            const auto load_v = [&](const uint8_t* p) {
+            for (int c = 0; c < 4; ++c) kc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + c * 1024));
+        };
+        const auto load_v = [&](const uint8_t* p) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) vc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4096 + c * 1024));
-            };
-            load_k(at(0));
-            load_v(at(0));
-            for (int k = 0; k < todo; ++k) {
-                const uint8_t* const next = at(min(k + 1, todo - 1));
-                const int kw = __builtin_amdgcn_readlane(words[0], k), vw = __builtin_amdgcn_readlane(words[1], k);
-                const bool there = __builtin_amdgcn_readlane(page, k) >= 0;
-                const int tok = (from + k * W) * 32;
-                float4v sc[R][1][2];
-                asm volatile("" ::: "memory");  // (queries would be kept in registers)
+            for (int c = 0; c < 4; ++c) vc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4096 + c * 1024));
+        };
+        load_k(at(0));
+        load_v(at(0));
+        for (int k = 0; k < todo; ++k) {
+            const uint8_t* const next = at(min(k + 1, todo - 1));
+            const int kw = __builtin_amdgcn_readlane(words[0], k), vw = __builtin_amdgcn_readlane(words[1], k);
+            const bool there = __builtin_amdgcn_readlane(page, k) >= 0;
+            const int tok = (from + k * W) * 32;
+            float4v sc[R][1][2];
+            asm volatile("" ::: "memory");  // (queries would be kept in registers)
 #pragma unroll
-                for (int sub = 0; sub < 2; ++sub) {
+            for (int sub = 0; sub < 2; ++sub) {
 #pragma unroll
-                    for (int r = 0; r < R; ++r) sc[r][0][sub] = float4v{0.f, 0.f, 0.f, 0.f};
+                for (int r = 0; r < R; ++r) sc[r][0][sub] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int grp = 0; grp < 4; ++grp) {
-                        const u32x4 w = kc[2 * sub + (grp >> 1)];
-                        const half8 a = widen(w[2 * (grp & 1)], w[2 * (grp & 1) + 1], 1.f);
+                for (int grp = 0; grp < 4; ++grp) {
+                    const u32x4 w = kc[2 * sub + (grp >> 1)];
+                    const half8 a = widen(w[2 * (grp & 1)], w[2 * (grp & 1) + 1], 1.f);
 #pragma unroll
-                        for (int r = 0; r < R; ++r) sc[r][0][sub] = mma(a, to_half8(lds_q[r][grp][lane]), sc[r][0][sub]);
+                    for (int r = 0; r < R; ++r) sc[r][0][sub] = mma(a, to_half8(lds_q[r][grp][lane]), sc[r][0][sub]);
+                }
+            }
+            load_k(next);
+            if (there) {
+                if (least < tok + 32) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const int over = limit[r] - tok - 8 * j;
+#pragma unroll
+                        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (4 * sub + i >= over) sc[r][0][sub][i] = -INFINITY;
                     }
                 }
-                load_k(next);
-                if (there) {
-                    if (least < tok + 32) {
+                uint32_t p[R][1][4];
+                const float factor = score_factor(A.scale_log2, kw);
+#pragma unroll
+                for (int r = 0; r < R; ++r) softmax_group<R, 1, false, true>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
+                const float vs = value_scale(vw);
+                const bool nan = (vw & KVQ_P8_NAN) != 0;
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) {
+                    uint32_t w[2] = {vc[nt >> 1][2 * (nt & 1)], vc[nt >> 1][2 * (nt & 1) + 1]};
+                    if (nan) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
-                            const int over = limit[r] - tok - 8 * j;
-#pragma unroll
-                            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    if (4 * sub + i >= over) sc[r][0][sub][i] = -INFINITY;
+                            uint32_t x[2] = {w[0], w[1]};
+                            st.o[r][nt] += nan_codes(x, tok + 8 * j, limit[r]);
+                            if (r == R - 1) w[0] = x[0], w[1] = x[1];
                         }
                     }
-                    uint32_t p[R][1][4];
-                    const float factor = score_factor(A.scale_log2, kw);
+                    const half8 a = widen(w[0], w[1], vs);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) softmax_group<R, 1, false, true>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
-                    const float vs = value_scale(vw);
-                    const bool nan = (vw & KVQ_P8_NAN) != 0;
-#pragma unroll
-                    for (int nt = 0; nt < 8; ++nt) {
-                        uint32_t w[2] = {vc[nt >> 1][2 * (nt & 1)], vc[nt >> 1][2 * (nt & 1) + 1]};
-                        if (nan) {
-#pragma unroll
-                            for (int r = 0; r < R; ++r) {
-                                uint32_t x[2] = {w[0], w[1]};
-                                st.o[r][nt] += nan_codes(x, tok + 8 * j, limit[r]);
-                                if (r == R - 1) w[0] = x[0], w[1] = x[1];
-                            }
-                        }
-                        const half8 a = widen(w[0], w[1], vs);
-#pragma unroll
-                        for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
-                    }
+                    for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][0]), st.o[r][nt]);
                 }
-                load_v(next);
             }
+            load_v(next);
         }
+    }
 
-        // ---- the wavefronts' states together, then the pieces of the unit, then the rows of the output
+    // ---- the wavefronts' states together, then the pieces of the unit, then the rows of the output
+    {
         // (the thread's index afresh: what follows from it would be kept in registers through the loop above)
         int fresh = threadIdx.x;
         asm volatile("" : "+v"(fresh));
         const int tid = fresh, lane = tid & 63, j = lane >> 4, n = lane & 15;
-        const int global0 = pos - t0, w0 = global0 / share, w1 = (global0 + tiles - 1) / share, pieces = w1 - w0 + 1;
         const int real_rows = min(RB, seq.rows * rows_per_token - block * RB);
-        const auto slot = [&](int piece) { return A.part + (int64_t)(2 * (w0 + piece) + (piece == 0 ? 1 : 0)) * (R * (KVQ_PART_BYTES / 4)); };
+        const auto slot = [&](int k) { return A.part + (int64_t)(pc.slot + k) * (R * (KVQ_PART_BYTES / 4)); };
         const int row = tid >> 5, chunk = tid & 31;
         float4v o[R];
         float m[R], l[R], fine[R];
@@ -283,7 +333,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
         }
         bool mine = true;
         if (pieces > 1) {
-            float* const to = slot(wg - w0);
+            float* const to = slot(piece);
             const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(to, 0, R * KVQ_PART_BYTES, 0x00020000);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -296,7 +346,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (tid == 0) {
-                uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
+                uint32_t* const counter = A.counters + (int64_t)pc.slot * KVQ_P8_COUNTER_STRIDE;
                 const uint32_t got = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 const bool last = got == (uint32_t)pieces - 1u;
                 if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -359,7 +409,6 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
                     A.lse[h * A.lse_hs + seq.row0 + i] = fine[r] == 0.f ? -INFINITY : (m[r] + __builtin_amdgcn_logf(fine[r])) * 0.69314718055994530942f;
             }
         }
-        pos += t1 - t0;
     }
 }
 
@@ -745,7 +794,7 @@ __global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     }
 }
 
-constexpr uint64_t kCounterBytes = (uint64_t)KVQ_P8_GROUPS * KVQ_P8_COUNTER_STRIDE * 4;
+constexpr uint64_t kCounterBytes = 2ull * KVQ_P8_GROUPS * KVQ_P8_COUNTER_STRIDE * 4;
 
 bool heads_ok(int32_t n_q, int32_t n_kv) { return n_q >= 1 && n_q % n_kv == 0 && n_q / n_kv <= KVQ_MAX_GQA; }
 
@@ -762,11 +811,12 @@ bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
     const int64_t tiles = (int64_t)P.table_pages << (P.page_shift - 5), heads = (int64_t)P.n_seqs * P.n_kv;
     // blocks of 16 rows bound both: every number on either line stays below 2^30
     if (heads && (most * maps + 15) / 16 * (tiles + 8 + P.max_rows / 32) > (1 << 30) / heads) return false;
-    const int64_t total = (rows + 16 * plan.r - 1) / (16 * plan.r) * tiles * heads;
-    plan.groups = std::min<int64_t>(KVQ_P8_GROUPS, (total + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
+    // as many workgroups as pieces there can be, and partial results of those of units that are cut
+    const int64_t units = (rows + 16 * plan.r - 1) / (16 * plan.r) * heads, cuts = units * ((tiles + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
+    plan.groups = std::min(cuts, 2 * units > KVQ_P8_GROUPS ? KVQ_P8_GROUPS + units : KVQ_P8_GROUPS);
     const int64_t line = ((most + 63) / 64) * (tiles + 8 + P.max_rows / 32) * heads;
     plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
-    plan.bytes = kCounterBytes + 2 * (uint64_t)KVQ_PART_BYTES * std::max<uint64_t>(plan.groups * plan.r, plan.chunk * 4 * (maps == 1 ? 2 : 4));
+    plan.bytes = kCounterBytes + 2 * (uint64_t)KVQ_PART_BYTES * std::max<uint64_t>(std::min<int64_t>(cuts, KVQ_P8_GROUPS) * plan.r, plan.chunk * 4 * (maps == 1 ? 2 : 4));
     return true;
 }
 
