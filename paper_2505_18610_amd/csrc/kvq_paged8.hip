@@ -42,6 +42,7 @@ __device__ inline bool touched_page(const KvqP8& P, int per_seq, int id, Touched
     int number;
     if (per_seq) {
         T.s = id / per_seq;
+        if (T.s >= P.n_seqs) return false;
         number = id - T.s * per_seq;
     } else {
         const auto count = [&](int s) { return pages(seq_of(P, s)); };
@@ -87,10 +88,34 @@ __device__ inline uint32_t byte_mask(uint32_t bits) {
     return ((bits & 1u) | (bits & 2u) << 7 | (bits & 4u) << 14 | (bits & 8u) << 21) * 0xffu;
 }
 
+// Between rows and tiles codes pass through LDS, a tile of a wavefront's own.  A lane (j, m) of the row side has channels 8 m .. 8 m + 7 of tokens
+// 8 j .. 8 j + 7, and reads or writes eight bytes at a time: keys of one token, values of one channel.  Chunks lie a little turned, so that
+// the 64 lanes of such an access meet every bank as often (as in memory 16 lanes met one).
+template <bool KEYS>
+__device__ inline int chunk_in_lds(int c, int j, int n) {
+    return (c * 64 + 16 * j + (KEYS ? (n & 12) | ((n + j) & 3) : (n & 8) | ((n + j + 4 * c) & 7))) * 16;
+}
+template <bool KEYS>
+__device__ inline int eight_in_lds(int j, int m, int i) {  // KEYS: token 8 j + i; else channel 8 m + i
+    if (KEYS) return chunk_in_lds<true>((i >> 2) * 2 + (m >> 3), m & 3, 4 * j + (i & 3)) + ((m >> 2) & 1) * 8;
+    return chunk_in_lds<false>(m >> 2, j, 8 * (m & 1) + i) + ((m >> 1) & 1) * 8;
+}
+// (written and read by one wavefront, whose LDS accesses stay in order)
+__device__ inline void lds_written() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+// The value of lane m ^ 8, or of lane m ^ 4, of the 16 lanes of a row.
+__device__ inline float partner(float x, int m, bool eight) {
+    const int v = __float_as_int(x);
+    const int by8 = __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);                                                          // row_ror:8
+    const int up = __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, true), down = __builtin_amdgcn_mov_dpp(v, 0x12c, 0xf, 0xf, true);  // row_ror:4, 12
+    return __int_as_float(eight ? by8 : m & 4 ? up : down);
+}
+
 // One page's keys or values of one head a workgroup, a tile a wavefront, in three steps: load (and rotate) the new tokens and take the
 // largest magnitude, over all wavefronts; settle the scale; round and store.  The new values stay in registers in between.
-// Keys are loaded where the tile's layout wants them, 64 bytes of a row by four lanes; values as whole rows by 16 lanes, eight tokens
-// a lane, which makes the four codes of a word four tokens of one channel; they pass through LDS into the layout's order.
+// Rows are loaded whole, by 16 lanes; the channel that one is rotated with is 8 or 4 lanes on.
 template <bool KEYS>
 __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv, uint8_t* lds, float* wave_max) {
     const KvqP8& P = A.p;
@@ -100,64 +125,51 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
     int32_t* const word = P.words + ((int64_t)T.page * P.n_kv + kv) * 2 + (KEYS ? 0 : 1);
     const int old_word = T.begin > 0 ? *word : 0;
     uint8_t* const tile = tile_of(P, T.page, kv, wave) + (KEYS ? 0 : KVQ_P8_TILE_BYTES / 2);
-    const int64_t row = (int64_t)T.row0 + ((T.at << P.page_shift) - T.first);  // the row that the page's first token would be
+    const int64_t row = (int64_t)T.row0 + ((T.at << P.page_shift) - T.first) + tok0 + 8 * j;  // of the lane's first token
+    const auto is_new = [&](int t) { return tok0 + t >= T.begin && tok0 + t < T.end; };       // t: token of the tile
 
-    // slots: KEYS: x[4 sub + grp][i], token 8 (n / 4) + 4 sub + n % 4, channel 32 grp + 8 j + i; else x[i][e], token 8 j + i, channel 8 n + e
-    float x[8][8];
+    float x[8][8];  // token 8 j + i, channel 8 n + e
     float largest = 0.f;
     bool nan = false;
-    const auto slot_token = [&](int a) { return tok0 + (KEYS ? 8 * (n >> 2) + 4 * (a >> 2) + (n & 3) : 8 * j + a); };
-    const auto is_new = [&](int a) { const int t = slot_token(a); return t >= T.begin && t < T.end; };
     if (any_new) {
+        half8 w[8];
+        const _Float16* const src = KEYS ? A.k + row * A.k_ts + kv * A.k_hs + 8 * n : A.v + row * A.v_ts + kv * A.v_hs + 8 * n;
+        const int64_t step = KEYS ? A.k_ts : A.v_ts;
 #pragma unroll
-        for (int a = 0; a < 8; ++a) {
-            half8 w = {};
-            if (is_new(a)) {
-                const int64_t r = row + slot_token(a);
-                w = KEYS ? *reinterpret_cast<const half8*>(A.k + r * A.k_ts + kv * A.k_hs + 32 * (a & 3) + 8 * j)
-                         : *reinterpret_cast<const half8*>(A.v + r * A.v_ts + kv * A.v_hs + 8 * n);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[a][e] = (float)w[e];
+        for (int i = 0; i < 8; ++i) {
+            w[i] = half8{};
+            if (is_new(8 * j + i)) w[i] = __builtin_nontemporal_load(reinterpret_cast<const half8*>(src + i * step));
         }
-        if (KEYS && A.pair) {
-            // a pair's channels are 64 or 32 apart: groups of 32 channels of one lane
-            const int step = A.pair >> 5;  // groups between them
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                if (!is_new(4 * sub)) continue;
-                const float* const angles = A.angles + (row + slot_token(4 * sub)) * (2 * A.pair);
+        for (int i = 0; i < 8; ++i) {
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {  // the pair's number among the lane's
-                    const float* const at = angles + (step == 2 ? 32 * g : 0) + 8 * j;
-                    float c[8], s[8];
+            for (int e = 0; e < 8; ++e) x[i][e] = (float)w[i][e];
+            if (KEYS && A.pair) {
+                float c[8] = {}, s[8] = {};
+                if (is_new(8 * j + i)) {
+                    const float* const at = A.angles + (row + i) * (2 * A.pair) + ((8 * n) & (A.pair - 1));
 #pragma unroll
                     for (int e = 0; e < 8; e += 4) {
                         const float4v cc = *reinterpret_cast<const float4v*>(at + e), ss = *reinterpret_cast<const float4v*>(at + A.pair + e);
 #pragma unroll
                         for (int d = 0; d < 4; ++d) c[e + d] = cc[d], s[e + d] = ss[d];
                     }
+                }
+                const bool eight = A.pair == 64, upper = n & (eight ? 8 : 4);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float a = step == 2 ? x[4 * sub + g][e] : x[4 * sub + 2 * g][e];
-                        const float b = step == 2 ? x[4 * sub + g + 2][e] : x[4 * sub + 2 * g + 1][e];
-                        // (each product and the sum rounded by itself, as elsewhere in the library)
-                        const float lo = __fsub_rn(__fmul_rn(a, c[e]), __fmul_rn(b, s[e]));
-                        const float hi = __fadd_rn(__fmul_rn(a, s[e]), __fmul_rn(b, c[e]));
-                        if (step == 2) x[4 * sub + g][e] = lo, x[4 * sub + g + 2][e] = hi;
-                        else x[4 * sub + 2 * g][e] = lo, x[4 * sub + 2 * g + 1][e] = hi;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    // (each product and the sum rounded by itself, as elsewhere in the library)
+                    const float other = __fmul_rn(partner(x[i][e], n, eight), s[e]), own = __fmul_rn(x[i][e], c[e]);
+                    x[i][e] = upper ? __fadd_rn(other, own) : __fsub_rn(own, other);
                 }
             }
-        }
-#pragma unroll
-        for (int a = 0; a < 8; ++a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[a][e] = finite_or_nan(x[a][e]);
-                largest = fmaxf(largest, fabsf(x[a][e]));  // (passes over NaN)
-                nan = nan || x[a][e] != x[a][e];
+                x[i][e] = finite_or_nan(x[i][e]);
+                largest = fmaxf(largest, fabsf(x[i][e]));  // (passes over NaN)
+                nan = nan || x[i][e] != x[i][e];
             }
+        }
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
@@ -189,28 +201,17 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
     }
     u32x4 fresh[4] = {};
     if (any_new) {
-        if (KEYS) {
+        uint8_t* const at = lds + wave * 4096;
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const float* const y = &x[2 * c + (d >> 1)][4 * (d & 1)];
-                    fresh[c][d] = code4(y[0], y[1], y[2], y[3]);
-                }
-        } else {
-            uint8_t* const at = lds + wave * 4096;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {  // channel 8 n + c: its eight tokens
-                const int ch = 8 * n + c;
-                const u32x2 w = {code4(x[0][c], x[1][c], x[2][c], x[3][c]), code4(x[4][c], x[5][c], x[6][c], x[7][c])};
-                *reinterpret_cast<u32x2*>(at + ((ch >> 5) * 64 + 16 * j + (ch & 15)) * 16 + ((ch >> 4) & 1) * 8) = w;
-            }
-            // (written and read by one wavefront, whose LDS accesses stay in order)
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) fresh[c] = *reinterpret_cast<const u32x4*>(at + (c * 64 + lane) * 16);
+        for (int k = 0; k < 8; ++k) {  // KEYS: token 8 j + k; else channel 8 n + k
+            u32x2 w;
+            if (KEYS) w = u32x2{code4(x[k][0], x[k][1], x[k][2], x[k][3]), code4(x[k][4], x[k][5], x[k][6], x[k][7])};
+            else w = u32x2{code4(x[0][k], x[1][k], x[2][k], x[3][k]), code4(x[4][k], x[5][k], x[6][k], x[7][k])};
+            *reinterpret_cast<u32x2*>(at + eight_in_lds<KEYS>(j, n, k)) = w;
         }
+        lds_written();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) fresh[c] = *reinterpret_cast<const u32x4*>(at + chunk_in_lds<KEYS>(c, j, n));
     }
     // A tile that held no token is written whole: slots that hold none are zero.
 #pragma unroll
@@ -218,15 +219,14 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
         u32x4 w = fresh[c];
         if (any_old) {
             if (KEYS) {
-                const bool take = is_new(4 * (c >> 1));
-                if (!take) {
+                if (!is_new(8 * (n >> 2) + 4 * (c >> 1) + (n & 3))) {
                     if (!lowered) continue;
                     w = held[c];
                 }
             } else {
                 uint32_t bits = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) bits |= (is_new(i) ? 1u : 0u) << i;
+                for (int i = 0; i < 8; ++i) bits |= (is_new(8 * j + i) ? 1u : 0u) << i;
                 const u32x4 mask = {byte_mask(bits), byte_mask(bits >> 4), byte_mask(bits), byte_mask(bits >> 4)};
                 w = (fresh[c] & mask) | (held[c] & ~mask);
                 if (bits == 0 && !lowered) continue;
@@ -236,24 +236,33 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
     }
 }
 
+// What a workgroup works on: the heads and kinds of eight pages in turn, so that those of one page, which read the same angles, are on one XCD.
+struct Job {
+    int page, kv, kind;
+};
+__device__ inline Job job_of(int n_kv) {
+    const int of_page = blockIdx.x >> 3, page8 = of_page / (2 * n_kv), at = of_page - page8 * 2 * n_kv;
+    return Job{page8 * 8 + ((int)blockIdx.x & 7), at >> 1, at & 1};
+}
+
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void kvq_paged8_append_kernel(const AppendArgs A) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES * 4096];
     __shared__ float wave_max[WAVES];
     Touched T;
-    const int kind = blockIdx.x & 1, at = blockIdx.x >> 1, kv = at % A.p.n_kv;
-    if (!touched_page(A.p, A.per_seq, at / A.p.n_kv, T)) return;
-    if (kind == 0) append_page<true>(A, T, kv, lds, wave_max);
-    else append_page<false>(A, T, kv, lds, wave_max);
+    const Job job = job_of(A.p.n_kv);
+    if (!touched_page(A.p, A.per_seq, job.page, T)) return;
+    if (job.kind == 0) append_page<true>(A, T, job.kv, lds, wave_max);
+    else append_page<false>(A, T, job.kv, lds, wave_max);
 }
 
-// Cached tokens as values, a tile of keys or values a wavefront.
+// Cached tokens as values, a tile of keys or values a wavefront; rows are stored whole, by 16 lanes.
 template <bool FP32>
 __device__ inline void store_values(void* to, int64_t at, const float (&x)[8]) {
     if (FP32) {
         float* const f = static_cast<float*>(to) + at;
-        *reinterpret_cast<float4v*>(f) = float4v{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<float4v*>(f + 4) = float4v{x[4], x[5], x[6], x[7]};
+        __builtin_nontemporal_store(float4v{x[0], x[1], x[2], x[3]}, reinterpret_cast<float4v*>(f));
+        __builtin_nontemporal_store(float4v{x[4], x[5], x[6], x[7]}, reinterpret_cast<float4v*>(f + 4));
     } else {
         half8 h;
 #pragma unroll
@@ -262,56 +271,50 @@ __device__ inline void store_values(void* to, int64_t at, const float (&x)[8]) {
             const float y = fabsf(x[e]) > 65504.f ? copysignf(65504.f, x[e]) : x[e];
             h[e] = (_Float16)y;
         }
-        *reinterpret_cast<half8*>(static_cast<_Float16*>(to) + at) = h;
+        __builtin_nontemporal_store(h, reinterpret_cast<half8*>(static_cast<_Float16*>(to) + at));
     }
 }
 __device__ inline float byte_value(uint32_t w, int byte) {
     return byte == 0 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 0) : byte == 1 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 1)
          : byte == 2 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 2) : __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
 }
-template <bool FP32, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void kvq_paged8_read_kernel(const ReadArgs A) {
+template <bool FP32, bool KEYS>
+__device__ inline void read_page(const ReadArgs& A, const Touched& T, int kv, uint8_t* lds) {
     const KvqP8& P = A.p;
-    Touched T;
-    const int kind = blockIdx.x & 1, at = blockIdx.x >> 1, kv = at % P.n_kv;
-    if (!touched_page(P, A.per_seq, at / P.n_kv, T)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
     const int tok0 = wave * 32;
     if (tok0 >= T.end || tok0 + 32 <= T.begin) return;
-    const uint8_t* const tile = tile_of(P, T.page, kv, wave) + kind * (KVQ_P8_TILE_BYTES / 2);
-    const float scale = ldexpf(1.f, exponent_of(P.words[((int64_t)T.page * P.n_kv + kv) * 2 + kind]));
-    const int64_t row = (int64_t)T.row0 + ((T.at << P.page_shift) - T.first);
-    if (kind == 0) {
+    const uint8_t* const tile = tile_of(P, T.page, kv, wave) + (KEYS ? 0 : KVQ_P8_TILE_BYTES / 2);
+    uint8_t* const in = lds + wave * 4096;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(tile + (c * 64 + lane) * 16);
-            const int t = tok0 + 8 * (n >> 2) + 4 * (c >> 1) + (n & 3);
-            if (t < T.begin || t >= T.end) continue;
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<u32x4*>(in + chunk_in_lds<KEYS>(c, j, n)) = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tile + (c * 64 + lane) * 16));
+    const float scale = ldexpf(1.f, exponent_of(P.words[((int64_t)T.page * P.n_kv + kv) * 2 + (KEYS ? 0 : 1)]));
+    lds_written();
+    u32x2 w[8];  // KEYS: token 8 j + k; else channel 8 n + k
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[8];
+    for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x2*>(in + eight_in_lds<KEYS>(j, n, k));
+    const int64_t row = (int64_t)T.row0 + ((T.at << P.page_shift) - T.first) + tok0 + 8 * j;
+    void* const to = KEYS ? A.k : A.v;
+    const int64_t step = KEYS ? A.k_ts : A.v_ts, at = row * step + kv * (KEYS ? A.k_hs : A.v_hs) + 8 * n;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = byte_value(w[2 * h + (e >> 2)], e & 3) * scale;
-                store_values<FP32>(A.k, (row + t) * A.k_ts + kv * A.k_hs + 64 * (c & 1) + 32 * h + 8 * j, x);
-            }
-        }
-    } else {
-        u32x2 w[8];  // channel 8 n + e: eight tokens
+    for (int i = 0; i < 8; ++i) {
+        const int t = tok0 + 8 * j + i;
+        if (t < T.begin || t >= T.end) continue;
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int ch = 8 * n + e;
-            w[e] = *reinterpret_cast<const u32x2*>(tile + ((ch >> 5) * 64 + 16 * j + (ch & 15)) * 16 + ((ch >> 4) & 1) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = tok0 + 8 * j + i;
-            if (t < T.begin || t >= T.end) continue;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = byte_value(w[e][i >> 2], i & 3) * scale;
-            store_values<FP32>(A.v, (row + t) * A.v_ts + kv * A.v_hs + 8 * n, x);
-        }
+        for (int e = 0; e < 8; ++e) x[e] = (KEYS ? byte_value(w[i][e >> 2], e & 3) : byte_value(w[e][i >> 2], i & 3)) * scale;
+        store_values<FP32>(to, at + i * step, x);
     }
+}
+template <bool FP32, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void kvq_paged8_read_kernel(const ReadArgs A) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES * 4096];
+    Touched T;
+    const Job job = job_of(A.p.n_kv);
+    if (!touched_page(A.p, A.per_seq, job.page, T)) return;
+    if (job.kind == 0) read_page<FP32, true>(A, T, job.kv, lds);
+    else read_page<FP32, false>(A, T, job.kv, lds);
 }
 
 // Workgroups that a call over the pages that rows touch needs, and pages of a sequence to count with (0: workgroups find theirs): straight
@@ -325,7 +328,7 @@ int64_t touched_pages(const KvqP8& P, int32_t& per_seq) {
 
 template <class Args, class Kernel>
 kvq_status_t launch(Kernel const (&kernels)[4], Args& A, hipStream_t stream) {
-    const int64_t groups = touched_pages(A.p, A.per_seq) * A.p.n_kv * 2;
+    const int64_t groups = ((touched_pages(A.p, A.per_seq) + 7) & ~7ll) * A.p.n_kv * 2;
     if (groups > INT32_MAX / (32 << (A.p.page_shift - 4))) return KVQ_E_INVALID;  // threads of a launch stay below 2^32
     const int waves = 1 << (A.p.page_shift - 5);
     hipLaunchKernelGGL(kernels[A.p.page_shift - 5], dim3((unsigned)groups), dim3(64 * waves), 0, stream, A);

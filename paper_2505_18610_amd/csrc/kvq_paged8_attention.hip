@@ -672,10 +672,15 @@ __global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                     uint32_t p[R][TT][4];
 #pragma unroll
                     for (int r = 0; r < R; ++r) softmax_tiles<R, TT>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
+                    int flagged = 0;
 #pragma unroll
-                    for (int x = 0; x < TT; ++x) {
-                        if ((now[x0 + x].vw & KVQ_P8_NAN) && now[x0 + x].page >= 0) {
-                            const uint8_t* const at = tile_of(P, now[x0 + x].page, kv, (t + x0 + x) & ((1 << per_page) - 1)) + 4096 + lane * 16;
+                    for (int x = 0; x < TT; ++x) flagged |= now[x0 + x].page >= 0 ? now[x0 + x].vw : 0;
+                    if (flagged & KVQ_P8_NAN) {  // (one branch in front of all products)
+#pragma unroll 1
+                        for (int x = 0; x < TT; ++x) {
+                            const Tile& at_x = x ? now[x0 + TT - 1] : now[x0];
+                            if (!(at_x.vw & KVQ_P8_NAN) || at_x.page < 0) continue;
+                            const uint8_t* const at = tile_of(P, at_x.page, kv, (t + x0 + x) & ((1 << per_page) - 1)) + 4096 + lane * 16;
 #pragma unroll
                             for (int nt = 0; nt < 8; ++nt) {
                                 const u32x2 w = *reinterpret_cast<const u32x2*>(at + (nt >> 1) * 1024 + (nt & 1) * 8);
@@ -686,13 +691,15 @@ __global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                                 }
                             }
                         }
+                    }
+#pragma unroll
+                    for (int x = 0; x < TT; ++x)
 #pragma unroll
                         for (int nt = 0; nt < 8; ++nt) {
                             const half8 a = to_half8(*reinterpret_cast<const u32x4*>(vt + x * TILE + nt * 1024));
 #pragma unroll
                             for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
                         }
-                    }
                 }
             }
             if (more) store(buf ^ 1);
