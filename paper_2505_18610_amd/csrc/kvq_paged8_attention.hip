@@ -22,10 +22,12 @@ using kvq_flash::reference_of;
 using kvq_flash::softmax_group;
 using kvq_flash::to_half8;
 
-#define KVQ_P8_GROUPS 512       // workgroups of a launch over ranges of tiles, at most
+#define KVQ_P8_GROUPS 512       // pieces of few units that a launch is cut into, at most
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
 #define KVQ_P8_LEAST_SHARE 8    // tiles of a workgroup, at least
 #define KVQ_P8_LEAST_CHUNK 16   // of a workgroup with a chunk
+#define KVQ_P8_CHUNK_GROUPS 256 // workgroups of a launch over chunks, at most: one a compute unit
+#define KVQ_P8_MAP_BYTES 17408  // partial results of a wavefront with a chunk and one map
 #define KVQ_P8_MOST_PIECES 128  // of a unit
 
 struct AttnArgs {
@@ -43,6 +45,11 @@ struct AttnArgs {
     uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
 };
 
+// A value that the compiler takes for a new one: what follows from it is worked out where it is used, not kept in registers through a loop.
+__device__ inline int opaque(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 // A lane's eight codes of one operand, widened: exact but for values below 2^-21, which keep the 2^-25 that fp16 has there.
 __device__ inline half8 widen(uint32_t lo, uint32_t hi, float scale) {
     const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
@@ -301,9 +308,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     // ---- the wavefronts' states together, then the pieces of the unit, then the rows of the output
     {
         // (the thread's index afresh: what follows from it would be kept in registers through the loop above)
-        int fresh = threadIdx.x;
-        asm volatile("" : "+v"(fresh));
-        const int tid = fresh, lane = tid & 63, j = lane >> 4, n = lane & 15;
+        const int tid = opaque(threadIdx.x), lane = tid & 63, j = lane >> 4, n = lane & 15;
         const int real_rows = min(RB, seq.rows * rows_per_token - block * RB);
         const auto slot = [&](int k) { return A.part + (int64_t)(pc.slot + k) * (R * (KVQ_PART_BYTES / 4)); };
         const int row = tid >> 5, chunk = tid & 31;
@@ -414,83 +419,113 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 
 // ---- Sequences with many rows: chunks of prompts
 
-// Probabilities of TT tiles for row group r as kvq_flash.h's softmax_group, the tiles with a factor each.
-template <int R, int TT>
-__device__ inline void softmax_tiles(State<R>& st, int r, const float4v (&s)[TT][2], const float (&factor)[TT], bool fine, uint32_t (&p)[TT][4]) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        float most = -INFINITY;
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, s[t][sub][i]);
-        top = fmaxf(top, most * factor[t]);
-    }
-    if (__any(top > st.m[r] + (KVQ_BELOW + KVQ_FOLLOW))) {
-        const float m_new = fmaxf(st.m[r], kvq_flash::quarters_max(top) - KVQ_BELOW);
-        const float alpha = __builtin_amdgcn_exp2f(st.m[r] - reference_of(m_new));
-        st.l[r] *= alpha;
-        st.fine[r] *= alpha;
-#pragma unroll
-        for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= alpha;
-        st.m[r] = m_new;
-    }
-    const float ref = reference_of(st.m[r]);
-    const half2v ones = {(_Float16)1.f, (_Float16)1.f};
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        float e[2][4];
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[sub][i] = __builtin_amdgcn_exp2f(fmaf(s[t][sub][i], factor[t], -ref));
-        if (fine) {
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.fine[r] += e[sub][i];
-        }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            p[t][v] = kvq_flash::pack2(e[v >> 1][2 * (v & 1)], e[v >> 1][2 * (v & 1) + 1]);
-            const uint32_t two = p[t][v];
-            st.l[r] = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), ones, st.l[r], false);
-        }
-    }
-}
-
 // Where the work of the units lies on one line that workgroups take equal shares of.  A block's length on it is its tiles, by the tokens that its last
 // row sees, and kLead for what a block costs beside them; blocks of a KV head lie one after the other, KV heads, sequences.
 struct Line {
-    int rows, seen0, per_token, blocks;  // flat rows, tokens that the rows of the first token see, flat rows of a token, blocks
-    int length;                          // of all blocks of one KV head
-    static constexpr int kLead = 4;
-    template <int RB>
-    __device__ int at(int b) const {  // where block b begins
-        return (int)(((int64_t)b * seen0 + (int64_t)b * (b + 1) / 2 * RB / per_token) >> 5) + kLead * b;
-    }
+    int rows, blocks;     // flat rows, blocks
+    int length;           // of all blocks of one KV head
+    double seen, growth;  // tiles that the rows of the first token see; half of those that a block adds to what the next one sees
+    static constexpr int kLead = 12;
+    // where block b begins (in 64-bit floating point, the same in every workgroup, where whole numbers would take a division that is a loop)
+    __device__ static int place(int b, double seen, double growth) { return (int)__builtin_fma((double)b * (b + 1), growth, b * seen) + kLead * b; }
+    __device__ int at(int b) const { return __builtin_amdgcn_readfirstlane(place(b, seen, growth)); }
 };
 template <int RB>
 __device__ inline Line line_of(const Seq& q, int per_token, int least_rows) {
     Line x;
     x.rows = q.rows * per_token;
-    x.seen0 = max(0, q.tokens - q.rows);
-    x.per_token = per_token;
+    x.seen = max(0, q.tokens - q.rows) * (1. / 32);
+    x.growth = RB / 64. / per_token;
     x.blocks = x.rows > least_rows ? (x.rows + RB - 1) / RB : 0;
-    x.length = x.blocks ? x.at<RB>(x.blocks) : 0;
+    x.length = Line::place(x.blocks, x.seen, x.growth);
     return x;
 }
 
-// RG groups of 16 rows a wavefront, MAPS states of each; four wavefronts with rows of their own share the tiles: two an iteration, widened to fp16 once on
-// their way into LDS, where the next ones are put while these are computed on.
-template <int RG, int MAPS, int TT>
-__global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
-    constexpr int R = RG * MAPS, RB = 64 * RG, NT = 2, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+typedef float float16v __attribute__((ext_vector_type(16)));
+#ifdef KVQ_NO_ARITHMETIC
+__device__ inline float16v mma32(half8, half8, float16v c) { return c; }
+#else
+__device__ inline float16v mma32(half8 a, half8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+#endif
+// over the two halves of a wavefront, in every lane
+__device__ inline float halves_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ inline float halves_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// One softmax map of 32 rows of a wavefront, as kvq_flash.h's State but by v_mfma_f32_32x32x16_f16: lane = 32 h + n has row n.
+struct Map {
+    float16v o[4];  // o[cb][i]: channel 32 cb + 8 (i / 4) + 4 h + i % 4
+    float m;        // the reference (log2 units), equal in both halves
+    float l, fine;  // this half's shares of the sums
+    __device__ void clear() {
+        m = -INFINITY;
+        l = fine = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
+    }
+    __device__ void scale(float by) {
+        l *= by;
+        fine *= by;
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) o[cb] *= by;
+    }
+};
+// Probabilities of NT tiles from raw scores (masked ones at -inf), the tiles with a factor each; reference and sums as in kvq_flash.h.
+// s[x][i]: token 16 (i / 8) + 8 h + i % 8 of tile x, and p in that order.
+template <int NT>
+__device__ inline void softmax_tiles(Map& st, const float16v (&s)[NT], const float (&factor)[NT], bool fine, uint32_t (&p)[NT][8]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+        float most = s[x][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, s[x][i]);
+        top = fmaxf(top, most * factor[x]);
+    }
+    if (__any(top > st.m + (KVQ_BELOW + KVQ_FOLLOW))) {
+        const float m_new = fmaxf(st.m, halves_max(top) - KVQ_BELOW);
+        st.scale(__builtin_amdgcn_exp2f(st.m - reference_of(m_new)));
+        st.m = m_new;
+    }
+    const float ref = reference_of(st.m);
+    const half2v ones = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+        float e[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[x][i], factor[x], -ref));
+        if (fine) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.fine += e[i];
+        }
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            p[x][v] = kvq_flash::pack2(e[2 * v], e[2 * v + 1]);
+            const uint32_t two = p[x][v];
+            st.l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), ones, st.l, false);
+        }
+    }
+}
+
+// A block of 256 rows, 32 a wavefront, MAPS softmax maps of each, against the tiles of a piece of its unit.  Two groups of four wavefronts, one of
+// either on a SIMD, take turns: while one has its products (scores of a stage of NT tiles, and the probabilities of the stage before times its values),
+// the other has its softmax, widens the codes of a stage two further on into LDS and loads the next.  A barrier stands between the turns.  A stage is
+// written in the turns 2 s - 3 and 2 s - 2, its keys are read in 2 s and 2 s + 1, its values in 2 s + 2 and 2 s + 3: four buffers.
+template <int MAPS>
+__global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
+    constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * STAGE];
+    __shared__ u32x4 lds_q[MAPS == 2 ? 8 : 1][4][64];  // two maps: the second's queries, for which there are no registers
     __shared__ int lds_last;
     const KvqP8& P = A.p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_page = P.page_shift - 5;
 
     const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.least_rows); };
@@ -506,295 +541,420 @@ __global__ __launch_bounds__(256, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     int first;
     int s = __builtin_amdgcn_readfirstlane(census.find(pos, first));
     first = __builtin_amdgcn_readfirstlane(first);
-    Seq seq = seq_of(P, s);
-    Line ln = line(seq);
     while (pos < range_end) {
-        while (pos - first >= ln.length * P.n_kv) {
-            first += ln.length * P.n_kv;
+        Seq seq = seq_of(P, s);
+        Line ln = line(seq);
+        for (;;) {
+            const int all = __builtin_amdgcn_readfirstlane(ln.length) * P.n_kv;
+            if (pos - first < all) break;
+            first += all;
             seq = seq_of(P, ++s);
             ln = line(seq);
         }
-        const int kv = (pos - first) / ln.length, in_head = pos - first - kv * ln.length;
+        int gqa = A.gqa;
+        asm volatile("" : "+s"(gqa));  // (as opaque(): its reciprocal would be kept in registers throughout)
+        const int flat = seq.rows * gqa;
+        const int head_length = __builtin_amdgcn_readfirstlane(ln.length), kv = (pos - first) / head_length, in_head = pos - first - kv * head_length;
         int block = 0;
         for (int step = 1 << 26; step; step >>= 1)
-            if (block + step < ln.blocks && ln.at<RB>(block + step) <= in_head) block += step;
-        const int unit = pos - in_head + ln.at<RB>(block), length = ln.at<RB>(block + 1) - ln.at<RB>(block);  // the unit's place on the line
+            if (block + step < ln.blocks && ln.at(block + step) <= in_head) block += step;
+        const int unit = pos - in_head + ln.at(block), length = ln.at(block + 1) - ln.at(block);  // the unit's place on the line
         const int unit_end = min(range_end, unit + length);
 
-        int limit[RG];
-        half8 q[RG][4];
-        int most = 0, least = 0x7fffffff;
+        // the lane's row
+        struct Row { int i, head; bool real; };
+        const auto row_of = [&](int at) {
+            const int f = block * RB + wave * 32 + at, i = f / gqa;
+            return Row{i, kv * gqa + f - i * gqa, f < flat};
+        };
+        int limit;
+        half8 q[KB];
+        int most, least;
+        {
+            const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
+            const Row row = row_of(n);
+            limit = least = row.real ? max(0, seq.tokens - seq.rows + row.i + 1) : seq.tokens;
+            most = row.real ? limit : 0;
+            const _Float16* const src = A.q + (seq.row0 + (row.real ? row.i : 0)) * A.q_rs + (int64_t)(row.real ? row.head : kv * gqa) * A.q_hs + 8 * h;
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            const int f = block * RB + wave * 16 * RG + 16 * g + n, i = f / A.gqa, h = f - i * A.gqa;
-            const bool real = f < ln.rows;
-            limit[g] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
-            most = max(most, real ? limit[g] : 0);
-            least = min(least, limit[g]);
-            const _Float16* const src = A.q + (seq.row0 + (real ? i : 0)) * A.q_rs + (int64_t)(kv * A.gqa + (real ? h : 0)) * A.q_hs + 8 * j;
-#pragma unroll
-            for (int grp = 0; grp < 4; ++grp) {
-                u32x4 w = *reinterpret_cast<const u32x4*>(src + 32 * grp);
+            for (int kb = 0; kb < 8; ++kb) {
+                u32x4 w = *reinterpret_cast<const u32x4*>(src + 16 * kb);
                 w ^= A.flip;
-                if (!real) w = u32x4{0, 0, 0, 0};
-                q[g][grp] = to_half8(w);
+                if (!row.real) w = u32x4{0, 0, 0, 0};
+                if (kb < KB) q[kb] = to_half8(w);
+                else lds_q[wave][kb & 3][lane] = w;
             }
         }
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
+        for (int d = 1; d < 32; d <<= 1) {
             most = max(most, __shfl_xor(most, d));
             least = min(least, __shfl_xor(least, d));
         }
         most = __builtin_amdgcn_readfirstlane(most);
         least = __builtin_amdgcn_readfirstlane(least);
         // the block's tiles: those that its last row sees
-        const int last_row = min(ln.rows, (block + 1) * RB) - 1;
-        const int tiles = (max(0, seq.tokens - seq.rows + last_row / A.gqa + 1) + 31) >> 5;
-        const auto tile_at = [&](int x) { return __builtin_amdgcn_readfirstlane((int)((int64_t)(x - unit) * tiles / length)); };
-        const int t0 = tile_at(pos), t1 = tile_at(unit_end);
+        const int last_row = min(flat, (block + 1) * RB) - 1;
+        const int tiles = (max(0, seq.tokens - seq.rows + last_row / gqa + 1) + 31) >> 5;
+        const auto tile_at = [&](int x) { return __builtin_amdgcn_readfirstlane((int)((double)(x - unit) * tiles / length)); };
+        const int t0 = tile_at(pos), t1 = tile_at(unit_end), stages = (t1 - t0 + NT - 1) / NT;
 
-        State<R> st;
-        st.clear();
+        Map st[MAPS];
+#pragma unroll
+        for (int m = 0; m < MAPS; ++m) st[m].clear();
 
-        // pages and scale words of 64 tiles, one a lane, and of the 64 behind them
-        int batch = t0, page, page_next;
-        u32x2 words, words_next;
-        const auto pages_from = [&](int t) { return t + lane < t1 ? page_of(P, s, (t + lane) >> per_page) : -1; };
-        const auto words_of = [&](int pg) {
-            u32x2 w = {0, 0};
-            if (pg >= 0) w = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)pg * P.n_kv + kv) * 2);
-            return w;
+        // Pages and scale words of 64 tiles, one a lane: those that are loaded from, what the softmax needs of those that it has come to, and the 64
+        // tiles behind.  A scale's info: exponents of keys and values in the low bytes, kNan, kThere.
+        constexpr int kNan = 1 << 16, kThere = 1 << 17;
+        const auto page_at = [&](int t) { const int lane = opaque(threadIdx.x) & 63; return t + lane < t1 ? page_of(P, s, (t + lane) >> per_page) : -1; };
+        const auto info_of = [&](int pg) {
+            if (pg < 0) return 0;
+            const u32x2 w = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)pg * P.n_kv + kv) * 2);
+            return (int)((w[0] & 0xffu) | (w[1] & 0xffu) << 8 | (w[1] & KVQ_P8_NAN ? kNan : 0) | kThere);
         };
-        page = pages_from(batch);
-        page_next = pages_from(batch + 64);
-        words = words_of(page);
-        words_next = u32x2{0, 0};
+        int load_batch = t0, soft_batch = t0;
+        int page = page_at(t0), page_next = page_at(t0 + 64), info = info_of(page), info_soft = info, info_next = 0;
 
-        struct Tile { int page, kw, vw; } now[NT], next[NT];
-        u32x4 kr[NT], vr[NT];
-        const auto load = [&](int t) {  // a quarter of every tile a wavefront
-            if (t - batch >= 64) {
+        struct Raw {
+            u32x4 w[NT];
+            int info;
+        } raw;
+        const auto load = [&](int stage, Raw& raw) {  // an eighth of a stage a wavefront: of two tiles a quarter of one, of one tile a quarter of its keys or values
+            const int t = t0 + stage * NT + (NT == 2 ? wave >> 2 : 0), lane = opaque(threadIdx.x) & 63;
+            if (t0 + stage * NT - load_batch >= 64) {
                 page = page_next;
-                words = words_next;
-                batch += 64;
-                page_next = pages_from(batch + 64);
+                info = info_next;
+                load_batch += 64;
+                page_next = page_at(load_batch + 64);
             }
-            if (t - batch == 32) words_next = words_of(page_next);
-#pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                next[x].page = __builtin_amdgcn_readlane(page, t - batch + x);
-                next[x].kw = __builtin_amdgcn_readlane(words[0], t - batch + x);
-                next[x].vw = __builtin_amdgcn_readlane(words[1], t - batch + x);
-                const uint8_t* const at = tile_of(P, max(0, next[x].page), kv, (t + x) & ((1 << per_page) - 1)) + wave * 1024 + lane * 16;
-                kr[x] = *reinterpret_cast<const u32x4*>(at);
-                vr[x] = *reinterpret_cast<const u32x4*>(at + 4096);
+            if (t0 + stage * NT - load_batch == 32) info_next = info_of(page_next);
+            const int page_here = __builtin_amdgcn_readlane(page, t - load_batch);
+            raw.info = __builtin_amdgcn_readlane(info, t - load_batch);
+            const uint8_t* const at = tile_of(P, max(0, page_here), kv, t & ((1 << per_page) - 1)) + (wave & 3) * 1024 + lane * 16;
+            if (NT == 2) {
+                raw.w[0] = *reinterpret_cast<const u32x4*>(at);
+                raw.w[NT - 1] = *reinterpret_cast<const u32x4*>(at + 4096);
+            } else {
+                raw.w[0] = *reinterpret_cast<const u32x4*>(at + (wave >> 2) * 4096);
             }
         };
-        const auto store = [&](int buf) {
+        const auto store = [&](int stage, const Raw& raw) {
+            uint8_t* const to = lds + (stage & 3) * STAGE + (NT == 2 ? wave >> 2 : 0) * TILE;
+            const int c = wave & 3, lane = opaque(threadIdx.x) & 63;
+            const auto keys = [&](u32x4 w) {  // sub-tile c / 2, channel groups 2 (c % 2) and + 1
+                const int at = ((lane >> 3) & 1) * 4096 + (lane >> 4) * 256 + ((c >> 1) * 8 + (lane & 7)) * 16 + (c & 1) * 2048;
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                uint8_t* const kt = lds + buf * STAGE + x * TILE + lane * 16;
-                uint8_t* const vt = kt + KVQ_FLASH_TILE_BYTES;
-                const float vs = value_scale(next[x].vw);
-                u32x4 v = vr[x];
-                if (next[x].page < 0) v = u32x4{0, 0, 0, 0};
-                if (next[x].vw & KVQ_P8_NAN) {
+                for (int k = 0; k < 2; ++k) *reinterpret_cast<half8*>(to + at + k * 1024) = widen(w[2 * k], w[2 * k + 1], 1.f);
+            };
+            const auto values = [&](u32x4 w) {  // channel blocks 2 c and + 1
+                if (!(raw.info & kThere)) w = u32x4{0, 0, 0, 0};
+                if (raw.info & kNan) {
 #pragma unroll
                     for (int d = 0; d < 4; ++d)
 #pragma unroll
                         for (int b = 0; b < 32; b += 8)
-                            if (((v[d] >> b) & 0x7fu) == 0x7fu) v[d] &= ~(0xffu << b);
+                            if (((w[d] >> b) & 0x7fu) == 0x7fu) w[d] &= ~(0xffu << b);
                 }
+                const float vs = value_scale(raw.info >> 8);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    // chunk `wave` of the K tile: sub-tile wave / 2, channel groups 2 (wave % 2) + h; of the V tile: channel block 2 wave + h
-                    *reinterpret_cast<half8*>(kt + (4 * (wave >> 1) + 2 * (wave & 1) + h) * 1024) = widen(kr[x][2 * h], kr[x][2 * h + 1], 1.f);
-                    *reinterpret_cast<half8*>(vt + (2 * wave + h) * 1024) = widen(v[2 * h], v[2 * h + 1], vs);
-                }
+                for (int k = 0; k < 2; ++k)
+                    *reinterpret_cast<half8*>(to + KVQ_FLASH_TILE_BYTES + (2 * c + k) * 1024 + lane * 16) = widen(w[2 * k], w[2 * k + 1], vs);
+            };
+            if (NT == 2) {
+                keys(raw.w[0]);
+                values(raw.w[NT - 1]);
+            } else if (wave < 4) {
+                keys(raw.w[0]);
+            } else {
+                values(raw.w[0]);
             }
         };
-        if (t0 < t1) {
-            load(t0);
-            store(0);
+        if constexpr (MAPS == 1) {  // the first two stages on their way together (of two maps there are no registers for it)
+            Raw early;
+            if (stages > 0) load(0, early);
+            if (stages > 1) load(1, raw);
+            if (stages > 0) store(0, early);
+        } else {
+            if (stages > 0) load(0, raw), store(0, raw);
+            if (stages > 1) load(1, raw);
         }
+        if (stages > 1) store(1, raw);
+        if (stages > 2) load(2, raw);
         __syncthreads();
-        int buf = 0;
-        for (int t = t0; t < t1; t += NT) {
-            const bool more = t + NT < t1;
+        const bool late = wave >= 4;
+        if (late) __syncthreads();
+
+        // Where the lane's operands lie.  Of keys, row n of the product is token 16 (n / 16) + 8 (n / 4 % 2) + 4 (n / 8 % 2) + n % 4, so that a half of the
+        // wavefront receives runs of eight tokens; the 16 rows of either half tile lie together, 256 bytes for eight channels, which 16 lanes read.
+        const auto keys_at = [](int lane) { return ((lane >> 4) & 1) * 4096 + (lane >> 5) * 256 + (lane & 15) * 16; };
+        const auto values_at = [](int lane) { return KVQ_FLASH_TILE_BYTES + ((lane >> 4) & 1) * 1024 + (lane >> 5) * 256 + (lane & 15) * 16; };
+
+        // stages that the wavefront's rows see; behind them it only loads (in a loop of its own: under a condition in one loop the accumulators were copied)
+        const int seen = max(0, min(stages, ((most + 31) / 32 - t0 + NT - 1) / NT));
+        int nan = 0;
+        uint32_t p[MAPS][NT][8];
+        // Products whose operands are read AHEAD steps in front of them, in this order (left to itself the compiler waits for every one)
+        const auto scores = [&](int stage, float16v (&sc)[MAPS][NT]) {
+            const int lane = opaque(threadIdx.x) & 63;
+            const uint8_t* const kt = lds + (stage & 3) * STAGE + keys_at(lane);
+            // step i: of two maps their 16 channels in turn, of one map the tiles
+            const auto kb_of = [](int i) { return MAPS == 2 ? (i & 1) * KB + (i >> 1) : i >> 1; };
+            const auto key = [&](int i) {
+                const int kb = kb_of(i), x = MAPS == 2 ? 0 : i & 1;
+                return to_half8(*reinterpret_cast<const u32x4*>(kt + x * TILE + (kb >> 1) * 1024 + (kb & 1) * 512));
+            };
+            half8 a[AHEAD], b[2];  // (b: the second map's queries, of every other step)
+            const auto query = [&](int i) { return to_half8(lds_q[wave][kb_of(i) & 3][lane]); };
 #pragma unroll
-            for (int x = 0; x < NT; ++x) now[x] = next[x];
-            if (more) load(t + NT);
-            if (t * 32 < most) {  // (behind what its rows see a wavefront only loads)
+            for (int i = 0; i < AHEAD; ++i) a[i] = key(i);
+            if (MAPS == 2) b[0] = query(1), b[1] = query(3);
 #pragma unroll
-                for (int x0 = 0; x0 < NT; x0 += TT) {
-                    const uint8_t* const kt = lds + buf * STAGE + x0 * TILE + lane * 16;
-                    const uint8_t* const vt = kt + KVQ_FLASH_TILE_BYTES;
-                    const int tok = (t + x0) * 32;
-                    float4v sc[R][TT][2];
+            for (int m = 0; m < MAPS; ++m)
 #pragma unroll
-                    for (int x = 0; x < TT; ++x)
+                for (int x = 0; x < NT; ++x)
 #pragma unroll
-                        for (int sub = 0; sub < 2; ++sub) {
+                    for (int i = 0; i < 16; ++i) sc[m][x][i] = 0.f;
 #pragma unroll
-                            for (int r = 0; r < R; ++r) sc[r][x][sub] = float4v{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 8 * NT; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int m = MAPS == 2 ? i & 1 : 0, x = MAPS == 2 ? 0 : i & 1;
+                sc[m][x] = mma32(a[i % AHEAD], m == 1 ? b[(i >> 1) & 1] : q[kb_of(i) % KB], sc[m][x]);
+                if (i + AHEAD < 8 * NT) a[i % AHEAD] = key(i + AHEAD);
+                if (m == 1 && i + 4 < 8) b[(i >> 1) & 1] = query(i + 4);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto values_times = [&](int stage) {
+            const int lane = opaque(threadIdx.x) & 63;
+            const uint8_t* const vt = lds + (stage & 3) * STAGE + values_at(lane);
+            const auto value = [&](int i) {  // step i: channel block i % 4 of tokens 16 (i / 4 % 2) .. of tile i / 8
+                return to_half8(*reinterpret_cast<const u32x4*>(vt + (i >> 3) * TILE + (i & 3) * 2048 + ((i >> 2) & 1) * 512));
+            };
+            half8 a[AHEAD];
 #pragma unroll
-                            for (int grp = 0; grp < 4; ++grp) {
-                                const half8 a = to_half8(*reinterpret_cast<const u32x4*>(kt + x * TILE + (sub * 4 + grp) * 1024));
+            for (int i = 0; i < AHEAD; ++i) a[i] = value(i);
 #pragma unroll
-                                for (int g = 0; g < RG; ++g) {
-                                    float4v& to = sc[MAPS * g + (MAPS == 2 ? grp >> 1 : 0)][x][sub];
-                                    to = mma(a, q[g][grp], to);
-                                }
-                            }
-                        }
-                    bool masked = least < tok + TT * 32;
-                    float factor[TT];
+            for (int i = 0; i < 8 * NT; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int x = i >> 3, u = (i >> 2) & 1;
 #pragma unroll
-                    for (int x = 0; x < TT; ++x) {
-                        masked = masked || now[x0 + x].page < 0;
-                        factor[x] = score_factor(A.scale_log2, now[x0 + x].kw);
-                    }
-                    if (masked) {
+                for (int m = 0; m < MAPS; ++m)
+                    st[m].o[i & 3] = mma32(a[i % AHEAD], to_half8(u32x4{p[m][x][4 * u], p[m][x][4 * u + 1], p[m][x][4 * u + 2], p[m][x][4 * u + 3]}), st[m].o[i & 3]);
+                if (i + AHEAD < 8 * NT) a[i % AHEAD] = value(i + AHEAD);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto softmax = [&](int stage, float16v (&sc)[MAPS][NT]) {
+            const int tok = (t0 + stage * NT) * 32, h = (opaque(threadIdx.x) >> 5) & 1;
+            if (t0 + stage * NT - soft_batch >= 64) {
+                info_soft = info;
+                soft_batch += 64;
+            }
+            int flags = kThere, here = 0, of[NT];
+            float factor[NT];
 #pragma unroll
-                        for (int g = 0; g < RG; ++g)
+            for (int x = 0; x < NT; ++x) {
+                of[x] = __builtin_amdgcn_readlane(info_soft, t0 + stage * NT + x - soft_batch);
+                factor[x] = score_factor(A.scale_log2, of[x]);
+                flags &= of[x];
+                here |= of[x];
+            }
+            if (least < tok + NT * 32 || !flags) {
 #pragma unroll
-                            for (int x = 0; x < TT; ++x) {
-                                const int over = (now[x0 + x].page < 0 ? 0 : limit[g] - tok - 32 * x) - 8 * j;
+                for (int x = 0; x < NT; ++x) {
+                    const int over = (of[x] & kThere ? limit - tok - 32 * x : 0) - 8 * h;
 #pragma unroll
-                                for (int m = 0; m < MAPS; ++m)
+                    for (int m = 0; m < MAPS; ++m)
 #pragma unroll
-                                    for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                                        for (int i = 0; i < 4; ++i)
-                                            if (4 * sub + i >= over) sc[MAPS * g + m][x][sub][i] = -INFINITY;
-                            }
-                    }
-                    uint32_t p[R][TT][4];
-#pragma unroll
-                    for (int r = 0; r < R; ++r) softmax_tiles<R, TT>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
-                    int flagged = 0;
-#pragma unroll
-                    for (int x = 0; x < TT; ++x) flagged |= now[x0 + x].page >= 0 ? now[x0 + x].vw : 0;
-                    if (flagged & KVQ_P8_NAN) {  // (one branch in front of all products)
-#pragma unroll 1
-                        for (int x = 0; x < TT; ++x) {
-                            const Tile& at_x = x ? now[x0 + TT - 1] : now[x0];
-                            if (!(at_x.vw & KVQ_P8_NAN) || at_x.page < 0) continue;
-                            const uint8_t* const at = tile_of(P, at_x.page, kv, (t + x0 + x) & ((1 << per_page) - 1)) + 4096 + lane * 16;
-#pragma unroll
-                            for (int nt = 0; nt < 8; ++nt) {
-                                const u32x2 w = *reinterpret_cast<const u32x2*>(at + (nt >> 1) * 1024 + (nt & 1) * 8);
-#pragma unroll
-                                for (int r = 0; r < R; ++r) {
-                                    uint32_t y[2] = {w[0], w[1]};
-                                    st.o[r][nt] += nan_codes(y, tok + 32 * x + 8 * j, limit[r / MAPS]);
-                                }
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int x = 0; x < TT; ++x)
-#pragma unroll
-                        for (int nt = 0; nt < 8; ++nt) {
-                            const half8 a = to_half8(*reinterpret_cast<const u32x4*>(vt + x * TILE + nt * 1024));
-#pragma unroll
-                            for (int r = 0; r < R; ++r) st.o[r][nt] = mma(a, to_half8(p[r][x]), st.o[r][nt]);
-                        }
+                        for (int i = 0; i < 16; ++i)
+                            sc[m][x][i] = 16 * (i >> 3) + (i & 7) < over ? sc[m][x][i] : -INFINITY;
                 }
             }
-            if (more) store(buf ^ 1);
+#pragma unroll
+            for (int m = 0; m < MAPS; ++m) {
+                softmax_tiles<NT>(st[m], sc[m], factor, MAPS == 1 && A.lse != nullptr, p[m]);
+                if (MAPS == 2) __builtin_amdgcn_sched_barrier(0);  // (side by side they take more registers than there are)
+            }
+            nan |= here;
+        };
+        const auto fetch = [&](int stage) {
+            if (stage + 2 < stages) store(stage + 2, raw);
+            if (stage + 3 < stages) load(stage + 3, raw);
             __syncthreads();
-            buf ^= 1;
+        };
+        for (int stage = 0; stage <= stages; ++stage) {
+            if (stage > 0 && stage <= seen) values_times(stage - 1);
+            float16v sc[MAPS][NT];  // (not beyond the turn: kept from one stage to the next they would be in the way of the outputs)
+            if (stage < seen) scores(stage, sc);
+            __syncthreads();
+            if (stage < seen) softmax(stage, sc);
+            fetch(stage);
+        }
+        if (!late) __syncthreads();
+        // NaN values, where a page has any: to the rows that see them, once more over the tiles (their codes were zeros above)
+        if (nan & kNan) {
+            const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
+            for (int tile = t0; tile < min(t1, t0 + seen * NT); ++tile) {
+                const int pg = __builtin_amdgcn_readfirstlane(page_of(P, s, tile >> per_page));
+                if (pg < 0 || !(P.words[((int64_t)pg * P.n_kv + kv) * 2 + 1] & KVQ_P8_NAN)) continue;
+                const uint8_t* const at = tile_of(P, pg, kv, tile & ((1 << per_page) - 1)) + 4096 + h * 256 + (n & 15) * 16 + (n >> 4) * 8;
+#pragma unroll
+                for (int cb = 0; cb < 4; ++cb) {
+                    float16v found;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) found[i] = 0.f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const u32x2 w = *reinterpret_cast<const u32x2*>(at + cb * 1024 + u * 512);
+                        half8 is, sees;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            is[e] = ((w[e >> 2] >> (8 * (e & 3))) & 0x7fu) == 0x7fu ? (_Float16)1.f : (_Float16)0.f;
+                            sees[e] = tile * 32 + 16 * u + 8 * h + e < limit ? (_Float16)1.f : (_Float16)0.f;
+                        }
+                        found = mma32(is, sees, found);
+                    }
+#pragma unroll
+                    for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) st[m].o[cb][i] += found[i] > 0.f ? __builtin_nanf("") : 0.f;
+                }
+            }
         }
 
+        const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
+        const Row row = row_of(n);
         // ---- the pieces of a unit that lies in several workgroups' shares, joined by the last of them in the order of the line
         const int w0 = unit / share, w1 = (unit + length - 1) / share, pieces = w1 - w0 + 1;
         bool mine = true;
         if (pieces > 1) {
-            constexpr int SLOT = 4 * R * KVQ_PART_BYTES;
+            constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP, LOADS = 8 / MAPS;
             const auto slot = [&](int k) {
                 return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(A.part) + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * SLOT, 0, SLOT, 0x00020000);
             };
-            const __amdgpu_buffer_rsrc_t to = slot(wg - w0);
-            const int own_at = wave * R * KVQ_PART_BYTES + lane * 16;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int at = own_at + r * KVQ_PART_BYTES;
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, st.o[r][nt]), to, at + nt * 1024, 0, 16);
-                const float l = quarters_sum(st.l[r]), fine = quarters_sum(st.fine[r]);
-                if (j == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st.m[r], l, fine, 0.f}), to, at + 8192, 0, 16);
-            }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
-                const uint32_t got = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                const bool last = got == (uint32_t)pieces - 1u;
-                if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                lds_last = last ? 1 : 0;
-            }
+            const int own_at = wave * MAPS * MAP + lane * 16;
+            uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
+            // Whoever finds that all others have stored theirs joins them; of two pieces that one does not store its own.  (Most often it is the piece that
+            // begins the unit: it comes last in its workgroup's share, the other first in its.)
+            if (threadIdx.x == 0)
+                lds_last = pieces == 2 && __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
             __syncthreads();
             mine = lds_last != 0;
+            if (!mine) {
+                const __amdgpu_buffer_rsrc_t to = slot(wg - w0);
+#pragma unroll
+                for (int m = 0; m < MAPS; ++m) {
+                    const int at = own_at + m * MAP;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float16v& o = st[m].o[v >> 2];
+                        const float4v x = {o[4 * (v & 3)], o[4 * (v & 3) + 1], o[4 * (v & 3) + 2], o[4 * (v & 3) + 3]};
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at + v * 1024, 0, 16);
+                    }
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st[m].m, st[m].l, st[m].fine, 0.f}), to, at + 16384, 0, 16);
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (threadIdx.x == 0) lds_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pieces - 1u ? 1 : 0;
+                __syncthreads();
+                mine = lds_last != 0;
+            }
+            if (mine && threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             asm volatile("" ::: "memory");
             if (mine) {
-                st.clear();
+                // (of two pieces one is in registers still; the products are rounded before they are added, so that it does not matter which)
+                const int own_piece = wg - w0;
+                if (pieces > 2)
+#pragma unroll
+                    for (int m = 0; m < MAPS; ++m) st[m].clear();
                 for (int k = 0; k < pieces; ++k) {
+                    if (pieces == 2 && k == own_piece) continue;
                     const __amdgpu_buffer_rsrc_t from = slot(k);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const int at = own_at + r * KVQ_PART_BYTES;
-                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at - j * 256 + 8192, 0, 16));
-                        float a, b;
-                        kvq_flash::join_row<R>(st, r, ml[0], j == 0 ? ml[1] : 0.f, j == 0 ? ml[2] : 0.f, a, b);
+                    for (int m = 0; m < MAPS; ++m) {
+                        const int at = own_at + m * MAP;
+                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + 16384, 0, 16));
+                        float a = 0.f, b = 0.f;
+                        const auto sum = [&](float own, float read) { return __fadd_rn(__fmul_rn(own, a), __fmul_rn(read, b)); };
 #pragma unroll
-                        for (int nt = 0; nt < 8; ++nt)
-                            st.o[r][nt] = st.o[r][nt] * a + __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + nt * 1024, 0, 16)) * b;
+                        for (int part = 0; part < 16 / LOADS; ++part) {
+                            float4v x[LOADS];  // on their way together
+#pragma unroll
+                            for (int v = 0; v < LOADS; ++v)
+                                x[v] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + (LOADS * part + v) * 1024, 0, 16));
+                            __builtin_amdgcn_sched_barrier(0);
+                            if (part == 0) {
+                                const float m_new = fmaxf(st[m].m, ml[0]), ref = reference_of(m_new);
+                                a = __builtin_amdgcn_exp2f(st[m].m - ref);
+                                b = __builtin_amdgcn_exp2f(ml[0] - ref);
+                                st[m].m = m_new;
+                                st[m].l = sum(st[m].l, ml[1]);
+                                st[m].fine = sum(st[m].fine, ml[2]);
+                            }
+#pragma unroll
+                            for (int v = 0; v < LOADS; ++v) {
+                                const int at_v = LOADS * part + v;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    st[m].o[at_v >> 2][4 * (at_v & 3) + i] = sum(st[m].o[at_v >> 2][4 * (at_v & 3) + i], x[v][i]);
+                            }
+                        }
                     }
                 }
             }
         }
         if (mine) {
+            float inv[MAPS], by;
 #pragma unroll
-            for (int g = 0; g < RG; ++g) {
-                const int f = block * RB + wave * 16 * RG + 16 * g + n, i = f / A.gqa, h = kv * A.gqa + f - i * A.gqa;
-                const bool real = f < ln.rows;
-                float inv[MAPS], fine = 0.f;
-#pragma unroll
-                for (int m = 0; m < MAPS; ++m) inv[m] = 2.f * kvq_flash::inverse_of(quarters_sum(st.l[MAPS * g + m]));
-                float4v x[8];
+            for (int m = 0; m < MAPS; ++m) inv[m] = 2.f * kvq_flash::inverse_of(halves_sum(st[m].l));
+            by = inv[0];
+            const float fine = MAPS == 1 ? halves_sum(st[0].fine) : 0.f;
+            if (MAPS == 2) {
+                inv[MAPS - 1] *= row.real ? A.lambda[row.head] : 0.f;
                 float square = 0.f;
-                const float lam = MAPS == 2 && real ? A.lambda[h] : 0.f;
 #pragma unroll
-                for (int nt = 0; nt < 8; ++nt) {
-                    x[nt] = st.o[MAPS * g][nt] * inv[0];
-                    if (MAPS == 2) {
-                        x[nt] = x[nt] - st.o[R - 1 - (MAPS * (RG - 1 - g))][nt] * inv[MAPS - 1] * lam;
+                for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) square = fmaf(x[nt][e], x[nt][e], square);
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = st[0].o[cb][i] * inv[0] - st[MAPS - 1].o[cb][i] * inv[MAPS - 1];
+                        st[0].o[cb][i] = x;
+                        square = fmaf(x, x, square);
+                    }
+                by = A.out_scale;
+                if (A.weight) {
+                    const float mean = halves_sum(square) * (1.f / KVQ_D) + A.eps;
+                    by *= mean > 0.f ? 1.f / sqrtf(mean) : mean;
+                }
+            }
+            if (row.real) {
+                const int64_t to = (seq.row0 + row.i) * A.o_rs + row.head * A.o_hs;
+                // two runs of eight channels at a time: after the exchange a half of the wavefront has one of them whole
+#pragma unroll
+                for (int v = 0; v < 16; v += 2) {
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float c = st[0].o[v >> 2][4 * (v & 3) + i], d = st[0].o[v >> 2][4 * (v & 3) + 4 + i];
+                        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(c), __float_as_uint(d), false, false);
+                        y[i] = __uint_as_float(both[0]) * by;
+                        y[4 + i] = __uint_as_float(both[1]) * by;
+                    }
+                    const int channel = 8 * (v + h);
+                    float4v lo = {y[0], y[1], y[2], y[3]}, hi = {y[4], y[5], y[6], y[7]};
+                    if (MAPS == 2 && A.weight) {
+                        lo *= *reinterpret_cast<const float4v*>(A.weight + channel);
+                        hi *= *reinterpret_cast<const float4v*>(A.weight + channel + 4);
+                    }
+                    if (A.out_fp32) {
+                        float4v* const to4 = reinterpret_cast<float4v*>(static_cast<float*>(A.out) + to + channel);
+                        to4[0] = lo;
+                        to4[1] = hi;
+                    } else {
+                        const u32x4 w = {kvq_flash::pack2(lo[0], lo[1]), kvq_flash::pack2(lo[2], lo[3]), kvq_flash::pack2(hi[0], hi[1]), kvq_flash::pack2(hi[2], hi[3])};
+                        *reinterpret_cast<u32x4*>(static_cast<_Float16*>(A.out) + to + channel) = w;
                     }
                 }
-                if (MAPS == 2) {
-                    float by = A.out_scale;
-                    if (A.weight) {
-                        const float mean = quarters_sum(square) * (1.f / KVQ_D) + A.eps;
-                        by *= mean > 0.f ? 1.f / sqrtf(mean) : mean;
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < 8; ++nt) {
-                        x[nt] *= by;
-                        if (A.weight) x[nt] *= *reinterpret_cast<const float4v*>(A.weight + 16 * nt + 4 * j);
-                    }
-                } else {
-                    fine = quarters_sum(st.fine[g]);
-                }
-                if (!real) continue;
-                const int64_t to = (seq.row0 + i) * A.o_rs + h * A.o_hs;
-                void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt) kvq_flash::store_out4(dst, A.out_fp32, 16 * nt + 4 * j, x[nt]);
-                if (MAPS == 1 && A.lse && j == 0)
-                    A.lse[h * A.lse_hs + seq.row0 + i] = fine == 0.f ? -INFINITY : (st.m[g] + __builtin_amdgcn_logf(fine)) * 0.69314718055994530942f;
+                if (MAPS == 1 && A.lse && h == 0)
+                    A.lse[row.head * A.lse_hs + seq.row0 + row.i] = fine == 0.f ? -INFINITY : (st[0].m + __builtin_amdgcn_logf(fine)) * 0.69314718055994530942f;
             }
         }
         pos = unit_end;
@@ -821,9 +981,9 @@ bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
     // as many workgroups as pieces there can be, and partial results of those of units that are cut
     const int64_t units = (rows + 16 * plan.r - 1) / (16 * plan.r) * heads, cuts = units * ((tiles + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
     plan.groups = std::min(cuts, 2 * units > KVQ_P8_GROUPS ? KVQ_P8_GROUPS + units : KVQ_P8_GROUPS);
-    const int64_t line = ((most + 63) / 64) * (tiles + 8 + P.max_rows / 32) * heads;
-    plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
-    plan.bytes = kCounterBytes + 2 * (uint64_t)KVQ_PART_BYTES * std::max<uint64_t>(std::min<int64_t>(cuts, KVQ_P8_GROUPS) * plan.r, plan.chunk * 4 * (maps == 1 ? 2 : 4));
+    const int64_t line = ((most + 255) / 256) * (tiles + 8 + P.max_rows / 32) * heads;
+    plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_CHUNK_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
+    plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(cuts, KVQ_P8_GROUPS) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
     return true;
 }
 
@@ -852,8 +1012,8 @@ kvq_status_t attend(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, 
     else hipLaunchKernelGGL(kvq_paged8_ranges_kernel<2>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
     if (!plan.chunk) return KVQ_OK;
-    if (A.maps == 1) hipLaunchKernelGGL((kvq_paged8_chunk_kernel<2, 1, 2>), dim3((unsigned)plan.chunk), dim3(256), 0, stream, A);
-    else hipLaunchKernelGGL((kvq_paged8_chunk_kernel<1, 2, 2>), dim3((unsigned)plan.chunk), dim3(256), 0, stream, A);
+    if (A.maps == 1) hipLaunchKernelGGL(kvq_paged8_chunk_kernel<1>, dim3((unsigned)plan.chunk), dim3(512), 0, stream, A);
+    else hipLaunchKernelGGL(kvq_paged8_chunk_kernel<2>, dim3((unsigned)plan.chunk), dim3(512), 0, stream, A);
     return hipGetLastError() == hipSuccess ? KVQ_OK : KVQ_E_HIP;
 }
 
