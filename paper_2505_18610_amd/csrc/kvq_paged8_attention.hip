@@ -29,6 +29,7 @@ using kvq_flash::to_half8;
 #define KVQ_P8_CHUNK_GROUPS 256 // workgroups of a launch over chunks, at most: one a compute unit
 #define KVQ_P8_MAP_BYTES 17408  // partial results of a wavefront with a chunk and one map
 #define KVQ_P8_MOST_PIECES 128  // of a unit
+#define KVQ_P8_ROOT 0.7f        // tiles of a piece by the root of the longest unit's, at least
 
 struct AttnArgs {
     KvqP8 p;
@@ -115,7 +116,8 @@ struct Cuts {
         sum([&](Shape x) { longest = max(longest, x.units ? x.tiles : 0); return 0; });
         longest = wave_max(longest);
         const int wanted = KVQ_P8_GROUPS;
-        int low = max(max(KVQ_P8_LEAST_SHARE, (tiles + wanted - 1) / wanted), (longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES);
+        int low = max(max(KVQ_P8_LEAST_SHARE, (tiles + wanted - 1) / wanted),
+                      max((longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES, (int)(KVQ_P8_ROOT * sqrtf((float)longest))));
         share = low;
         if (2 * units > wanted) return;
         int high = max(low, (tiles + wanted - units - 1) / (wanted - units));  // enough: a unit has at most one piece more than its tiles by the share
@@ -361,22 +363,56 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
             mine = lds_last != 0;
             asm volatile("" ::: "memory");
             if (mine) {
+                // All pieces of a row by the 32 lanes that have its channels: references and sums a piece a lane, whose weights pass through LDS, then the
+                // outputs, eight pieces on their way together.  Pieces beyond the last read as zeros, by the buffer's range, with a weight of zero.
+                float(*const weights)[KVQ_P8_MOST_PIECES] = reinterpret_cast<float(*)[KVQ_P8_MOST_PIECES]>(lds_o);
+                const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot(0), 0, pieces * R * KVQ_PART_BYTES, 0x00020000);
+                constexpr int STEP = R * KVQ_PART_BYTES;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     if (16 * r + row >= real_rows) continue;
+                    const auto load = [&](int k) {
+                        return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, k * STEP + r * KVQ_PART_BYTES + tid * 16, 0, 16));
+                    };
+                    float4v x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = load(k);
+                    constexpr int PER = KVQ_P8_MOST_PIECES / 32;
+                    float4v ml[PER];
+#pragma unroll
+                    for (int c = 0; c < PER; ++c)
+                        ml[c] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, (chunk + 32 * c) * STEP + r * KVQ_PART_BYTES + KVQ_PART_O_FLOATS * 4 + row * 16, 0, 16));
                     m[r] = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < PER; ++c) m[r] = chunk + 32 * c < pieces ? fmaxf(m[r], ml[c][0]) : m[r];
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) m[r] = fmaxf(m[r], __shfl_xor(m[r], d));
+                    const float ref = reference_of(m[r]);
                     l[r] = fine[r] = 0.f;
+#pragma unroll
+                    for (int c = 0; c < PER; ++c) {
+                        const float w = chunk + 32 * c < pieces ? __builtin_amdgcn_exp2f(ml[c][0] - ref) : 0.f;
+                        l[r] += ml[c][1] * w;
+                        fine[r] += ml[c][2] * w;
+                        weights[row][chunk + 32 * c] = w;
+                    }
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        l[r] += __shfl_xor(l[r], d);
+                        fine[r] += __shfl_xor(fine[r], d);
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (a row's weights are written and read by one wavefront)
+                    __builtin_amdgcn_wave_barrier();
                     o[r] = float4v{0.f, 0.f, 0.f, 0.f};
-                    for (int k = 0; k < pieces; ++k) {
-                        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot(k), 0, R * KVQ_PART_BYTES, 0x00020000);
-                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, r * KVQ_PART_BYTES + KVQ_PART_O_FLOATS * 4 + row * 16, 0, 16));
-                        const float4v x = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, r * KVQ_PART_BYTES + tid * 16, 0, 16));
-                        const float m_new = fmaxf(m[r], ml[0]), ref = reference_of(m_new);
-                        const float a = __builtin_amdgcn_exp2f(m[r] - ref), b = __builtin_amdgcn_exp2f(ml[0] - ref);
-                        o[r] = o[r] * a + x * b;
-                        l[r] = l[r] * a + ml[1] * b;
-                        fine[r] = fine[r] * a + ml[2] * b;
-                        m[r] = m_new;
+                    for (int k0 = 0; k0 < pieces; k0 += 8) {
+                        float4v y[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) y[k] = x[k];
+                        if (k0 + 8 < pieces)
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) x[k] = load(k0 + 8 + k);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) o[r] += y[k] * weights[row][k0 + k];
                     }
                 }
             }
