@@ -26,8 +26,12 @@ using kvq_flash::to_half8;
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
 #define KVQ_P8_LEAST_SHARE 8    // tiles of a workgroup, at least
 #define KVQ_P8_LEAST_CHUNK 16   // of a workgroup with a chunk
+#define KVQ_P8_CHUNK_ROOT 2.f   // of a workgroup with a chunk by the root of the longest unit's, at least
+#define KVQ_P8_CHUNK_PIECES 64  // of a unit
 #define KVQ_P8_CHUNK_GROUPS 256 // workgroups of a launch over chunks, at most: one a compute unit
 #define KVQ_P8_MAP_BYTES 17408  // partial results of a wavefront with a chunk and one map
+#define KVQ_P8_SMALL_UNITS 512
+#define KVQ_P8_SMALL_TILES 40000 // of all units
 #define KVQ_P8_MOST_PIECES 128  // of a unit
 #define KVQ_P8_ROOT 0.7f        // tiles of a piece by the root of the longest unit's, at least
 
@@ -41,7 +45,7 @@ struct AttnArgs {
     float* part;
     int64_t q_rs, q_hs, o_rs, o_hs, lse_hs;
     int32_t gqa, maps, out_fp32;   // gqa: query heads of a KV head
-    int32_t least_rows;            // sequences with more flat rows (of one map) are chunks
+    int32_t few_rows;              // sequences with more flat rows (of one map) are chunks, unless the call is small
     float scale_log2, eps, out_scale;
     uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
 };
@@ -87,31 +91,40 @@ __device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
 // map by map; a block has 16 R of them.  Units of many tiles are cut into pieces of `share` tiles at most, one workgroup each: where the units
 // are few, of the smallest share that leaves no more pieces than the device takes workgroups at a time (a workgroup that came behind them would
 // have the device for itself), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
+// Calls in which sequences of many rows are taken like those of few: what they would be joined by costs more than their larger blocks save.
+__device__ inline bool small_call(int units, int tiles) { return units <= KVQ_P8_SMALL_UNITS && tiles <= KVQ_P8_SMALL_TILES; }
 struct Piece {
     int seq, unit, tiles, pieces, piece;
     int slot;  // of the unit's first piece among those of all units that are cut
 };
 struct Cuts {
-    struct Shape { int tiles, units; };
+    struct Shape { int tiles, units, few; };  // few: 1 where the sequence has few rows
     const Shape* all;  // of all sequences, where they are more than lanes
     Shape mine;
+    bool small;
     int n, per, lane, share;
 
     // over this lane's sequences
     template <class F>
     __device__ int sum(F f) const {
-        if (per == 1) return f(mine);
+        const auto part = [&](Shape x) { return f(Shape{x.tiles, small || x.few ? x.units : 0, 0}); };  // without what is another kernel's
+        if (per == 1) return part(mine);
         int x = 0;
         for (int k = 0; k < per; ++k)
-            if (lane * per + k < n) x += f(all[lane * per + k]);
+            if (lane * per + k < n) x += part(all[lane * per + k]);
         return x;
     }
     template <class F>
     __device__ int total(F f) const { return __builtin_amdgcn_readlane(wave_scan(sum(f)), 63); }
     __device__ int cuts_of(Shape x) const { return (x.tiles + share - 1) / share; }
 
-    __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_) : all(shapes), mine(own), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
-        const int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
+    __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_) : all(shapes), mine(own), small(true), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
+        int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
+        if (!small_call(units, tiles)) {
+            small = false;
+            units = total([](Shape x) { return x.units; });
+            tiles = total([](Shape x) { return x.units * x.tiles; });
+        }
         int longest = 0;
         sum([&](Shape x) { longest = max(longest, x.units ? x.tiles : 0); return 0; });
         longest = wave_max(longest);
@@ -141,7 +154,8 @@ struct Cuts {
         p.seq = at;
         if (per > 1) {  // among that lane's sequences, one a lane
             const int i = at * per + lane;
-            s = lane < per && i < n ? all[i] : Shape{1, 0};
+            s = lane < per && i < n ? all[i] : Shape{1, 0, 0};
+            if (!small && !s.few) s.units = 0;
             x = pieces(s);
             y = cut(s);
             upto = before + wave_scan(x);
@@ -176,15 +190,15 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     // ---- which piece
     const auto shape = [&](int at) {
         const Seq q = seq_of(P, at);
-        const int blocks = q.rows * A.gqa > A.least_rows ? 0 : (q.rows * rows_per_token + RB - 1) / RB;
-        return Cuts::Shape{max(1, (q.tokens + 31) >> 5), blocks * P.n_kv};
+        const int blocks = (q.rows * rows_per_token + RB - 1) / RB;
+        return Cuts::Shape{max(1, (q.tokens + 31) >> 5), blocks * P.n_kv, q.rows * A.gqa <= A.few_rows ? 1 : 0};
     };
     Cuts::Shape* const shapes = reinterpret_cast<Cuts::Shape*>(lds_o);
     if (P.n_seqs > 64) {
         for (int at = threadIdx.x; at < P.n_seqs; at += 512) shapes[at] = shape(at);
         __syncthreads();
     }
-    Cuts cuts(shapes, P.n_seqs, P.n_seqs <= 64 && lane < P.n_seqs ? shape(lane) : Cuts::Shape{1, 0}, lane);
+    Cuts cuts(shapes, P.n_seqs, P.n_seqs <= 64 && lane < P.n_seqs ? shape(lane) : Cuts::Shape{1, 0, 0}, lane);
     Piece pc;
     if (!cuts.find(blockIdx.x, pc)) return;
     const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
@@ -467,12 +481,12 @@ struct Line {
     __device__ int at(int b) const { return __builtin_amdgcn_readfirstlane(place(b, seen, growth)); }
 };
 template <int RB>
-__device__ inline Line line_of(const Seq& q, int per_token, int least_rows) {
+__device__ inline Line line_of(const Seq& q, int per_token, int few_rows) {
     Line x;
     x.rows = q.rows * per_token;
     x.seen = max(0, q.tokens - q.rows) * (1. / 32);
     x.growth = RB / 64. / per_token;
-    x.blocks = x.rows > least_rows ? (x.rows + RB - 1) / RB : 0;
+    x.blocks = x.rows > few_rows ? (x.rows + RB - 1) / RB : 0;
     x.length = Line::place(x.blocks, x.seen, x.growth);
     return x;
 }
@@ -564,11 +578,27 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_page = P.page_shift - 5;
 
-    const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.least_rows); };
-    const auto count = [&](int s) { return line(seq_of(P, s)).length * P.n_kv; };
+    {
+        const auto units_of = [&](int s) { return (seq_of(P, s).rows * A.gqa * MAPS + 31) / 32 * P.n_kv; };  // as the launch over pieces counts them
+        const auto tiles_of = [&](int s) { return units_of(s) * max(1, (seq_of(P, s).tokens + 31) >> 5); };
+        const Census<decltype(units_of)> units(units_of, P.n_seqs);
+        const Census<decltype(tiles_of)> tiles(tiles_of, P.n_seqs);
+        if (small_call(units.total, tiles.total)) return;
+    }
+    const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.few_rows); };
+    int longest = 0;
+    const auto count = [&](int s) {
+        const Seq q = seq_of(P, s);
+        const Line x = line(q);
+        if (x.blocks) longest = max(longest, (q.tokens >> 5) + Line::kLead);
+        return x.length * P.n_kv;
+    };
     const Census<decltype(count)> census(count, P.n_seqs);
     if (census.total == 0) return;
-    const int groups = gridDim.x, share = max(KVQ_P8_LEAST_CHUNK, (census.total + groups - 1) / groups);
+    // (joining a piece takes as long as several tiles: with n pieces of a unit of t tiles t / n + 4 n is least about there)
+    const int groups = gridDim.x;
+    const auto least_share = [](int t) { return max((int)(KVQ_P8_CHUNK_ROOT * sqrtf((float)t)), (t + 16) / (KVQ_P8_CHUNK_PIECES - 4) + 1); };
+    const int share = max(max(KVQ_P8_LEAST_CHUNK, (census.total + groups - 1) / groups), least_share(wave_max(longest)));
     // neighbours on the line go to one XCD, whose L2 then holds the keys and values that they have in common
     const int wg = groups % 8 == 0 ? (blockIdx.x & 7) * (groups >> 3) + (blockIdx.x >> 3) : blockIdx.x;
     int pos = wg * share;
@@ -863,7 +893,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         const int w0 = unit / share, w1 = (unit + length - 1) / share, pieces = w1 - w0 + 1;
         bool mine = true;
         if (pieces > 1) {
-            constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP, LOADS = 8 / MAPS;
+            constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP;
+            const bool rows_here = block * RB + wave * 32 < flat;  // whether the wavefront has any
             const auto slot = [&](int k) {
                 return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(A.part) + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * SLOT, 0, SLOT, 0x00020000);
             };
@@ -877,6 +908,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             mine = lds_last != 0;
             if (!mine) {
                 const __amdgpu_buffer_rsrc_t to = slot(wg - w0);
+                if (rows_here)
 #pragma unroll
                 for (int m = 0; m < MAPS; ++m) {
                     const int at = own_at + m * MAP;
@@ -896,44 +928,57 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             }
             if (mine && threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             asm volatile("" ::: "memory");
-            if (mine) {
-                // (of two pieces one is in registers still; the products are rounded before they are added, so that it does not matter which)
-                const int own_piece = wg - w0;
-                if (pieces > 2)
+            if (mine && rows_here) {
+                // References and sums first, the references into LDS, then the outputs, FLY loads on their way throughout.  Of two pieces one is in registers
+                // still: products are rounded before they are added, so that it does not matter which.
+                const int skip = pieces == 2 ? wg - w0 : -1;
+                float* const refs = reinterpret_cast<float*>(lds) + wave * (KVQ_P8_CHUNK_PIECES * 32) + n;
 #pragma unroll
-                    for (int m = 0; m < MAPS; ++m) st[m].clear();
-                for (int k = 0; k < pieces; ++k) {
-                    if (pieces == 2 && k == own_piece) continue;
-                    const __amdgpu_buffer_rsrc_t from = slot(k);
+                for (int m = 0; m < MAPS; ++m) {
+                    const int at = own_at + m * MAP;
+                    const float own = st[m].m;
+                    if (pieces > 2) st[m].clear();
+                    for (int k0 = 0; k0 < pieces; k0 += 8) {
+                        float4v ml[8];  // on their way together; the last piece's again behind it
 #pragma unroll
-                    for (int m = 0; m < MAPS; ++m) {
-                        const int at = own_at + m * MAP;
-                        const float4v ml = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + 16384, 0, 16));
-                        float a = 0.f, b = 0.f;
-                        const auto sum = [&](float own, float read) { return __fadd_rn(__fmul_rn(own, a), __fmul_rn(read, b)); };
+                        for (int i = 0; i < 8; ++i)
+                            ml[i] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(slot(min(k0 + i, pieces - 1)), at + 16384, 0, 16));
 #pragma unroll
-                        for (int part = 0; part < 16 / LOADS; ++part) {
-                            float4v x[LOADS];  // on their way together
-#pragma unroll
-                            for (int v = 0; v < LOADS; ++v)
-                                x[v] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + (LOADS * part + v) * 1024, 0, 16));
-                            __builtin_amdgcn_sched_barrier(0);
-                            if (part == 0) {
-                                const float m_new = fmaxf(st[m].m, ml[0]), ref = reference_of(m_new);
-                                a = __builtin_amdgcn_exp2f(st[m].m - ref);
-                                b = __builtin_amdgcn_exp2f(ml[0] - ref);
-                                st[m].m = m_new;
-                                st[m].l = sum(st[m].l, ml[1]);
-                                st[m].fine = sum(st[m].fine, ml[2]);
-                            }
-#pragma unroll
-                            for (int v = 0; v < LOADS; ++v) {
-                                const int at_v = LOADS * part + v;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    st[m].o[at_v >> 2][4 * (at_v & 3) + i] = sum(st[m].o[at_v >> 2][4 * (at_v & 3) + i], x[v][i]);
-                            }
+                        for (int i = 0; i < 8; ++i) {
+                            const int k = k0 + i;
+                            if (k == skip || k >= pieces) continue;
+                            const float m_new = fmaxf(st[m].m, ml[i][0]), ref = reference_of(m_new);
+                            const float a = __builtin_amdgcn_exp2f(st[m].m - ref), b = __builtin_amdgcn_exp2f(ml[i][0] - ref);
+                            st[m].l = __fadd_rn(__fmul_rn(st[m].l, a), __fmul_rn(ml[i][1], b));
+                            st[m].fine = __fadd_rn(__fmul_rn(st[m].fine, a), __fmul_rn(ml[i][2], b));
+                            st[m].m = m_new;
+                            refs[k * 32] = ml[i][0];  // (both halves of the wavefront write the same)
                         }
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (read by the wavefront that has written it)
+                    __builtin_amdgcn_wave_barrier();
+                    const float ref = reference_of(st[m].m);
+                    if (pieces == 2) {
+                        const float a = __builtin_amdgcn_exp2f(own - ref);
+#pragma unroll
+                        for (int cb = 0; cb < 4; ++cb) st[m].o[cb] *= a;
+                    }
+                    const auto load = [&](int k, int v) { return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(slot(k), at + v * 1024, 0, 16)); };
+                    constexpr int FLY = MAPS == 1 ? 16 : 4;
+                    float4v x[FLY];
+                    int k = skip == 0 ? 1 : 0;
+#pragma unroll
+                    for (int v = 0; v < FLY; ++v) x[v] = load(k, v);
+                    while (k < pieces) {
+                        const int next = k + 1 == skip ? k + 2 : k + 1, from = min(next, pieces - 1);
+                        const float w = __builtin_amdgcn_exp2f(refs[k * 32] - ref);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) st[m].o[v >> 2][4 * (v & 3) + i] = __fadd_rn(st[m].o[v >> 2][4 * (v & 3) + i], __fmul_rn(x[v % FLY][i], w));
+                            x[v % FLY] = load(v + FLY < 16 ? k : from, (v + FLY) & 15);
+                        }
+                        k = next;
                     }
                 }
             }
@@ -1014,12 +1059,16 @@ bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
     const int64_t tiles = (int64_t)P.table_pages << (P.page_shift - 5), heads = (int64_t)P.n_seqs * P.n_kv;
     // blocks of 16 rows bound both: every number on either line stays below 2^30
     if (heads && (most * maps + 15) / 16 * (tiles + 8 + P.max_rows / 32) > (1 << 30) / heads) return false;
-    // as many workgroups as pieces there can be, and partial results of those of units that are cut
-    const int64_t units = (rows + 16 * plan.r - 1) / (16 * plan.r) * heads, cuts = units * ((tiles + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
-    plan.groups = std::min(cuts, 2 * units > KVQ_P8_GROUPS ? KVQ_P8_GROUPS + units : KVQ_P8_GROUPS);
+    // as many workgroups as pieces there can be (of few rows, or of all in a small call), and partial results of those of units that are cut
+    const auto pieces = [&](int64_t flat, int64_t limit) {
+        const int64_t units = std::min(limit, (flat * maps + 16 * plan.r - 1) / (16 * plan.r) * heads);
+        const int64_t cuts = units * ((tiles + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
+        return std::min(cuts, 2 * units > KVQ_P8_GROUPS ? KVQ_P8_GROUPS + units : KVQ_P8_GROUPS);
+    };
+    plan.groups = std::max(pieces(std::min<int64_t>(most, kFewRows), INT32_MAX), pieces(most, KVQ_P8_SMALL_UNITS));
     const int64_t line = ((most + 255) / 256) * (tiles + 8 + P.max_rows / 32) * heads;
     plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_CHUNK_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
-    plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(cuts, KVQ_P8_GROUPS) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
+    plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(plan.groups, KVQ_P8_GROUPS) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
     return true;
 }
 
@@ -1043,7 +1092,7 @@ kvq_status_t attend(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, 
     A.flip = scale < 0.f ? 0x80008000u : 0u;
     A.counters = static_cast<uint32_t*>(workspace);
     A.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterBytes);
-    A.least_rows = kFewRows;
+    A.few_rows = kFewRows;
     if (plan.r == 1) hipLaunchKernelGGL(kvq_paged8_ranges_kernel<1>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     else hipLaunchKernelGGL(kvq_paged8_ranges_kernel<2>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;
