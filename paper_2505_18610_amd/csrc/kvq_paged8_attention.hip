@@ -24,7 +24,9 @@ using kvq_flash::to_half8;
 
 #define KVQ_P8_GROUPS 512       // pieces of few units that a launch is cut into, at most
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
-#define KVQ_P8_LEAST_SHARE 8    // tiles of a workgroup, at least
+#define KVQ_P8_LEAST_SHARE 8    // tiles of a piece, at least: one for each wavefront
+#define KVQ_P8_WHOLE 16         // tiles of units that are not cut: a second round takes 0.6 us, joining 1.7 (300 tokens 8.3 -> 7.2 us)
+#define KVQ_P8_MANY_SHARE 24    // tiles of a piece where units are many, at least (264 units of 22 to 32 tiles 19.4 -> 15.9 us)
 #define KVQ_P8_LEAST_CHUNK 16   // of a workgroup with a chunk
 #define KVQ_P8_CHUNK_ROOT 2.f   // of a workgroup with a chunk by the root of the longest unit's, at least
 #define KVQ_P8_CHUNK_PIECES 64  // of a unit
@@ -116,7 +118,7 @@ struct Cuts {
     }
     template <class F>
     __device__ int total(F f) const { return __builtin_amdgcn_readlane(wave_scan(sum(f)), 63); }
-    __device__ int cuts_of(Shape x) const { return (x.tiles + share - 1) / share; }
+    __device__ int cuts_of(int tiles) const { return tiles <= KVQ_P8_WHOLE ? 1 : (uint32_t)(tiles + share - 1) / (uint32_t)share; }
 
     __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_) : all(shapes), mine(own), small(true), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
         int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
@@ -131,20 +133,20 @@ struct Cuts {
         const int wanted = KVQ_P8_GROUPS;
         int low = max(max(KVQ_P8_LEAST_SHARE, (tiles + wanted - 1) / wanted),
                       max((longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES, (int)(KVQ_P8_ROOT * sqrtf((float)longest))));
-        share = low;
+        share = max(low, KVQ_P8_MANY_SHARE);
         if (2 * units > wanted) return;
         int high = max(low, (tiles + wanted - units - 1) / (wanted - units));  // enough: a unit has at most one piece more than its tiles by the share
         while (high - low > low >> 4) {
             share = (low + high) >> 1;
-            if (total([&](Shape x) { return x.units * cuts_of(x); }) <= wanted) high = share;
+            if (total([&](Shape x) { return x.units * cuts_of(x.tiles); }) <= wanted) high = share;
             else low = share + 1;
         }
         share = high;
     }
     // Piece `id`, the same in all lanes.
     __device__ bool find(int id, Piece& p) const {
-        const auto pieces = [&](Shape x) { return x.units * cuts_of(x); };
-        const auto cut = [&](Shape x) { const int c = cuts_of(x); return c > 1 ? x.units * c : 0; };
+        const auto pieces = [&](Shape x) { return x.units * cuts_of(x.tiles); };
+        const auto cut = [&](Shape x) { const int c = cuts_of(x.tiles); return c > 1 ? x.units * c : 0; };
         int x = sum(pieces), y = sum(cut), upto = wave_scan(x), cut_upto = wave_scan(y);
         uint64_t behind = __ballot(upto > id);
         if (!behind) return false;
@@ -166,8 +168,8 @@ struct Cuts {
             p.seq = __builtin_amdgcn_readlane(i, at);
         }
         p.tiles = __builtin_amdgcn_readlane(s.tiles, at);
-        p.pieces = (p.tiles + share - 1) / share;
-        p.unit = (id - before) / p.pieces;
+        p.pieces = cuts_of(p.tiles);
+        p.unit = (uint32_t)(id - before) / (uint32_t)p.pieces;
         p.piece = id - before - p.unit * p.pieces;
         p.slot = slots + p.unit * p.pieces;
         return true;
@@ -188,48 +190,38 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     const int rows_per_token = A.gqa * A.maps;
 
     // ---- which piece
-    const auto shape = [&](int at) {
-        const Seq q = seq_of(P, at);
-        const int blocks = (q.rows * rows_per_token + RB - 1) / RB;
-        return Cuts::Shape{max(1, (q.tokens + 31) >> 5), blocks * P.n_kv, q.rows * A.gqa <= A.few_rows ? 1 : 0};
+    const auto shape = [&](const Seq& q) {
+        const uint32_t blocks = (uint32_t)(q.rows * rows_per_token + RB - 1) / RB;
+        return Cuts::Shape{max(1, (q.tokens + 31) >> 5), (int)blocks * P.n_kv, q.rows * A.gqa <= A.few_rows ? 1 : 0};
     };
     Cuts::Shape* const shapes = reinterpret_cast<Cuts::Shape*>(lds_o);
+    Seq seq = {0, 0, 0};
     if (P.n_seqs > 64) {
-        for (int at = threadIdx.x; at < P.n_seqs; at += 512) shapes[at] = shape(at);
+        for (int at = threadIdx.x; at < P.n_seqs; at += 512) shapes[at] = shape(seq_of(P, at));
         __syncthreads();
+    } else if (lane < P.n_seqs) {
+        seq = seq_of(P, lane);
     }
-    Cuts cuts(shapes, P.n_seqs, P.n_seqs <= 64 && lane < P.n_seqs ? shape(lane) : Cuts::Shape{1, 0, 0}, lane);
+    Cuts cuts(shapes, P.n_seqs, shape(seq), lane);
     Piece pc;
     if (!cuts.find(blockIdx.x, pc)) return;
     const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
-    const Seq seq = seq_of(P, s);
-    const int blocks = (seq.rows * rows_per_token + RB - 1) / RB, kv = pc.unit / blocks, block = pc.unit - kv * blocks;
+    if (P.n_seqs > 64) seq = seq_of(P, s);
+    else seq = Seq{__builtin_amdgcn_readlane(seq.row0, s), __builtin_amdgcn_readlane(seq.rows, s), __builtin_amdgcn_readlane(seq.tokens, s)};
+    const int blocks = (uint32_t)(seq.rows * rows_per_token + RB - 1) / RB, kv = (uint32_t)pc.unit / (uint32_t)blocks, block = pc.unit - kv * blocks;
     // (equal ranges: 33 tiles are 17 and 16, not 32 and 1)
-    const int t0 = (int)((int64_t)tiles * piece / pieces), t1 = (int)((int64_t)tiles * (piece + 1) / pieces);
-    int limit[R];
+    const int each = (uint32_t)tiles / (uint32_t)pieces, left = tiles - each * pieces;
+    const int t0 = piece * each + min(piece, left), t1 = t0 + each + (piece < left ? 1 : 0);
+    int limit[R], row_i[R];
     int most = 0, least = 0x7fffffff;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int f = block * RB + 16 * r + n, i = f / rows_per_token;
-        const bool real = i < seq.rows;
-        limit[r] = real ? max(0, seq.tokens - seq.rows + i + 1) : seq.tokens;
+        row_i[r] = (uint32_t)(block * RB + 16 * r + n) / (uint32_t)rows_per_token;
+        const bool real = row_i[r] < seq.rows;
+        limit[r] = real ? max(0, seq.tokens - seq.rows + row_i[r] + 1) : seq.tokens;
         most = max(most, real ? limit[r] : 0);
         least = min(least, limit[r]);
     }
-    if (wave < 4) {  // four channel groups of the rows, one a wavefront
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int f = block * RB + 16 * r + n, i = f / rows_per_token, rest = f - i * rows_per_token;
-            const int h = A.maps == 2 ? rest >> 1 : rest, map = A.maps == 2 ? rest & 1 : 0;
-            u32x4 w = {0, 0, 0, 0};
-            if (i < seq.rows && (A.maps == 1 || (wave >> 1) == map)) {
-                w = *reinterpret_cast<const u32x4*>(A.q + (seq.row0 + i) * A.q_rs + (int64_t)(kv * A.gqa + h) * A.q_hs + 32 * wave + 8 * j);
-                w ^= A.flip;
-            }
-            lds_q[r][wave][lane] = w;
-        }
-    }
-    __syncthreads();
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
         most = max(most, __shfl_xor(most, d));
@@ -239,32 +231,57 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     least = __builtin_amdgcn_readfirstlane(least);
     const int end = min(t1, (most + 31) >> 5);
 
+    // ---- the wavefront's tiles: pages and scale words of 64 of them, one a lane, and one tile's codes on their way.  What lies behind the last, or
+    // on no page, is behind its buffer's end: a load under a condition would make the compiler wait for it at once.
+    int from = t0 + wave, page = -1;
+    u32x2 words = {0, 0};
+    u32x4 kc[4], vc[4];
+    const auto describe = [&]() {
+        const int mine = from + lane * W;
+        page = mine < end ? page_of(P, s, mine >> (P.page_shift - 5)) : -1;
+        words = u32x2{0, 0};
+        if (page >= 0) words = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)page * P.n_kv + kv) * 2);
+    };
+    const auto tile_at = [&](int k) {
+        const int pg = k < 64 ? __builtin_amdgcn_readlane(page, k & 63) : -1;
+        return __builtin_amdgcn_make_buffer_rsrc(tile_of(P, max(0, pg), kv, (from + k * W) & ((1 << (P.page_shift - 5)) - 1)), 0,
+                                                 pg >= 0 ? KVQ_P8_TILE_BYTES : 0, 0x00020000);
+    };
+    const auto load_k = [&](__amdgpu_buffer_rsrc_t p) {  // (2: read once)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) kc[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, c * 1024, 2));
+    };
+    const auto load_v = [&](__amdgpu_buffer_rsrc_t p) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) vc[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, 4096 + c * 1024, 2));
+    };
+    u32x4 q_mine[R];
+    if (wave < 4) {  // four channel groups of the rows, one a wavefront
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int rest = block * RB + 16 * r + n - row_i[r] * rows_per_token;
+            const int h = A.maps == 2 ? rest >> 1 : rest, map = A.maps == 2 ? rest & 1 : 0;
+            q_mine[r] = u32x4{0, 0, 0, 0};
+            if (row_i[r] < seq.rows && (A.maps == 1 || (wave >> 1) == map)) {
+                q_mine[r] = *reinterpret_cast<const u32x4*>(A.q + (seq.row0 + row_i[r]) * A.q_rs + (int64_t)(kv * A.gqa + h) * A.q_hs + 32 * wave + 8 * j);
+                q_mine[r] ^= A.flip;
+            }
+        }
+    }
+    describe();
+    load_k(tile_at(0));
+    load_v(tile_at(0));
+    if (wave < 4)
+#pragma unroll
+        for (int r = 0; r < R; ++r) lds_q[r][wave][lane] = q_mine[r];
+    __syncthreads();
+
     State<R> st;
     st.clear();
-    for (int from = t0 + wave; from < end; from += 64 * W) {
-        // the pages and scale words of the wavefront's next 64 tiles, one a lane
-        const int mine = from + lane * W;
-        const int page = mine < end ? page_of(P, s, mine >> (P.page_shift - 5)) : -1;
-        u32x2 words = {0, 0};
-        if (page >= 0) words = *reinterpret_cast<const u32x2*>(P.words + ((int64_t)page * P.n_kv + kv) * 2);
-        const int todo = min(64, (end - from + W - 1) / W);
-        u32x4 kc[4], vc[4];
-        const auto at = [&](int k) {
-            const int pg = max(0, __builtin_amdgcn_readlane(page, k));
-            return tile_of(P, pg, kv, (from + k * W) & ((1 << (P.page_shift - 5)) - 1)) + lane * 16;
-        };
-        const auto load_k = [&](const uint8_t* p) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) kc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + c * 1024));
-        };
-        const auto load_v = [&](const uint8_t* p) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) vc[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4096 + c * 1024));
-        };
-        load_k(at(0));
-        load_v(at(0));
+    while (from < end) {
+        const int todo = min(64, (int)((uint32_t)(end - from + W - 1) / W));
         for (int k = 0; k < todo; ++k) {
-            const uint8_t* const next = at(min(k + 1, todo - 1));
+            const __amdgpu_buffer_rsrc_t next = tile_at(k + 1);
             const int kw = __builtin_amdgcn_readlane(words[0], k), vw = __builtin_amdgcn_readlane(words[1], k);
             const bool there = __builtin_amdgcn_readlane(page, k) >= 0;
             const int tok = (from + k * W) * 32;
@@ -318,6 +335,12 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
                 }
             }
             load_v(next);
+        }
+        from += 64 * W;
+        if (from < end) {
+            describe();
+            load_k(tile_at(0));
+            load_v(tile_at(0));
         }
     }
 
