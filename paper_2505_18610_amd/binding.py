@@ -220,6 +220,10 @@ def _is_fp32(out):
     return 1 if out.dtype == torch.float32 else 0
 
 
+def _torch():
+    return sys.modules["torch"]
+
+
 def _is_int32(t):
     torch = sys.modules["torch"]
     return t.dtype in (torch.int32, torch.uint32) and t.is_cuda
@@ -305,19 +309,19 @@ class KvqPaged8Batch:
         assert pages <= 1 or table.stride(1) == 1
         assert row_begin is None or (_is_int32(row_begin) and row_begin.shape == (n + 1,) and row_begin.is_contiguous())
         self.table, self.lengths, self.row_begin = table, lengths, row_begin
-        self._c = _Paged8Batch(table.data_ptr(), lengths.data_ptr(), None if row_begin is None else row_begin.data_ptr(),
-                               pages if n <= 1 else table.stride(0), n, pages, 0, max_rows)
+        self.max_rows = max_rows
+        self._fixed = (table.data_ptr(), lengths.data_ptr(), None if row_begin is None else row_begin.data_ptr(),
+                       pages if n <= 1 else table.stride(0), n, pages)
 
     def _of(self, n_rows):
-        self._c.n_rows = n_rows
-        return C.byref(self._c)
+        return C.byref(_Paged8Batch(*self._fixed, n_rows, self.max_rows))  # (a structure of the call's own: threads may share a batch)
 
 
 def _paged8_rows(t, rows, heads):
-    """A packed tensor [rows, heads, 128] (a dimension of one element may carry any stride)."""
+    """A packed tensor [rows, heads, 128] on a device (a dimension of one element may carry any stride)."""
     n, h, d = t.shape
     row, head, channel = t.stride()
-    assert n == rows and h == heads and d == 128 and channel == 1
+    assert n == rows and h == heads and d == 128 and channel == 1 and t.is_cuda
     return C.byref(_Paged8Rows(t.data_ptr(), 128 if n <= 1 else row, 128 if h == 1 else head))
 
 
@@ -334,50 +338,52 @@ class KvqPaged8:
         self._c = _Paged8(codes.data_ptr(), words.data_ptr(), pages, kv, 32 * tiles)
         self._ref = C.byref(self._c)
 
-    @staticmethod
-    def _check(st, where):
-        if st != KVQ_OK:
-            raise KvqError(st, where)
-
     def kvq_paged8_append(self, batch, k, v, cos_sin=None, stream=None):
         """k, v: fp16 device tensors [rows, n_kv_heads, 128] of any strides whose channels follow one another; cos_sin: fp32 device tensor
         [rows, 128] (cos 64 | sin 64 of channel pairs i, i + 64) or [rows, 64] (cos 32 | sin 32 of pairs i, i + 32 of both halves), or
         None for keys that are rotated already."""
-        n, pair = k.shape[0], 0
-        assert _half(k, v)
+        n, pair, kv = k.shape[0], 0, self.n_kv_heads
+        assert k.dtype == v.dtype == _torch().float16
         if cos_sin is not None:
-            pair = cos_sin.shape[1] // 2
-            assert cos_sin.shape in ((n, 128), (n, 64)) and _is_fp32(cos_sin)
-        self._check(self.lib.kvq_paged8_append(self._ref, batch._of(n), _paged8_rows(k, n, self.n_kv_heads), _paged8_rows(v, n, self.n_kv_heads),
-                                               _ptr(cos_sin), pair, _stream(stream)), "kvq_paged8_append")
+            rows, angles = cos_sin.shape
+            assert rows == n and angles in (128, 64) and _is_fp32(cos_sin)
+            pair = angles // 2
+        st = self.lib.kvq_paged8_append(self._ref, batch._of(n), _paged8_rows(k, n, kv), _paged8_rows(v, n, kv), _ptr(cos_sin), pair, _stream(stream))
+        if st:
+            raise KvqError(st, "kvq_paged8_append")
 
     def kvq_paged8_read(self, batch, k_out, v_out, stream=None):
         """The rows' tokens into k_out, v_out: fp16 or fp32 device tensors [rows, n_kv_heads, 128]."""
         n, kv = k_out.shape[0], self.n_kv_heads
-        assert k_out.dtype == v_out.dtype and v_out.is_cuda
-        self._check(self.lib.kvq_paged8_read(self._ref, batch._of(n), _paged8_rows(k_out, n, kv), _paged8_rows(v_out, n, kv), _is_fp32(k_out),
-                                             _stream(stream)), "kvq_paged8_read")
+        assert k_out.dtype == v_out.dtype
+        st = self.lib.kvq_paged8_read(self._ref, batch._of(n), _paged8_rows(k_out, n, kv), _paged8_rows(v_out, n, kv), _is_fp32(k_out), _stream(stream))
+        if st:
+            raise KvqError(st, "kvq_paged8_read")
 
     def kvq_paged8_attention(self, batch, q, out, softmax_scale=0.0, lse=None, workspace=None, stream=None):
         """q: fp16 device tensor [rows, n_q_heads, 128], out: fp16 or fp32 like it, of any strides; lse: fp32 device tensor
         [n_q_heads, rows] or None; workspace: uint8 device tensor of kvq_paged8_workspace_bytes, zeros before its first use."""
         n, heads, _ = q.shape
-        assert _half(q) and (lse is None or (tuple(lse.shape) == (heads, n) and _is_fp32(lse))) and (workspace is None or workspace.is_cuda)
-        self._check(self.lib.kvq_paged8_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _paged8_rows(out, n, heads), heads,
-                                                  _is_fp32(out), softmax_scale, _ptr(lse), _ptr(workspace),
-                                                  0 if workspace is None else workspace.numel(), _stream(stream)), "kvq_paged8_attention")
+        assert q.dtype == _torch().float16 and (lse is None or (tuple(lse.shape) == (heads, n) and _is_fp32(lse)))
+        assert workspace is None or workspace.is_cuda
+        st = self.lib.kvq_paged8_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _paged8_rows(out, n, heads), heads, _is_fp32(out),
+                                           softmax_scale, _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream))
+        if st:
+            raise KvqError(st, "kvq_paged8_attention")
 
     def kvq_paged8_diff_attention(self, batch, q, lam, out, norm_weight=None, norm_eps=1e-5, out_scale=1.0, softmax_scale=0.0, workspace=None,
                                   stream=None):
         """Differential attention; q, out and workspace as in kvq_paged8_attention.  lam: fp32 device tensor [n_q_heads], norm_weight:
         fp32 device tensor [128] or None."""
         n, heads, _ = q.shape
-        assert _half(q) and tuple(lam.shape) == (heads,) and _is_fp32(lam) and (workspace is None or workspace.is_cuda)
+        assert q.dtype == _torch().float16 and tuple(lam.shape) == (heads,) and _is_fp32(lam)
+        assert workspace is None or workspace.is_cuda
         assert norm_weight is None or (tuple(norm_weight.shape) == (128,) and _is_fp32(norm_weight))
-        self._check(self.lib.kvq_paged8_diff_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _ptr(lam), _paged8_rows(out, n, heads),
-                                                       heads, _is_fp32(out), softmax_scale, _ptr(norm_weight), norm_eps, out_scale,
-                                                       _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
-                    "kvq_paged8_diff_attention")
+        st = self.lib.kvq_paged8_diff_attention(self._ref, batch._of(n), _paged8_rows(q, n, heads), _ptr(lam), _paged8_rows(out, n, heads), heads,
+                                                _is_fp32(out), softmax_scale, _ptr(norm_weight), norm_eps, out_scale, _ptr(workspace),
+                                                0 if workspace is None else workspace.nbytes, _stream(stream))
+        if st:
+            raise KvqError(st, "kvq_paged8_diff_attention")
 
 
 def kvq_paged8_workspace_bytes(cache, batch, n_q_heads, n_rows, two_maps=False) -> int:

@@ -144,6 +144,7 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
         for (int i = 0; i < 8; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = (float)w[i][e];
+            if (!__any(is_new(8 * j + i))) continue;  // (of a decode step one of eight)
             if (KEYS && A.pair) {
                 float c[8] = {}, s[8] = {};
                 if (is_new(8 * j + i)) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2505_18610_amd as kq
-from paged8_plain import D, Plain, attention, check, value
+from paged8_plain import D, Plain, attention, check
 
 pytestmark = pytest.mark.gpu
 
@@ -240,6 +240,90 @@ def test_rows(rows, gqa, diff):
     attend(c, 2 * gqa, rows, lengths, diff=diff, norm=gqa != 4)
 
 
+def in_blocks(kv, gqa, rows, lengths, diff):
+    """Whether sequences of more than 64 rows x heads are taken in blocks of 256 (calls of more than 512 units of 32 rows, or of 40,000 tiles of
+    units): asked so that the tests below are of that kernel."""
+    units = [-(-r * gqa * (2 if diff else 1) // 32) * kv for r in rows]
+    return sum(units) > 512 or sum(u * max(1, -(-n // 32)) for u, n in zip(units, lengths)) > 40000
+
+
+@pytest.mark.parametrize("diff", [False, True])
+@pytest.mark.parametrize("page,kv,gqa,rows,lengths", [
+    (64, 4, 4, [400, 257, 70, 300], [400, 900, 257, 513]), (32, 3, 7, [300, 1, 257, 12], [301, 64, 270, 1000]), (256, 8, 1, [700, 900, 65, 64], [3000, 900, 65, 640]),
+    (128, 2, 16, [180, 160, 33], [180, 1000, 290]), (64, 5, 5, [650], [650])])
+def test_chunks(page, kv, gqa, rows, lengths, diff):
+    """Blocks of 256 rows beside sequences of few, whole prompts and chunks behind cached tokens; blocks that end inside a token's heads."""
+    if not in_blocks(kv, gqa, rows, lengths, diff):
+        rows, lengths = rows * 3, lengths * 3
+    assert in_blocks(kv, gqa, rows, lengths, diff)
+    c = Pair(kv, page, len(rows), max(lengths) // page + 1, seed=30).filled(lengths)
+    attend(c, kv * gqa, rows, lengths, diff=diff, norm=gqa != 4, out=torch.float32 if gqa == 7 else torch.float16, scale=-0.1 if gqa == 5 else 0.0)
+
+
+@pytest.mark.parametrize("kv,gqa,rows,lengths", [
+    (2, 4, [1, 1, 1], [33, 700, 1025]), (1, 2, [1, 4], [9001, 4097]), (1, 8, [8], [30000]), (2, 4, [40, 1], [900, 50]),   # pieces of few rows
+    (4, 4, [500, 300, 300], [500, 1100, 300]), (1, 16, [80], [36000])])                                                    # blocks of 256
+def test_every_tile_counts(kv, gqa, rows, lengths):
+    """Equal weights, and values that are zero but for one channel in each tile: a tile that is lost or counted twice is a part of its channel that
+    no bound lets pass."""
+    c = Pair(kv, 64, len(rows), max(lengths) // 64 + 1, seed=34)
+    k, v, _ = c.new(lengths)
+    tile = torch.cat([torch.arange(n) // 32 for n in lengths])
+    v = torch.where(torch.arange(D)[None, None] == (tile % D)[:, None, None], torch.full_like(v, 96.0), torch.zeros_like(v))
+    c.append(lengths, lengths, k, v)
+    attend(c, kv * gqa, rows, lengths, spread=0.0)
+    attend(c, kv * gqa, rows, lengths, spread=0.0, diff=True, norm=False)
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_chunk_in_many_pieces(diff):
+    """One block's rows over many tiles, which several workgroups share; and a block of two pieces."""
+    for kv, gqa, rows, lengths in ((1, 16, [70], [38500]), (2, 16, [90, 17], [14000, 9000])):
+        assert in_blocks(kv, gqa, rows, lengths, diff)
+        c = Pair(kv, 128, len(rows), max(lengths) // 128 + 1, seed=31).filled(lengths)
+        attend(c, kv * gqa, rows, lengths, diff=diff)
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_chunks_of_what_does_not_exist(diff):
+    """Rows that see nothing, pages that are not there, NaN among keys and values, lengths beyond the table: in blocks of 256 rows."""
+    rows, lengths = [300, 280, 310, 90, 290], [150, 280, 0, 1 << 30, 290]
+    have = [150, 280, 0, 320, 290]
+    c = Pair(4, 32, 5, 10, seed=32)
+    k, v, _ = c.new(have)
+    k[10, 0, 3], v[149, 1, 77], v[150 + 100, 2, 5], v[150 + 279, 3, 0], k[150 + 200, 1, 1] = math.nan, math.inf, math.nan, math.nan, math.inf
+    c.append(have, have, k, v)
+    table = c.table.clone()
+    table[3, 2], table[3, 9], table[4, 0] = -1, 1 << 20, -7
+    assert in_blocks(4, 4, rows, [150, 280, 0, 320, 290], diff)
+    attend(c, 16, rows, lengths, diff=diff, table=table)
+    attend(c, 16, rows, lengths, diff=diff, table=table, eps=0.0, norm=True, max_rows=310)
+
+
+def test_chunk_captured():
+    """A captured call whose rows and lengths change between replays, from few rows to blocks of 256, over one workspace."""
+    c = Pair(4, 64, 4, 12, seed=33).filled([600, 700, 64, 300])
+    g = torch.Generator().manual_seed(5)
+    n, heads = 1400, 16
+    q = torch.randn(n, heads, D, generator=g).half()
+    q_dev, out = q.cuda(), torch.empty(n, heads, D, device="cuda").half()
+    begin, lengths = ints([0, 1, 2, 3, 4]), ints([1, 1, 1, 1])
+    batch = kq.KvqPaged8Batch(c.table.cuda(), lengths, begin, max_rows=700)
+    ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, heads, n), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.kvq_paged8_attention(batch, q_dev, out, workspace=ws, stream=torch.cuda.current_stream())
+    for rows, held in (([1, 1, 1, 1], [600, 700, 64, 300]), ([600, 300, 64, 300], [600, 700, 64, 300]), ([0, 500, 20, 100], [5, 500, 64, 299]),
+                       ([600, 300, 64, 300], [600, 700, 64, 300]), ([2, 0, 0, 7], [33, 700, 64, 300])):
+        begin.copy_(ints(begins(rows)))
+        lengths.copy_(ints(held))
+        out.fill_(777.0)
+        graph.replay()
+        want, tol, _, _ = attention(c.plain, c.table, held, begins(rows), q)
+        check(out[:sum(rows)], want[:sum(rows)], tol[:sum(rows)])
+        assert bool((out[sum(rows):] == 777.0).all())
+
+
 @pytest.mark.parametrize("diff", [False, True])
 def test_rows_that_see_nothing(diff):
     """More rows than tokens, no tokens, lengths below zero: zeros, also behind a norm without eps."""
@@ -325,9 +409,9 @@ def test_strides_of_queries_and_outputs():
     q = torch.randn(2, 8, D, generator=g).half()
     batch = c.batch([1, 1], [100, 50])
     ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, 8, 2), dtype=torch.uint8, device="cuda")
-    plain, other = torch.empty(2, 8, D, device="cuda").half(), torch.full((9, 4, 160), 7.0, device="cuda").half()
+    plain = torch.empty(2, 8, D, device="cuda").half()
     c.cache.kvq_paged8_attention(batch, q.cuda(), plain, workspace=ws)
-    sliced = other.as_strided((2, 8, D), (8, 160), 0) if False else torch.full((8, 2, 160), 7.0, device="cuda").half().transpose(0, 1)[:, :, 16:144]
+    sliced = torch.full((8, 2, 160), 7.0, device="cuda").half().transpose(0, 1)[:, :, 16:144]
     wide = torch.zeros(2, 24, D, device="cuda").half()
     wide[:, 8:16] = q.cuda()
     c.cache.kvq_paged8_attention(batch, wide[:, 8:16], sliced, workspace=ws)
