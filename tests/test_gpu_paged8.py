@@ -395,6 +395,43 @@ def test_long_and_short_together():
     attend(c, 8, [9] + [1] * 79 + [2], lengths)
 
 
+@pytest.mark.parametrize("diff", [False, True])
+@pytest.mark.parametrize("n,kv,gqa,rows,most", [(150, 4, 2, 1, 300), (90, 8, 4, 4, 200), (1100, 1, 4, 1, 40), (70, 8, 16, 1, 33)])
+def test_many_short_sequences(n, kv, gqa, rows, most, diff):
+    """More units than workgroups that the device takes at a time; more sequences than a wavefront has lanes."""
+    lengths = [1 + (37 * s) % most for s in range(n)]
+    counts = [min(rows, x) if s % 7 else 0 for s, x in enumerate(lengths)]
+    c = Pair(kv, 32, n, most // 32 + 1, seed=35).filled(lengths)
+    attend(c, kv * gqa, counts, lengths, diff=diff, lse=rows == 1)
+
+
+def test_chunks_of_many_sequences():
+    """Blocks of 256 rows of more sequences than a wavefront has lanes, beside single tokens."""
+    rows = [1 if s % 3 else 70 + s for s in range(75)]
+    lengths = [r + 5 * s % 50 for s, r in enumerate(rows)]
+    assert in_blocks(2, 4, rows, lengths, False)
+    c = Pair(2, 64, 75, 4, seed=36).filled(lengths)
+    attend(c, 8, rows, lengths)
+    attend(c, 8, rows, lengths, diff=True)
+
+
+def test_queries_that_are_not_finite():
+    """NaN in a query is its row's own affair, and so is an infinity."""
+    for rows, lengths, kv in (([1, 1], [500, 40], 2), ([600, 600], [700, 600], 4)):
+        c = Pair(kv, 64, 2, 12, seed=37).filled(lengths)
+        n = sum(rows)
+        q = torch.randn(n, 4 * kv, D, generator=torch.Generator().manual_seed(6)).half().cuda()
+        batch = c.batch(rows, lengths)
+        ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, 4 * kv, n), dtype=torch.uint8, device="cuda")
+        want, got = torch.empty_like(q), torch.empty_like(q)
+        c.cache.kvq_paged8_attention(batch, q, want, workspace=ws)
+        q[1, 2, 7], q[0, 3, 100] = math.nan, math.inf
+        c.cache.kvq_paged8_attention(batch, q, got, workspace=ws)
+        assert bool(torch.isnan(got[1, 2]).all()) and bool(torch.isnan(got[0, 3]).any())
+        want[1, 2], want[0, 3] = got[1, 2], got[0, 3]
+        assert torch.equal(torch.nan_to_num(want, 5.0), torch.nan_to_num(got, 5.0))
+
+
 def test_shared_pages():
     """Two sequences over the same pages, which differ in length; the order of pages is the table's."""
     c = Pair(2, 32, 3, 5, seed=20).filled([160, 100, 20])
