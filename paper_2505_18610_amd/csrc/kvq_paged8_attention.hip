@@ -22,20 +22,24 @@ using kvq_flash::reference_of;
 using kvq_flash::softmax_group;
 using kvq_flash::to_half8;
 
-#define KVQ_P8_GROUPS 512       // pieces of few units that a launch is cut into, at most
+#define KVQ_P8_GROUPS 512        // pieces that units are cut into where they are few: two workgroups a compute unit (384 and 768 pieces: 4 x 32,768 tokens
+                                 // 53.3 and 55.7 us, 512 49.3)
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
-#define KVQ_P8_LEAST_SHARE 8    // tiles of a piece, at least: one for each wavefront
-#define KVQ_P8_WHOLE 16         // tiles of units that are not cut: a second round takes 0.6 us, joining 1.7 (300 tokens 8.3 -> 7.2 us)
-#define KVQ_P8_MANY_SHARE 24    // tiles of a piece where units are many, at least (264 units of 22 to 32 tiles 19.4 -> 15.9 us)
-#define KVQ_P8_LEAST_CHUNK 16   // of a workgroup with a chunk
-#define KVQ_P8_CHUNK_ROOT 2.f   // of a workgroup with a chunk by the root of the longest unit's, at least
-#define KVQ_P8_CHUNK_PIECES 64  // of a unit
-#define KVQ_P8_CHUNK_GROUPS 256 // workgroups of a launch over chunks, at most: one a compute unit
-#define KVQ_P8_MAP_BYTES 17408  // partial results of a wavefront with a chunk and one map
+#define KVQ_P8_LEAST_SHARE 8     // tiles of a piece, at least: one for each wavefront
+#define KVQ_P8_WHOLE 16          // tiles of units that are not cut: a second round takes 0.6 us, joining 1.7 (300 tokens 8.3 -> 7.2 us)
+#define KVQ_P8_MANY_SHARE 24     // tiles of a piece where units are many, at least (264 units of 22 to 32 tiles 19.4 -> 15.9 us)
+#define KVQ_P8_MOST_PIECES 128   // of a unit
+#define KVQ_P8_ROOT 0.7f         // tiles of a piece by the root of the longest unit's, at least: more pieces take longer to join than they save
+                                 // (0.5, 0.9, 2: 4,001 tokens 8.6, 9.1, 10.2 us; 18,547 with two maps 24.0, 19.7, 20.7)
+#define KVQ_P8_CHUNK_GROUPS 256  // workgroups of a launch over chunks, at most: one a compute unit
+#define KVQ_P8_LEAST_CHUNK 16    // tiles of a workgroup with a chunk, at least,
+#define KVQ_P8_CHUNK_ROOT 2.f    // and by the root of the longest unit's (1, 2, 4: 506 rows x 7 heads over 36,423 tokens 126, 122, 178 us)
+#define KVQ_P8_CHUNK_PIECES 64   // of a unit
+#define KVQ_P8_MAP_BYTES 17408   // partial results of a wavefront with a chunk and one map
+// Calls in which chunks are taken like few rows: units of 32 rows and their tiles, at most (64 rows x 32 heads over 4,000 tokens 55 -> 34 us, 92 rows
+// with two maps over 9,651 99 -> 42; with twice as many tiles sixteen sequences of 40 rows 95 -> 126).
 #define KVQ_P8_SMALL_UNITS 512
-#define KVQ_P8_SMALL_TILES 40000 // of all units
-#define KVQ_P8_MOST_PIECES 128  // of a unit
-#define KVQ_P8_ROOT 0.7f        // tiles of a piece by the root of the longest unit's, at least
+#define KVQ_P8_SMALL_TILES 40000
 
 struct AttnArgs {
     KvqP8 p;
@@ -177,7 +181,14 @@ struct Cuts {
 };
 
 // A piece a workgroup; the pieces of a unit are joined by the last of them to arrive.  Eight wavefronts take a piece's tiles in turn, every one
-// from memory straight into operand registers: nothing but the queries is shared before the end.
+// from memory straight into operand registers: nothing but the queries is shared before the end.  S^T = K q^T and O^T += V^T P^T with the rows
+// in the N dimension, the reference and sums of kvq_flash.h; a scale is a power of two, K's goes to the scores, V's into the widening.
+// Memory bounds it: a unit's codes are read once, 16 wavefronts of a compute unit have 128 KB on their way (R = 1, at most 128 registers, which is why the
+// queries lie in LDS: 67.0 -> 54.8 us).  4 x 32,768 tokens x 40 heads 49.4 us = 5.4 TB/s, as much as a copy moves; two maps over eight sequences of up
+// to 16,384 tokens 42 us = 5.0; 48 sequences of 41 to 30,000 tokens 49 us = 4.8 (107 with equal shares of all tiles over the units, as short
+// units then waited for one another in one workgroup).  A short call is a chain of trips: 1,001 tokens x 8 heads 8.4 us.
+// The hand-over: partial results go out with device-scope stores (sc1), a wait and a barrier stand before the arrival counter, the last to arrive reads
+// them with device-scope loads and leaves the counter at zero for the next call.
 template <int R>
 __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(const AttnArgs A) {
     constexpr int RB = 16 * R, W = 8;
@@ -493,7 +504,8 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 // ---- Sequences with many rows: chunks of prompts
 
 // Where the work of the units lies on one line that workgroups take equal shares of.  A block's length on it is its tiles, by the tokens that its last
-// row sees, and kLead for what a block costs beside them; blocks of a KV head lie one after the other, KV heads, sequences.
+// row sees, and kLead for what a block costs beside them (12 of them take as long as a block's start and end: a prompt of 8,192 tokens, whose first
+// blocks have few, 902 us with 4, 832 with 12, 859 with 28); blocks of a KV head lie one after the other, KV heads, sequences.
 struct Line {
     int rows, blocks;     // flat rows, blocks
     int length;           // of all blocks of one KV head
@@ -591,6 +603,11 @@ __device__ inline void softmax_tiles(Map& st, const float16v (&s)[NT], const flo
 // either on a SIMD, take turns: while one has its products (scores of a stage of NT tiles, and the probabilities of the stage before times its values),
 // the other has its softmax, widens the codes of a stage two further on into LDS and loads the next.  A barrier stands between the turns.  A stage is
 // written in the turns 2 s - 3 and 2 s - 2, its keys are read in 2 s and 2 s + 1, its values in 2 s + 2 and 2 s + 3: four buffers.
+// Products and vector instructions bound it, which overlap by half at best (16,000 products of one wavefront a SIMD 298 us, 128,000 multiply-adds of another
+// 316, both 439): matrix cores 41 % busy, vector ALUs 36 %.  So what counts is few instructions: codes are widened once a workgroup of 256 rows, products
+// are of 32 x 32 (half the instructions and operand reads of 16 x 16), a lane has one row's statistics, the sum is a dot product of the rounded pairs.
+// Two chunks of 1,024 behind 16,000 tokens x 40 heads 690 us = 942 TFLOP/s (770 with four wavefronts of 32 rows each and products of 16 x 16, two workgroups
+// a compute unit), a prompt of 8,192 x 28 heads with two maps 855 us = 844 TFLOP/s (1,110).
 template <int MAPS>
 __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
