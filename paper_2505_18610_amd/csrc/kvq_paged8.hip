@@ -119,7 +119,7 @@ __device__ inline float partner(float x, int m, bool eight) {
 // 190 us = 4.6 TB/s (248 with keys loaded in the tile's order, 64 bytes of a row by four lanes, and values scattered into the tile).  95 registers:
 // with more than 96 a SIMD holds four wavefronts instead of five, 210 us.
 template <bool KEYS>
-__device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv, uint8_t* lds, float* wave_max) {
+__device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv, uint8_t* lds, uint32_t* wave_max) {
     const KvqP8& P = A.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, n = lane & 15;
     const int tok0 = wave * 32;  // of the page
@@ -176,11 +176,17 @@ __device__ inline void append_page(const AppendArgs& A, const Touched& T, int kv
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
-    if (lane == 0) wave_max[wave] = largest;
-    const int any_nan = __syncthreads_or(nan ? 1 : 0);
+    const bool wave_nan = __any(nan);
+    if (lane == 0) wave_max[wave] = __float_as_uint(largest) | (wave_nan ? 1u << 31 : 0u);  // (the sign: whether any is NaN)
+    __syncthreads();
     const int waves = blockDim.x >> 6;
+    uint32_t any_nan = 0;
     largest = 0.f;
-    for (int w = 0; w < waves; ++w) largest = fmaxf(largest, wave_max[w]);
+    for (int w = 0; w < waves; ++w) {
+        const uint32_t x = wave_max[w];
+        largest = fmaxf(largest, __uint_as_float(x & 0x7fffffffu));
+        any_nan |= x >> 31;
+    }
     int e = exponent_for(largest);
     const int e_old = exponent_of(old_word);
     if (T.begin > 0) e = max(e, e_old);
@@ -251,7 +257,7 @@ __device__ inline Job job_of(int n_kv) {
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void kvq_paged8_append_kernel(const AppendArgs A) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES * 4096];
-    __shared__ float wave_max[WAVES];
+    __shared__ uint32_t wave_max[WAVES];
     Touched T;
     const Job job = job_of(A.p.n_kv);
     if (!touched_page(A.p, A.per_seq, job.page, T)) return;

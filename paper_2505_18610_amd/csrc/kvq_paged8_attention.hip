@@ -1022,6 +1022,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                     }
                 }
             }
+            if (mine && unit_end < range_end) __syncthreads();  // the next block's codes come where the references lie
         }
         if (mine) {
             float inv[MAPS], by;

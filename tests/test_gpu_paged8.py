@@ -200,14 +200,15 @@ def attend(c, q_heads, rows, lengths, out=torch.float16, scale=0.0, diff=False, 
     need = kq.kvq_paged8_workspace_bytes(c.cache, batch, q_heads, n, diff)
     assert need > 0
     ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    each = []
     for _ in range(2):  # the second time over the workspace that the first has left
         if diff:
             c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, norm_weight=weight.cuda() if norm else None, norm_eps=eps,
                                               out_scale=out_scale, softmax_scale=scale, workspace=ws)
         else:
             c.cache.kvq_paged8_attention(batch, q.cuda(), got, softmax_scale=scale, lse=logs, workspace=ws)
-        first = got.clone()
-    assert torch.equal(torch.nan_to_num(first, 5.0), torch.nan_to_num(got, 5.0))
+        each.append(got.clone())
+    assert torch.equal(*(torch.nan_to_num(x, 5.0) for x in each))
     want, tol, wl, tl = attention(c.plain, c.table if table is None else table, lengths, begins(rows), q, scale, lam if diff else None,
                                   weight if norm else None, eps, out_scale, 2.0 ** -11 if out == torch.float16 else 2.0 ** -24)
     m = sum(rows)
@@ -282,6 +283,27 @@ def test_chunk_in_many_pieces(diff):
         assert in_blocks(kv, gqa, rows, lengths, diff)
         c = Pair(kv, 128, len(rows), max(lengths) // 128 + 1, seed=31).filled(lengths)
         attend(c, kv * gqa, rows, lengths, diff=diff)
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_cut_blocks_of_few_rows(diff):
+    """Blocks most of whose wavefronts have no rows, each cut into pieces of several workgroups, which go on to another block after a piece: equal
+    bits, whoever joins the pieces."""
+    rows, lengths = [17, 20, 24, 19, 30, 17, 22, 17, 18, 40], [3000 + 41 * s for s in range(10)]
+    c = Pair(8, 64, 10, 54, seed=38).filled(lengths)
+    rows = rows if diff else [2 * r for r in rows]
+    assert in_blocks(8, 4, rows, lengths, diff)
+    attend(c, 32, rows, lengths, diff=diff)
+    batch, n = c.batch(rows, lengths), sum(rows)
+    q, lam = torch.randn(n, 32, D, generator=torch.Generator().manual_seed(39)).half().cuda(), torch.ones(32, device="cuda")
+    ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, 32, n, diff), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty_like(q) for _ in range(20)]
+    for out in outs:
+        if diff:
+            c.cache.kvq_paged8_diff_attention(batch, q, lam, out, workspace=ws)
+        else:
+            c.cache.kvq_paged8_attention(batch, q, out, workspace=ws)
+    assert all(torch.equal(outs[0], out) for out in outs)
 
 
 @pytest.mark.parametrize("diff", [False, True])
