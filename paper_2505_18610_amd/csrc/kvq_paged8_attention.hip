@@ -32,9 +32,7 @@ using kvq_flash::to_half8;
 #define KVQ_P8_ROOT 0.7f         // tiles of a piece by the root of the longest unit's, at least: more pieces take longer to join than they save
                                  // (0.5, 0.9, 2: 4,001 tokens 8.6, 9.1, 10.2 us; 18,547 with two maps 24.0, 19.7, 20.7)
 #define KVQ_P8_CHUNK_GROUPS 256  // workgroups of a launch over chunks, at most: one a compute unit
-#define KVQ_P8_LEAST_CHUNK 16    // tiles of a workgroup with a chunk, at least,
-#define KVQ_P8_CHUNK_ROOT 2.f    // and by the root of the longest unit's (1, 2, 4: 506 rows x 7 heads over 36,423 tokens 126, 122, 178 us)
-#define KVQ_P8_CHUNK_PIECES 64   // of a unit
+#define KVQ_P8_LEAST_CHUNK 16    // tiles of a workgroup with a chunk, at least
 #define KVQ_P8_MAP_BYTES 17408   // partial results of a wavefront with a chunk and one map
 // Calls in which chunks are taken like few rows: units of 32 rows and their tiles, at most (64 rows x 32 heads over 4,000 tokens 55 -> 34 us, 92 rows
 // with two maps over 9,651 99 -> 42; with twice as many tiles sixteen sequences of 40 rows 95 -> 126).
@@ -613,7 +611,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * STAGE];
     __shared__ u32x4 lds_q[MAPS == 2 ? 8 : 1][4][64];  // two maps: the second's queries, for which there are no registers
-    __shared__ int lds_last;
+    __shared__ int lds_last[2];
     const KvqP8& P = A.p;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_page = P.page_shift - 5;
@@ -626,19 +624,10 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         if (small_call(units.total, tiles.total)) return;
     }
     const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.few_rows); };
-    int longest = 0;
-    const auto count = [&](int s) {
-        const Seq q = seq_of(P, s);
-        const Line x = line(q);
-        if (x.blocks) longest = max(longest, (q.tokens >> 5) + Line::kLead);
-        return x.length * P.n_kv;
-    };
+    const auto count = [&](int s) { return line(seq_of(P, s)).length * P.n_kv; };
     const Census<decltype(count)> census(count, P.n_seqs);
     if (census.total == 0) return;
-    // (joining a piece takes as long as several tiles: with n pieces of a unit of t tiles t / n + 4 n is least about there)
-    const int groups = gridDim.x;
-    const auto least_share = [](int t) { return max((int)(KVQ_P8_CHUNK_ROOT * sqrtf((float)t)), (t + 16) / (KVQ_P8_CHUNK_PIECES - 4) + 1); };
-    const int share = max(max(KVQ_P8_LEAST_CHUNK, (census.total + groups - 1) / groups), least_share(wave_max(longest)));
+    const int groups = gridDim.x, share = max(KVQ_P8_LEAST_CHUNK, (census.total + groups - 1) / groups);
     // neighbours on the line go to one XCD, whose L2 then holds the keys and values that they have in common
     const int wg = groups % 8 == 0 ? (blockIdx.x & 7) * (groups >> 3) + (blockIdx.x >> 3) : blockIdx.x;
     int pos = wg * share;
@@ -927,104 +916,77 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             }
         }
 
-        const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
-        const Row row = row_of(n);
-        // ---- the pieces of a unit that lies in several workgroups' shares, joined by the last of them in the order of the line
-        const int w0 = unit / share, w1 = (unit + length - 1) / share, pieces = w1 - w0 + 1;
+        // ---- the pieces of a unit that lies in several workgroups' shares, joined two by two as a tree over their order on the line: of two neighbours
+        // whoever finds the other's stored joins it to its own, in registers, and goes on to the next level.  Products are rounded before they are added,
+        // so that it does not matter who.  A pair's counter is that of the workgroup at which its second half begins, its slot that of its first.
+        const int w0 = unit / share, pieces = (unit + length - 1) / share - w0 + 1;
         bool mine = true;
-        if (pieces > 1) {
-            constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP;
+        for (int width = 1, at = wg - w0, turn = 0; mine && width < pieces; width *= 2, turn ^= 1) {
+            const int other = at ^ width, begin = min(at, other), second = max(at, other);
+            if (second >= pieces) continue;
+            constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP, FLY = MAPS == 1 ? 16 : 8;
             const bool rows_here = block * RB + wave * 32 < flat;  // whether the wavefront has any
             const auto slot = [&](int k) {
                 return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(A.part) + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * SLOT, 0, SLOT, 0x00020000);
             };
-            const int own_at = wave * MAPS * MAP + lane * 16;
-            uint32_t* const counter = A.counters + (int64_t)w0 * KVQ_P8_COUNTER_STRIDE;
-            // Whoever finds that all others have stored theirs joins them; of two pieces that one does not store its own.  (Most often it is the piece that
-            // begins the unit: it comes last in its workgroup's share, the other first in its.)
-            if (threadIdx.x == 0)
-                lds_last = pieces == 2 && __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
+            const int own_at = wave * MAPS * MAP + (opaque(threadIdx.x) & 63) * 16;
+            uint32_t* const counter = A.counters + (int64_t)(w0 + second) * KVQ_P8_COUNTER_STRIDE;
+            if (threadIdx.x == 0) lds_last[turn] = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
             __syncthreads();
-            mine = lds_last != 0;
+            mine = lds_last[turn] != 0;
             if (!mine) {
-                const __amdgpu_buffer_rsrc_t to = slot(wg - w0);
+                const __amdgpu_buffer_rsrc_t to = slot(at);
                 if (rows_here)
 #pragma unroll
                 for (int m = 0; m < MAPS; ++m) {
-                    const int at = own_at + m * MAP;
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const float16v& o = st[m].o[v >> 2];
                         const float4v x = {o[4 * (v & 3)], o[4 * (v & 3) + 1], o[4 * (v & 3) + 2], o[4 * (v & 3) + 3]};
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at + v * 1024, 0, 16);
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, own_at + m * MAP + v * 1024, 0, 16);
                     }
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st[m].m, st[m].l, st[m].fine, 0.f}), to, at + 16384, 0, 16);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st[m].m, st[m].l, st[m].fine, 0.f}), to, own_at + m * MAP + 16384, 0, 16);
                 }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
-                if (threadIdx.x == 0) lds_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pieces - 1u ? 1 : 0;
+                if (threadIdx.x == 0) lds_last[turn] = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
                 __syncthreads();
-                mine = lds_last != 0;
+                mine = lds_last[turn] != 0;
             }
             if (mine && threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             asm volatile("" ::: "memory");
             if (mine && rows_here) {
-                // References and sums first, the references into LDS, then the outputs, FLY loads on their way throughout.  Of two pieces one is in registers
-                // still: products are rounded before they are added, so that it does not matter which.
-                const int skip = pieces == 2 ? wg - w0 : -1;
-                float* const refs = reinterpret_cast<float*>(lds) + wave * (KVQ_P8_CHUNK_PIECES * 32) + n;
+                const __amdgpu_buffer_rsrc_t from = slot(other);
+                const auto load = [&](int i) {  // the outputs of both maps, one after the other
+                    return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, own_at + (i >> 4) * MAP + (i & 15) * 1024, 0, 16));
+                };
+                float4v ml[MAPS], x[FLY];
+#pragma unroll
+                for (int m = 0; m < MAPS; ++m) ml[m] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(from, own_at + m * MAP + 16384, 0, 16));
+#pragma unroll
+                for (int i = 0; i < FLY; ++i) x[i] = load(i);
 #pragma unroll
                 for (int m = 0; m < MAPS; ++m) {
-                    const int at = own_at + m * MAP;
-                    const float own = st[m].m;
-                    if (pieces > 2) st[m].clear();
-                    for (int k0 = 0; k0 < pieces; k0 += 8) {
-                        float4v ml[8];  // on their way together; the last piece's again behind it
+                    const float m_new = fmaxf(st[m].m, ml[m][0]), ref = reference_of(m_new);
+                    const float a = __builtin_amdgcn_exp2f(st[m].m - ref), b = __builtin_amdgcn_exp2f(ml[m][0] - ref);
+                    st[m].m = m_new;
+                    st[m].l = __fadd_rn(__fmul_rn(st[m].l, a), __fmul_rn(ml[m][1], b));
+                    st[m].fine = __fadd_rn(__fmul_rn(st[m].fine, a), __fmul_rn(ml[m][2], b));
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            ml[i] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(slot(min(k0 + i, pieces - 1)), at + 16384, 0, 16));
+                    for (int v = 0; v < 16; ++v) {
+                        const int i = m * 16 + v;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int k = k0 + i;
-                            if (k == skip || k >= pieces) continue;
-                            const float m_new = fmaxf(st[m].m, ml[i][0]), ref = reference_of(m_new);
-                            const float a = __builtin_amdgcn_exp2f(st[m].m - ref), b = __builtin_amdgcn_exp2f(ml[i][0] - ref);
-                            st[m].l = __fadd_rn(__fmul_rn(st[m].l, a), __fmul_rn(ml[i][1], b));
-                            st[m].fine = __fadd_rn(__fmul_rn(st[m].fine, a), __fmul_rn(ml[i][2], b));
-                            st[m].m = m_new;
-                            refs[k * 32] = ml[i][0];  // (both halves of the wavefront write the same)
-                        }
-                    }
-                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (read by the wavefront that has written it)
-                    __builtin_amdgcn_wave_barrier();
-                    const float ref = reference_of(st[m].m);
-                    if (pieces == 2) {
-                        const float a = __builtin_amdgcn_exp2f(own - ref);
-#pragma unroll
-                        for (int cb = 0; cb < 4; ++cb) st[m].o[cb] *= a;
-                    }
-                    const auto load = [&](int k, int v) { return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(slot(k), at + v * 1024, 0, 16)); };
-                    constexpr int FLY = MAPS == 1 ? 16 : 4;
-                    float4v x[FLY];
-                    int k = skip == 0 ? 1 : 0;
-#pragma unroll
-                    for (int v = 0; v < FLY; ++v) x[v] = load(k, v);
-                    while (k < pieces) {
-                        const int next = k + 1 == skip ? k + 2 : k + 1, from = min(next, pieces - 1);
-                        const float w = __builtin_amdgcn_exp2f(refs[k * 32] - ref);
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) st[m].o[v >> 2][4 * (v & 3) + i] = __fadd_rn(st[m].o[v >> 2][4 * (v & 3) + i], __fmul_rn(x[v % FLY][i], w));
-                            x[v % FLY] = load(v + FLY < 16 ? k : from, (v + FLY) & 15);
-                        }
-                        k = next;
+                        for (int e = 0; e < 4; ++e)
+                            st[m].o[v >> 2][4 * (v & 3) + e] = __fadd_rn(__fmul_rn(st[m].o[v >> 2][4 * (v & 3) + e], a), __fmul_rn(x[i % FLY][e], b));
+                        if (i + FLY < 16 * MAPS) x[i % FLY] = load(i + FLY);
                     }
                 }
             }
-            if (mine && unit_end < range_end) __syncthreads();  // the next block's codes come where the references lie
+            at = begin;
         }
         if (mine) {
+            const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
+            const Row row = row_of(n);
             float inv[MAPS], by;
 #pragma unroll
             for (int m = 0; m < MAPS; ++m) inv[m] = 2.f * kvq_flash::inverse_of(halves_sum(st[m].l));
