@@ -22,8 +22,9 @@ using kvq_flash::reference_of;
 using kvq_flash::softmax_group;
 using kvq_flash::to_half8;
 
-#define KVQ_P8_GROUPS 512        // pieces that units are cut into where they are few: two workgroups a compute unit (384 and 768 pieces: 4 x 32,768 tokens
-                                 // 53.3 and 55.7 us, 512 49.3)
+#define KVQ_P8_GROUPS 512        // pieces of 16 rows that units are cut into where they are few: two workgroups a compute unit (384 and 768 pieces: 4 x
+                                 // 32,768 tokens 53.3 and 55.7 us, 512 49.3).  Of 32 rows half as many, whose workgroups have a compute unit each:
+                                 // 32 sequences of 8 rows x 32 heads over 2,000 tokens 27.4 us, with 384 39.0, with 512 40.6.
 #define KVQ_P8_COUNTER_STRIDE 16 // words: a line for each arrival counter
 #define KVQ_P8_LEAST_SHARE 8     // tiles of a piece, at least: one for each wavefront
 #define KVQ_P8_WHOLE 16          // tiles of units that are not cut: a second round takes 0.6 us, joining 1.7 (300 tokens 8.3 -> 7.2 us)
@@ -97,6 +98,8 @@ __device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
 // have the device for itself), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
 // Calls in which sequences of many rows are taken like those of few: what they would be joined by costs more than their larger blocks save.
 __device__ inline bool small_call(int units, int tiles) { return units <= KVQ_P8_SMALL_UNITS && tiles <= KVQ_P8_SMALL_TILES; }
+// Whether units are cut into no more pieces than the device takes at a time.
+__host__ __device__ inline bool few_units(int64_t units, int64_t at_a_time) { return units <= at_a_time - (at_a_time >> 4); }
 struct Piece {
     int seq, unit, tiles, pieces, piece;
     int slot;  // of the unit's first piece among those of all units that are cut
@@ -122,7 +125,7 @@ struct Cuts {
     __device__ int total(F f) const { return __builtin_amdgcn_readlane(wave_scan(sum(f)), 63); }
     __device__ int cuts_of(int tiles) const { return tiles <= KVQ_P8_WHOLE ? 1 : (uint32_t)(tiles + share - 1) / (uint32_t)share; }
 
-    __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_) : all(shapes), mine(own), small(true), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
+    __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_, int wanted) : all(shapes), mine(own), small(true), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
         int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
         if (!small_call(units, tiles)) {
             small = false;
@@ -132,15 +135,16 @@ struct Cuts {
         int longest = 0;
         sum([&](Shape x) { longest = max(longest, x.units ? x.tiles : 0); return 0; });
         longest = wave_max(longest);
-        const int wanted = KVQ_P8_GROUPS;
         int low = max(max(KVQ_P8_LEAST_SHARE, (tiles + wanted - 1) / wanted),
                       max((longest + KVQ_P8_MOST_PIECES - 1) / KVQ_P8_MOST_PIECES, (int)(KVQ_P8_ROOT * sqrtf((float)longest))));
-        share = max(low, KVQ_P8_MANY_SHARE);
-        if (2 * units > wanted) return;
+        const auto all_pieces = [&]() { return total([&](Shape x) { return x.units * cuts_of(x.tiles); }); };
+        if (2 * units > wanted) low = max(low, KVQ_P8_MANY_SHARE);
+        share = low;
+        if (longest <= KVQ_P8_WHOLE || !few_units(units, wanted) || (2 * units > wanted && all_pieces() <= wanted)) return;
         int high = max(low, (tiles + wanted - units - 1) / (wanted - units));  // enough: a unit has at most one piece more than its tiles by the share
         while (high - low > low >> 4) {
             share = (low + high) >> 1;
-            if (total([&](Shape x) { return x.units * cuts_of(x.tiles); }) <= wanted) high = share;
+            if (all_pieces() <= wanted) high = share;
             else low = share + 1;
         }
         share = high;
@@ -211,7 +215,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     } else if (lane < P.n_seqs) {
         seq = seq_of(P, lane);
     }
-    Cuts cuts(shapes, P.n_seqs, shape(seq), lane);
+    Cuts cuts(shapes, P.n_seqs, shape(seq), lane, KVQ_P8_GROUPS / R);
     Piece pc;
     if (!cuts.find(blockIdx.x, pc)) return;
     const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
@@ -508,7 +512,7 @@ struct Line {
     int rows, blocks;     // flat rows, blocks
     int length;           // of all blocks of one KV head
     double seen, growth;  // tiles that the rows of the first token see; half of those that a block adds to what the next one sees
-    static constexpr int kLead = 12;
+    static constexpr int kLead = 8;
     // where block b begins (in 64-bit floating point, the same in every workgroup, where whole numbers would take a division that is a loop)
     __device__ static int place(int b, double seen, double growth) { return (int)__builtin_fma((double)b * (b + 1), growth, b * seen) + kLead * b; }
     __device__ int at(int b) const { return __builtin_amdgcn_readfirstlane(place(b, seen, growth)); }
@@ -881,7 +885,14 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             float16v sc[MAPS][NT];  // (not beyond the turn: kept from one stage to the next they would be in the way of the outputs)
             if (stage < seen) scores(stage, sc);
             __syncthreads();
-            if (stage < seen) softmax(stage, sc);
+            if (stage < seen) {
+                // (scores where they are: with the conditions before and behind the barrier taken together, half of them were copied)
+#pragma unroll
+                for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) asm volatile("" : "+v"(sc[m][x]));
+                softmax(stage, sc);
+            }
             fetch(stage);
         }
         if (!late) __syncthreads();
@@ -1063,15 +1074,16 @@ bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
     // blocks of 16 rows bound both: every number on either line stays below 2^30
     if (heads && (most * maps + 15) / 16 * (tiles + 8 + P.max_rows / 32) > (1 << 30) / heads) return false;
     // as many workgroups as pieces there can be (of few rows, or of all in a small call), and partial results of those of units that are cut
+    const int64_t at_a_time = KVQ_P8_GROUPS / plan.r;
     const auto pieces = [&](int64_t flat, int64_t limit) {
         const int64_t units = std::min(limit, (flat * maps + 16 * plan.r - 1) / (16 * plan.r) * heads);
         const int64_t cuts = units * ((tiles + KVQ_P8_LEAST_SHARE - 1) / KVQ_P8_LEAST_SHARE);
-        return std::min(cuts, 2 * units > KVQ_P8_GROUPS ? KVQ_P8_GROUPS + units : KVQ_P8_GROUPS);
+        return std::min(cuts, few_units(units, at_a_time) ? at_a_time : at_a_time + units);
     };
     plan.groups = std::max(pieces(std::min<int64_t>(most, kFewRows), INT32_MAX), pieces(most, KVQ_P8_SMALL_UNITS));
     const int64_t line = ((most + 255) / 256) * (tiles + 8 + P.max_rows / 32) * heads;
     plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_CHUNK_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
-    plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(plan.groups, KVQ_P8_GROUPS) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
+    plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(plan.groups, at_a_time) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
     return true;
 }
 
