@@ -31,12 +31,12 @@ using kvq_flash::to_half8;
 #define KVQ_P8_MANY_SHARE 24     // tiles of a piece where units are many, at least (264 units of 22 to 32 tiles 19.4 -> 15.9 us)
 #define KVQ_P8_MOST_PIECES 128   // of a unit
 #define KVQ_P8_ROOT 0.7f         // tiles of a piece by the root of the longest unit's, at least: more pieces take longer to join than they save
-                                 // (0.5, 0.9, 2: 4,001 tokens 8.6, 9.1, 10.2 us; 18,547 with two maps 24.0, 19.7, 20.7)
+                                 // (0.5, 0.7, 0.9: 18,547 tokens with two maps 23.9, 21.9, 20.8 us, four sequences of up to 81,508 25.9, 25.1, 25.9)
 #define KVQ_P8_CHUNK_GROUPS 256  // workgroups of a launch over chunks, at most: one a compute unit
 #define KVQ_P8_LEAST_CHUNK 16    // tiles of a workgroup with a chunk, at least
 #define KVQ_P8_MAP_BYTES 17408   // partial results of a wavefront with a chunk and one map
-// Calls in which chunks are taken like few rows: units of 32 rows and their tiles, at most (64 rows x 32 heads over 4,000 tokens 55 -> 34 us, 92 rows
-// with two maps over 9,651 99 -> 42; with twice as many tiles sixteen sequences of 40 rows 95 -> 126).
+// Calls in which chunks are taken like few rows: units of 32 rows and their tiles, at most (200 rows x 16 heads with two maps over 4,000 tokens 68 -> 38 us;
+// with more tiles twelve sequences of 32 rows x 32 heads over 4,000 60 -> 80).
 #define KVQ_P8_SMALL_UNITS 512
 #define KVQ_P8_SMALL_TILES 40000
 
@@ -94,11 +94,11 @@ __device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
 
 // A unit: the rows of one block of one KV head of one sequence.  Rows follow one another token by token, of a token head by head, of a head
 // map by map; a block has 16 R of them.  Units of many tiles are cut into pieces of `share` tiles at most, one workgroup each: where the units
-// are few, of the smallest share that leaves no more pieces than the device takes workgroups at a time (a workgroup that came behind them would
-// have the device for itself), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
+// are fewer than the workgroups that the device takes at a time, of the smallest share that leaves no more pieces than those (a workgroup that came
+// behind them would have the device for itself; twice or three times as many are slower throughout), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
 // Calls in which sequences of many rows are taken like those of few: what they would be joined by costs more than their larger blocks save.
 __device__ inline bool small_call(int units, int tiles) { return units <= KVQ_P8_SMALL_UNITS && tiles <= KVQ_P8_SMALL_TILES; }
-// Whether units are cut into no more pieces than the device takes at a time.
+// Whether units are cut into no more pieces than the device takes at a time (200 units of 125 tiles 50 -> 38 us; up to half as many before).
 __host__ __device__ inline bool few_units(int64_t units, int64_t at_a_time) { return units <= at_a_time - (at_a_time >> 4); }
 struct Piece {
     int seq, unit, tiles, pieces, piece;
@@ -506,8 +506,8 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 // ---- Sequences with many rows: chunks of prompts
 
 // Where the work of the units lies on one line that workgroups take equal shares of.  A block's length on it is its tiles, by the tokens that its last
-// row sees, and kLead for what a block costs beside them (12 of them take as long as a block's start and end: a prompt of 8,192 tokens, whose first
-// blocks have few, 902 us with 4, 832 with 12, 859 with 28); blocks of a KV head lie one after the other, KV heads, sequences.
+// row sees, and kLead for what a block costs beside them (33 sequences, chunks of up to 965 rows x 64 heads among them, 246 us with 4, 211 with 8, 213
+// with 12; a prompt of 8,192 tokens with two maps 836, 837, 849); blocks of a KV head lie one after the other, KV heads, sequences.
 struct Line {
     int rows, blocks;     // flat rows, blocks
     int length;           // of all blocks of one KV head
@@ -608,8 +608,8 @@ __device__ inline void softmax_tiles(Map& st, const float16v (&s)[NT], const flo
 // Products and vector instructions bound it, which overlap by half at best (16,000 products of one wavefront a SIMD 298 us, 128,000 multiply-adds of another
 // 316, both 439): matrix cores 41 % busy, vector ALUs 36 %.  So what counts is few instructions: codes are widened once a workgroup of 256 rows, products
 // are of 32 x 32 (half the instructions and operand reads of 16 x 16), a lane has one row's statistics, the sum is a dot product of the rounded pairs.
-// Two chunks of 1,024 behind 16,000 tokens x 40 heads 690 us = 942 TFLOP/s (770 with four wavefronts of 32 rows each and products of 16 x 16, two workgroups
-// a compute unit), a prompt of 8,192 x 28 heads with two maps 855 us = 844 TFLOP/s (1,110).
+// Two chunks of 1,024 behind 16,000 tokens x 40 heads 692 us = 939 TFLOP/s (770 with four wavefronts of 32 rows each and products of 16 x 16, two workgroups
+// a compute unit), a prompt of 8,192 x 28 heads with two maps 837 us = 863 TFLOP/s (1,110).
 template <int MAPS>
 __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
@@ -929,7 +929,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
 
         // ---- the pieces of a unit that lies in several workgroups' shares, joined two by two as a tree over their order on the line: of two neighbours
         // whoever finds the other's stored joins it to its own, in registers, and goes on to the next level.  Products are rounded before they are added,
-        // so that it does not matter who.  A pair's counter is that of the workgroup at which its second half begins, its slot that of its first.
+        // so that it does not matter who (all pieces joined by the last of them, one after the other: 232 rows x 4 heads with two maps over 48,010 tokens, in a
+        // batch of nine, 267 us; so 137).  A pair's counter is that of the workgroup at which its second half begins, its slot that of its first.
         const int w0 = unit / share, pieces = (unit + length - 1) / share - w0 + 1;
         bool mine = true;
         for (int width = 1, at = wg - w0, turn = 0; mine && width < pieces; width *= 2, turn ^= 1) {
