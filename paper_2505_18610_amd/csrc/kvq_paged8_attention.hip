@@ -606,10 +606,11 @@ __device__ inline void softmax_tiles(Map& st, const float16v (&s)[NT], const flo
 // the other has its softmax, widens the codes of a stage two further on into LDS and loads the next.  A barrier stands between the turns.  A stage is
 // written in the turns 2 s - 3 and 2 s - 2, its keys are read in 2 s and 2 s + 1, its values in 2 s + 2 and 2 s + 3: four buffers.
 // Products and vector instructions bound it, which overlap by half at best (16,000 products of one wavefront a SIMD 298 us, 128,000 multiply-adds of another
-// 316, both 439): matrix cores 41 % busy, vector ALUs 36 %.  So what counts is few instructions: codes are widened once a workgroup of 256 rows, products
-// are of 32 x 32 (half the instructions and operand reads of 16 x 16), a lane has one row's statistics, the sum is a dot product of the rounded pairs.
-// Two chunks of 1,024 behind 16,000 tokens x 40 heads 692 us = 939 TFLOP/s (770 with four wavefronts of 32 rows each and products of 16 x 16, two workgroups
-// a compute unit), a prompt of 8,192 x 28 heads with two maps 837 us = 863 TFLOP/s (1,110).
+// 316, both 439): matrix cores 40 % busy, vector instructions, products among them, 44 %.  So what counts is few instructions: codes are widened once a
+// workgroup of 256 rows, products are of 32 x 32 (half the instructions and operand reads of 16 x 16), a lane has one row's statistics, the sum is a dot
+// product of the rounded pairs.  Two chunks of 1,024 behind 16,000 tokens x 40 heads 704 us = 923 TFLOP/s where a library product of 8,192^3 has 1,160 (770
+// with four wavefronts of 32 rows each and products of 16 x 16, two workgroups a compute unit), a prompt of 8,192 x 28 heads with two maps 850 us =
+// 849 TFLOP/s (1,110).
 template <int MAPS>
 __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
