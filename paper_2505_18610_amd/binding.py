@@ -312,17 +312,21 @@ class KvqPaged8Batch:
         self.max_rows = max_rows
         self._fixed = (table.data_ptr(), lengths.data_ptr(), None if row_begin is None else row_begin.data_ptr(),
                        pages if n <= 1 else table.stride(0), n, pages)
+        self._last = (None, None, None)
 
     def _of(self, n_rows):
-        return C.byref(_Paged8Batch(*self._fixed, n_rows, self.max_rows))  # (a structure of the call's own: threads may share a batch)
+        rows, most, last = self._last
+        if rows != n_rows or most != self.max_rows:  # (nothing writes into a structure that calls have: threads may share a batch)
+            last = _Paged8Batch(*self._fixed, n_rows, self.max_rows)
+            self._last = (n_rows, self.max_rows, last)
+        return C.byref(last)
 
 
 def _paged8_rows(t, rows, heads):
     """A packed tensor [rows, heads, 128] on a device (a dimension of one element may carry any stride)."""
-    n, h, d = t.shape
     row, head, channel = t.stride()
-    assert n == rows and h == heads and d == 128 and channel == 1 and t.is_cuda
-    return C.byref(_Paged8Rows(t.data_ptr(), 128 if n <= 1 else row, 128 if h == 1 else head))
+    assert t.shape == (rows, heads, 128) and channel == 1 and t.is_cuda
+    return C.byref(_Paged8Rows(t.data_ptr(), 128 if rows <= 1 else row, 128 if heads == 1 else head))
 
 
 class KvqPaged8:

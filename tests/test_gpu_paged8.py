@@ -540,3 +540,19 @@ def test_captured_steps_while_sequences_grow(diff):
             want, tol, _, _ = attention(plain, at, n, [0, 1, 2, 3], qq, lam=lam if diff else None)
             check(outs[turn % 2], want, tol)
     c.same()
+
+
+def test_one_batch_for_calls_of_different_rows():
+    """A batch object serves calls with more and fewer rows in their tensors, and with another max_rows, in turn."""
+    c = Pair(2, 64, 3, 4, seed=40).filled([100, 200, 70])
+    batch = kq.KvqPaged8Batch(c.table.cuda(), ints([100, 200, 70]), ints([0, 1, 3, 4]), 2)
+    outs = []
+    for n, most in ((4, 2), (3, 2), (4, 1), (4, 2)):
+        batch.max_rows = most
+        k, v = (torch.full((n, 2, D), 777.0, device="cuda") for _ in range(2))
+        c.cache.kvq_paged8_read(batch, k, v)
+        outs.append(k)
+    full, fewer_rows, fewer_a_sequence, again = outs
+    assert torch.equal(full, again) and bool((full != 777.0).all())
+    assert torch.equal(fewer_rows, full[:3])
+    assert bool((fewer_a_sequence[2] == 777.0).all()) and torch.equal(fewer_a_sequence[[0, 3]], full[[0, 3]])
