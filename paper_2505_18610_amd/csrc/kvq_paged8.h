@@ -109,6 +109,13 @@ struct Census {
     }
 };
 
+// A unit's pieces are joined level by level, width = 1, 2, 4, ...: of two neighbours whoever finds the other's results stored joins them and goes on
+// as the first.  A level's answer goes through a word of LDS of its own: a piece without a neighbour at a level passes it without a barrier, so
+// that at the next one slower wavefronts may still be reading the word of the level before.
+constexpr int kJoinLevels = 8;  // of at most 256 pieces
+KVQ_HD int join_other(int at, int width) { return at ^ width; }
+KVQ_HD int join_word(int level) { return level; }
+
 }  // namespace kvq_p8
 
 #endif

@@ -616,7 +616,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * STAGE];
     __shared__ u32x4 lds_q[MAPS == 2 ? 8 : 1][4][64];  // two maps: the second's queries, for which there are no registers
-    __shared__ int lds_last[2];
+    static_assert(KVQ_P8_CHUNK_GROUPS <= 1 << kJoinLevels, "levels of a join");
+    __shared__ int lds_last[kJoinLevels];
     const KvqP8& P = A.p;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_page = P.page_shift - 5;
@@ -934,8 +935,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         // batch of nine, 267 us; so 137).  A pair's counter is that of the workgroup at which its second half begins, its slot that of its first.
         const int w0 = unit / share, pieces = (unit + length - 1) / share - w0 + 1;
         bool mine = true;
-        for (int width = 1, at = wg - w0, turn = 0; mine && width < pieces; width *= 2, turn ^= 1) {
-            const int other = at ^ width, begin = min(at, other), second = max(at, other);
+        for (int width = 1, at = wg - w0, level = 0; mine && width < pieces; width *= 2, ++level) {
+            const int other = join_other(at, width), begin = min(at, other), second = max(at, other);
             if (second >= pieces) continue;
             constexpr int MAP = KVQ_P8_MAP_BYTES, SLOT = 8 * MAPS * MAP, FLY = MAPS == 1 ? 16 : 8;
             const bool rows_here = block * RB + wave * 32 < flat;  // whether the wavefront has any
@@ -944,9 +945,9 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             };
             const int own_at = wave * MAPS * MAP + (opaque(threadIdx.x) & 63) * 16;
             uint32_t* const counter = A.counters + (int64_t)(w0 + second) * KVQ_P8_COUNTER_STRIDE;
-            if (threadIdx.x == 0) lds_last[turn] = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
+            if (threadIdx.x == 0) lds_last[join_word(level)] = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
             __syncthreads();
-            mine = lds_last[turn] != 0;
+            mine = lds_last[join_word(level)] != 0;
             if (!mine) {
                 const __amdgpu_buffer_rsrc_t to = slot(at);
                 if (rows_here)
@@ -962,9 +963,9 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                 }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
-                if (threadIdx.x == 0) lds_last[turn] = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
+                if (threadIdx.x == 0) lds_last[join_word(level)] = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1u ? 1 : 0;
                 __syncthreads();
-                mine = lds_last[turn] != 0;
+                mine = lds_last[join_word(level)] != 0;
             }
             if (mine && threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             asm volatile("" ::: "memory");

@@ -1,0 +1,139 @@
+// What the kernels of the paged cache of 8-bit floating point work out from device arrays (paper_2505_18610_amd/csrc/kvq_paged8.h), on the CPU.
+// tests/test_paged8_stub.py builds it with sanitizers; argument: the scenario.  Exit code 0 = pass.  No GPU and no HIP library is involved.
+#include <algorithm>
+#include <barrier>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <functional>
+#include <random>
+#include <set>
+#include <string>
+#include <thread>
+#include <vector>
+
+using std::max;
+using std::min;
+
+// ---- A wavefront: 64 threads, and what its lanes tell one another
+struct Dim {
+    unsigned x;
+};
+thread_local Dim threadIdx;
+std::barrier<> lanes(64);
+int told[64];
+template <class F>
+auto tell(int x, F f) {
+    told[threadIdx.x] = x;
+    lanes.arrive_and_wait();
+    const auto y = f();
+    lanes.arrive_and_wait();
+    return y;
+}
+inline int dpp(int old, int x, int ctrl, int rows, int, bool) {
+    return tell(x, [&] {
+        const int lane = threadIdx.x, row = lane >> 4, shift = ctrl & 15;
+        if (!(rows >> row & 1)) return old;
+        if (ctrl > 0x110 && ctrl < 0x120) return (lane & 15) >= shift ? told[lane - shift] : old;  // row_shr
+        if (ctrl == 0x142) return row ? told[16 * row - 1] : old;                                  // row_bcast:15
+        if (ctrl == 0x143) return row >= 2 ? told[31] : old;                                       // row_bcast:31
+        abort();
+    });
+}
+inline int readlane(int x, int lane) {
+    return tell(x, [&] { return told[lane & 63]; });
+}
+inline uint64_t ballot(bool x) {
+    return tell(x, [&] {
+        uint64_t bits = 0;
+        for (int i = 0; i < 64; ++i) bits |= (uint64_t)(told[i] != 0) << i;
+        return bits;
+    });
+}
+template <class F>
+void wavefront(F f) {
+    std::vector<std::thread> threads;
+    for (unsigned i = 0; i < 64; ++i)
+        threads.emplace_back([i, &f] {
+            threadIdx.x = i;
+            f((int)i);
+        });
+    for (auto& t : threads) t.join();
+}
+#define __builtin_amdgcn_update_dpp dpp
+#define __builtin_amdgcn_readlane readlane
+#define __ballot ballot
+#include "../paper_2505_18610_amd/csrc/kvq_paged8.h"
+
+namespace {
+
+int failures = 0;
+#define CHECK(cond, ...)                                                                                                        \
+    do {                                                                                                                        \
+        if (!(cond) && ++failures < 20) { printf("line %d: %s: ", __LINE__, #cond); printf(__VA_ARGS__); printf("\n"); fflush(stdout); } \
+    } while (0)
+
+// ---- The join of a unit's pieces, in any order of arrival.  At each level a workgroup writes the word that `word` says and all its wavefronts read it
+// behind a barrier; the next barrier is that of the next level that has a neighbour: whether its word is that of the level before says
+// whether a slower wavefront's read can meet the write.
+int joins_on_a_word_still_read(int pieces, const std::function<int(int)>& word, std::mt19937& rng) {
+    using namespace kvq_p8;
+    int bad = 0;
+    std::vector<int> order(pieces), stored(pieces, 0);
+    std::vector<std::set<int>> holds(pieces);
+    std::set<int> counters;
+    for (int p = 0; p < pieces; ++p) order[p] = p, holds[p] = {p};
+    std::shuffle(order.begin(), order.end(), rng);
+    int whole = 0;
+    for (int piece : order) {
+        std::set<int> mine = {piece};
+        bool go_on = true;
+        int last = -1;
+        for (int width = 1, at = piece, level = 0; go_on && width < pieces; width *= 2, ++level) {
+            const int other = join_other(at, width), begin = min(at, other), second = max(at, other);
+            if (second >= pieces) continue;
+            const int w = word(level);
+            CHECK(w >= 0 && w < kJoinLevels && level < kJoinLevels, "word %d at level %d of %d pieces", w, level, pieces);
+            bad += w == last;
+            last = w;
+            if (stored[second] == 0) {  // the first of the two: its results stay in its slot
+                stored[second] = 1;
+                holds[at] = mine;
+                go_on = false;
+            } else {  // a pair's counter is its second half's: of one level only
+                CHECK(stored[second] == 1 && counters.insert(second).second, "the counter of piece %d of %d twice", second, pieces);
+                stored[second] = 2;
+                for (int p : holds[other]) CHECK(mine.insert(p).second, "piece %d of %d twice", p, pieces);
+            }
+            at = begin;
+        }
+        if (go_on) {
+            ++whole;
+            CHECK((int)mine.size() == pieces, "%d of %d pieces", (int)mine.size(), pieces);
+        }
+    }
+    CHECK(whole == 1, "%d results of %d pieces", whole, pieces);
+    return bad;
+}
+void join() {
+    std::mt19937 rng(1);
+    std::set<int> alternating;
+    for (int pieces = 1; pieces <= 256; ++pieces)
+        for (int turn = 0; turn < 20; ++turn) {
+            CHECK(joins_on_a_word_still_read(pieces, kvq_p8::join_word, rng) == 0, "%d pieces", pieces);
+            if (joins_on_a_word_still_read(pieces, [](int level) { return level & 1; }, rng)) alternating.insert(pieces);
+        }
+    // (two words in turn would not do: levels are passed without a barrier)
+    for (int pieces : {6, 11, 12, 14}) CHECK(alternating.count(pieces), "%d pieces, two words", pieces);
+}
+
+}  // namespace
+
+int main(int argc, char** argv) {
+    const std::string what = argc > 1 ? argv[1] : "";
+    if (what == "join") join();
+    else return 2;
+    if (failures) printf("%d failures\n", failures);
+    else printf("ok\n");
+    return failures ? 1 : 0;
+}
