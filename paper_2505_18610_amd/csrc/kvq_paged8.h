@@ -95,7 +95,8 @@ struct Census {
         upto = wave_scan(mine);
         total = __builtin_amdgcn_readlane(upto, 63);
     }
-    // The sequence of thing p (0 <= p < total) and, in `first`, the number of the sequence's first one.
+    // The sequence of thing p (0 <= p < total) and, in `first`, the number of the sequence's first one; -1 where counts that are asked again have
+    // changed meanwhile.
     __device__ int find(int p, int& first) const {
         const int at = __builtin_ctzll(__ballot(upto > p)), before = __builtin_amdgcn_readlane(upto - mine, at);
         if (per == 1) {
@@ -103,11 +104,24 @@ struct Census {
             return at;
         }
         const int s = at * per + lane, x = lane < per && s < n ? count(s) : 0, sum = before + wave_scan(x);
-        const int k = __builtin_ctzll(__ballot(sum > p));
+        const uint64_t behind = __ballot(sum > p);
+        if (!behind) return -1;
+        const int k = __builtin_ctzll(behind);
         first = __builtin_amdgcn_readlane(sum - x, k);
         return at * per + k;
     }
 };
+
+// On from sequence s, whose first thing has the number `first` <= p, to the sequence of thing p; false where there is none (any more).
+template <class Count>
+__device__ inline bool walk(const Count& count, int n, int p, int& s, int& first) {
+    for (;;) {
+        const int things = count(s);
+        if (p - first < things) return true;
+        first += things;
+        if (++s >= n) return false;
+    }
+}
 
 // A unit's pieces are joined level by level, width = 1, 2, 4, ...: of two neighbours whoever finds the other's results stored joins them and goes on
 // as the first.  A level's answer goes through a word of LDS of its own: a piece without a neighbour at a level passes it without a barrier, so

@@ -50,6 +50,7 @@ __device__ inline bool touched_page(const KvqP8& P, int per_seq, int id, Touched
         if (id >= census.total) return false;
         int before;
         T.s = census.find(id, before);
+        if (T.s < 0) return false;
         number = id - before;
     }
     const Seq q = seq_of(P, T.s);

@@ -221,7 +221,9 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
     if (P.n_seqs > 64) seq = seq_of(P, s);
     else seq = Seq{__builtin_amdgcn_readlane(seq.row0, s), __builtin_amdgcn_readlane(seq.rows, s), __builtin_amdgcn_readlane(seq.tokens, s)};
-    const int blocks = (uint32_t)(seq.rows * rows_per_token + RB - 1) / RB, kv = (uint32_t)pc.unit / (uint32_t)blocks, block = pc.unit - kv * blocks;
+    const int blocks = (uint32_t)(seq.rows * rows_per_token + RB - 1) / RB;
+    if (pc.unit >= blocks * P.n_kv) return;  // (rows have changed since the units were counted)
+    const int kv = (uint32_t)pc.unit / (uint32_t)blocks, block = pc.unit - kv * blocks;
     // (equal ranges: 33 tiles are 17 and 16, not 32 and 1)
     const int each = (uint32_t)tiles / (uint32_t)pieces, left = tiles - each * pieces;
     const int t0 = piece * each + min(piece, left), t1 = t0 + each + (piece < left ? 1 : 0);
@@ -641,17 +643,17 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     const int range_end = min(census.total, pos + share);
     int first;
     int s = __builtin_amdgcn_readfirstlane(census.find(pos, first));
+    if (s < 0) return;
     first = __builtin_amdgcn_readfirstlane(first);
     while (pos < range_end) {
-        Seq seq = seq_of(P, s);
-        Line ln = line(seq);
-        for (;;) {
-            const int all = __builtin_amdgcn_readfirstlane(ln.length) * P.n_kv;
-            if (pos - first < all) break;
-            first += all;
-            seq = seq_of(P, ++s);
+        Seq seq;
+        Line ln;
+        const auto length_of = [&](int s) {
+            seq = seq_of(P, s);
             ln = line(seq);
-        }
+            return __builtin_amdgcn_readfirstlane(ln.length) * P.n_kv;
+        };
+        if (!walk(length_of, P.n_seqs, pos, s, first)) return;
         int gqa = A.gqa;
         asm volatile("" : "+s"(gqa));  // (as opaque(): its reciprocal would be kept in registers throughout)
         const int flat = seq.rows * gqa;
@@ -933,7 +935,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         // whoever finds the other's stored joins it to its own, in registers, and goes on to the next level.  Products are rounded before they are added,
         // so that it does not matter who (all pieces joined by the last of them, one after the other: 232 rows x 4 heads with two maps over 48,010 tokens, in a
         // batch of nine, 267 us; so 137).  A pair's counter is that of the workgroup at which its second half begins, its slot that of its first.
-        const int w0 = unit / share, pieces = (unit + length - 1) / share - w0 + 1;
+        // (no piece lies behind the line's end, also where lengths have changed since it was measured)
+        const int w0 = unit / share, pieces = (min(unit + length, census.total) - 1) / share - w0 + 1;
         bool mine = true;
         for (int width = 1, at = wg - w0, level = 0; mine && width < pieces; width *= 2, ++level) {
             const int other = join_other(at, width), begin = min(at, other), second = max(at, other);

@@ -127,11 +127,65 @@ void join() {
     for (int pieces : {6, 11, 12, 14}) CHECK(alternating.count(pieces), "%d pieces, two words", pieces);
 }
 
+// ---- Which sequence a thing belongs to, also where the counts change between two readings
+void lookup() {
+    std::mt19937 rng(2);
+    const auto upto = [&](int n) { return (int)(rng() % n); };
+    for (int n : {1, 2, 63, 64, 65, 128, 300, 1000, 4096}) {
+        std::vector<int> now(n);
+        for (int& x : now) x = upto(3) ? upto(9) : 0;
+        now[upto(n)] = 40;
+        std::vector<int> starts;
+        for (int s = 0, at = 0; s < n; at += now[s++]) starts.push_back(at);
+        const int total = starts[n - 1] + now[n - 1];
+        const std::vector<int> before = now;
+        std::vector<int> things = {0, total - 1};
+        for (int i = 0; i < 12; ++i) things.push_back(upto(total));
+        std::vector<std::vector<int>> after;
+        after.push_back(std::vector<int>(n, 0));  // all gone; some fewer; more
+        after.push_back(before);
+        for (int& x : after.back()) x = x && upto(2) ? x - 1 : x;
+        after.push_back(before);
+        for (int& x : after.back()) x += upto(4);
+        wavefront([&](int lane) {
+            const auto count = [&](int s) { return now.at(s); };
+            const kvq_p8::Census<decltype(count)> census(count, n);
+            if (lane == 0) CHECK(census.total == total, "%d of %d things", census.total, total);
+            for (int p : things) {
+                int first;
+                const int s = census.find(p, first);
+                if (lane == 0) CHECK(s >= 0 && s < n && first == starts[s] && p < first + before[s], "thing %d of %d: sequence %d of %d", p, total, s, n);
+                for (int q : {p, min(total - 1, p + 1), total - 1}) {
+                    int t = s, at = first;
+                    const bool there = kvq_p8::walk(count, n, q, t, at);
+                    if (lane == 0) CHECK(there && t < n && at == starts[t] && q < at + before[t], "thing %d from sequence %d", q, s);
+                }
+            }
+            for (const auto& changed : after) {
+                lanes.arrive_and_wait();
+                if (lane == 0) now = changed;
+                lanes.arrive_and_wait();
+                for (int p : things) {
+                    int first = 0;
+                    const int s = census.find(p, first);
+                    if (lane == 0) CHECK(s >= -1 && s < n, "sequence %d of %d", s, n);
+                    if (s < 0) continue;
+                    if (lane == 0) CHECK(first >= 0 && first <= p, "first %d of thing %d", first, p);
+                    int t = s, at = first;
+                    const bool there = kvq_p8::walk(count, n, total - 1, t, at);  // (counts are read with their bounds checked)
+                    if (lane == 0 && there) CHECK(t < n && at <= total - 1 && total - 1 < at + now[t], "thing %d: sequence %d", total - 1, t);
+                }
+            }
+        });
+    }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "join") join();
+    else if (what == "lookup") lookup();
     else return 2;
     if (failures) printf("%d failures\n", failures);
     else printf("ok\n");
