@@ -112,6 +112,15 @@ struct Census {
     }
 };
 
+// Whether the sequences have no more rows together than the tensors (row numbers that fall can have it otherwise).
+__device__ inline bool rows_fit(const KvqP8& P) {
+    const int lane = threadIdx.x & 63, per = (P.n_seqs + 63) >> 6;
+    int mine = 0;  // (64 times n_rows are within 32 bits)
+    for (int k = 0; k < per; ++k)
+        if (lane * per + k < P.n_seqs) mine += seq_of(P, lane * per + k).rows;
+    return !__ballot(mine > P.n_rows) && __builtin_amdgcn_readlane(wave_scan(min(mine, P.n_rows)), 63) <= P.n_rows;
+}
+
 // On from sequence s, whose first thing has the number `first` <= p, to the sequence of thing p; false where there is none (any more).
 template <class Count>
 __device__ inline bool walk(const Count& count, int n, int p, int& s, int& first) {

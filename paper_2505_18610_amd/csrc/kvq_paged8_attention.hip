@@ -51,6 +51,7 @@ struct AttnArgs {
     int64_t q_rs, q_hs, o_rs, o_hs, lse_hs;
     int32_t gqa, maps, out_fp32;   // gqa: query heads of a KV head
     int32_t few_rows;              // sequences with more flat rows (of one map) are chunks, unless the call is small
+    int32_t packed;                // the line of all chunks was measured for n_rows rows in all, not for max_rows of every sequence
     float scale_log2, eps, out_scale;
     uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
 };
@@ -98,6 +99,9 @@ __device__ inline float4v nan_codes(uint32_t (&w)[2], int token, int limit) {
 // behind them would have the device for itself; twice or three times as many are slower throughout), else of what an equal share of all tiles is, short units behind long pieces as workgroups end.
 // Calls in which sequences of many rows are taken like those of few: what they would be joined by costs more than their larger blocks save.
 __device__ inline bool small_call(int units, int tiles) { return units <= KVQ_P8_SMALL_UNITS && tiles <= KVQ_P8_SMALL_TILES; }
+// What a sequence adds to either number: no more than is too many, so that the sums of 4,096 sequences stay within 32 bits.
+__device__ inline int small_units(int units) { return min(units, KVQ_P8_SMALL_UNITS + 1); }
+__device__ inline int small_tiles(int units, int tiles) { return min(small_units(units) * min(tiles, KVQ_P8_SMALL_TILES + 1), KVQ_P8_SMALL_TILES + 1); }
 // Whether units are cut into no more pieces than the device takes at a time (200 units of 125 tiles 50 -> 38 us; up to half as many before).
 __host__ __device__ inline bool few_units(int64_t units, int64_t at_a_time) { return units <= at_a_time - (at_a_time >> 4); }
 struct Piece {
@@ -126,7 +130,7 @@ struct Cuts {
     __device__ int cuts_of(int tiles) const { return tiles <= KVQ_P8_WHOLE ? 1 : (uint32_t)(tiles + share - 1) / (uint32_t)share; }
 
     __device__ Cuts(const Shape* shapes, int n_seqs, Shape own, int lane_, int wanted) : all(shapes), mine(own), small(true), n(n_seqs), per((n_seqs + 63) >> 6), lane(lane_) {
-        int units = total([](Shape x) { return x.units; }), tiles = total([](Shape x) { return x.units * x.tiles; });
+        int units = total([](Shape x) { return small_units(x.units); }), tiles = total([](Shape x) { return small_tiles(x.units, x.tiles); });
         if (!small_call(units, tiles)) {
             small = false;
             units = total([](Shape x) { return x.units; });
@@ -625,12 +629,13 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
     const int per_page = P.page_shift - 5;
 
     {
-        const auto units_of = [&](int s) { return (seq_of(P, s).rows * A.gqa * MAPS + 31) / 32 * P.n_kv; };  // as the launch over pieces counts them
-        const auto tiles_of = [&](int s) { return units_of(s) * max(1, (seq_of(P, s).tokens + 31) >> 5); };
+        const auto units_of = [&](int s) { return small_units((seq_of(P, s).rows * A.gqa * MAPS + 31) / 32 * P.n_kv); };  // as the launch over pieces counts them
+        const auto tiles_of = [&](int s) { return small_tiles(units_of(s), max(1, (seq_of(P, s).tokens + 31) >> 5)); };
         const Census<decltype(units_of)> units(units_of, P.n_seqs);
         const Census<decltype(tiles_of)> tiles(tiles_of, P.n_seqs);
         if (small_call(units.total, tiles.total)) return;
     }
+    if (A.packed && !rows_fit(P)) return;
     const auto line = [&](const Seq& q) { return line_of<RB>(q, A.gqa, A.few_rows); };
     const auto count = [&](int s) { return line(seq_of(P, s)).length * P.n_kv; };
     const Census<decltype(count)> census(count, P.n_seqs);
@@ -1068,17 +1073,27 @@ bool heads_ok(int32_t n_q, int32_t n_kv) { return n_q >= 1 && n_q % n_kv == 0 &&
 
 // The launches of a call: over ranges of tiles for sequences of few rows, of more where there may be any.  Either uses the workspace from its start.
 constexpr int kFewRows = 64;  // flat rows of one map
+constexpr int64_t kMostSum = 1 << 30;  // what the kernels add up, at most
 struct Plan {
     int r;                  // groups of 16 rows of the first launch
+    bool packed;
     int64_t groups, chunk;  // workgroups
     uint64_t bytes;
 };
 bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
-    const int64_t most = (int64_t)P.max_rows * gqa, rows = std::min<int64_t>(most, kFewRows) * maps;
-    plan.r = rows <= 16 ? 1 : 2;
+    const int64_t most = (int64_t)P.max_rows * gqa, few = std::min<int64_t>(most, kFewRows) * maps;
+    plan.r = few <= 16 ? 1 : 2;
     const int64_t tiles = (int64_t)P.table_pages << (P.page_shift - 5), heads = (int64_t)P.n_seqs * P.n_kv;
-    // blocks of 16 rows bound both: every number on either line stays below 2^30
-    if (heads && (most * maps + 15) / 16 * (tiles + 8 + P.max_rows / 32) > (1 << 30) / heads) return false;
+    // the sums of a launch over pieces, which counts all sequences' rows as few
+    if (heads && (few + 16 * plan.r - 1) / (16 * plan.r) * tiles > kMostSum / heads) return false;
+    // and the line of all chunks: blocks of every sequence as if each had max_rows, or where that is too many, of the rows that there are
+    const int64_t length = tiles + 2 * Line::kLead + P.max_rows / 64, of_each = (most + 255) / 256 * P.n_seqs;
+    int64_t blocks = of_each;
+    plan.packed = most > kFewRows && heads && of_each * length > kMostSum / P.n_kv;
+    if (plan.packed) {
+        blocks = std::min(of_each, (int64_t)P.n_rows * gqa / 256 + P.n_seqs);
+        if (blocks * length > kMostSum / P.n_kv) return false;
+    }
     // as many workgroups as pieces there can be (of few rows, or of all in a small call), and partial results of those of units that are cut
     const int64_t at_a_time = KVQ_P8_GROUPS / plan.r;
     const auto pieces = [&](int64_t flat, int64_t limit) {
@@ -1087,7 +1102,8 @@ bool plan_of(const KvqP8& P, int gqa, int maps, Plan& plan) {
         return std::min(cuts, few_units(units, at_a_time) ? at_a_time : at_a_time + units);
     };
     plan.groups = std::max(pieces(std::min<int64_t>(most, kFewRows), INT32_MAX), pieces(most, KVQ_P8_SMALL_UNITS));
-    const int64_t line = ((most + 255) / 256) * (tiles + 8 + P.max_rows / 32) * heads;
+    if (plan.groups > UINT32_MAX / 512) return false;  // threads of a launch
+    const int64_t line = blocks * length * P.n_kv;
     plan.chunk = most > kFewRows ? std::min<int64_t>(KVQ_P8_CHUNK_GROUPS, (line / KVQ_P8_LEAST_CHUNK + 8) & ~7ll) : 0;
     plan.bytes = kCounterBytes + 2 * (uint64_t)std::max<int64_t>(std::min<int64_t>(plan.groups, at_a_time) * plan.r * KVQ_PART_BYTES, plan.chunk * 8 * maps * KVQ_P8_MAP_BYTES);
     return true;
@@ -1114,6 +1130,7 @@ kvq_status_t attend(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, 
     A.counters = static_cast<uint32_t*>(workspace);
     A.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterBytes);
     A.few_rows = kFewRows;
+    A.packed = plan.packed ? 1 : 0;
     if (plan.r == 1) hipLaunchKernelGGL(kvq_paged8_ranges_kernel<1>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     else hipLaunchKernelGGL(kvq_paged8_ranges_kernel<2>, dim3((unsigned)plan.groups), dim3(512), 0, stream, A);
     if (hipGetLastError() != hipSuccess) return KVQ_E_HIP;

@@ -180,12 +180,37 @@ void lookup() {
     }
 }
 
+// ---- Whether rows are no more than the tensors have, also where row numbers fall, up to the largest that there can be
+void rows() {
+    std::mt19937 rng(3);
+    const auto upto = [&](int64_t n) { return (int32_t)(rng() % n); };
+    for (int n : {1, 5, 64, 65, 4096})
+        for (int n_rows : {1, 77, 100000, INT32_MAX / 64})
+            for (int kind = 0; kind < 4; ++kind) {
+                std::vector<int32_t> begin(n + 1), lengths(n, 5), table(n, 0);
+                for (int32_t& b : begin) b = upto((int64_t)n_rows + 1);
+                if (kind < 2) std::sort(begin.begin(), begin.end());
+                if (kind == 1) begin[0] = -7, begin[n] = INT32_MAX;
+                if (kind == 3)
+                    for (int s = 0; s <= n; ++s) begin[s] = s & 1 ? n_rows : 0;
+                KvqP8 P{nullptr, nullptr, table.data(), lengths.data(), begin.data(), 1, 1, 1, 5, 1, n, n_rows, kind == 1 ? max(1, n_rows / 2) : n_rows};
+                int64_t all = 0;
+                for (int s = 0; s < n; ++s) all += kvq_p8::seq_of(P, s).rows;
+                wavefront([&](int lane) {
+                    const bool fit = kvq_p8::rows_fit(P);
+                    if (lane == 0) CHECK(fit == (all <= n_rows), "%lld of %d rows, %d sequences", (long long)all, n_rows, n);
+                });
+                CHECK(kind >= 2 || all <= n_rows, "%lld of %d rows", (long long)all, n_rows);
+            }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "join") join();
     else if (what == "lookup") lookup();
+    else if (what == "rows") rows();
     else return 2;
     if (failures) printf("%d failures\n", failures);
     else printf("ok\n");

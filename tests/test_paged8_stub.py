@@ -23,7 +23,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["join", "lookup"])
+@pytest.mark.parametrize("scenario", ["join", "lookup", "rows"])
 def test_on_the_cpu(program, scenario):
     r = subprocess.run([program, scenario], capture_output=True, text=True, timeout=600)
     if r.returncode != 0 and "ASan runtime does not come first" in r.stderr:
