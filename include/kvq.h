@@ -331,7 +331,8 @@ kvq_status_t kvq_cache_export_segment(kvq_cache_t* cache, int32_t layer, int32_t
  * where a NaN has been appended.  A value stands for code * 2^e.
  *
  * What no page, row or token is named by does not exist, and nothing is read or written for it: rows of a sequence beyond max_rows or
- * n_rows, tokens beyond the table (lengths count as table_pages * page_tokens at most, negative ones as 0), table entries outside
+ * n_rows, tokens at table_pages * page_tokens and beyond (rows that are such tokens are neither appended nor read; as queries they see all
+ * that the table has) and, where there are more rows than tokens, in front of the first (negative lengths count as 0), table entries outside
  * 0 .. n_pages - 1 (a page that has been given up: attention passes over its tokens).  Rows that belong to no sequence are left as they were.
  * The device arrays are read while a call runs and must not change before it ends: where they do, nothing outside the call's tensors and workspace is
  * touched, but what the sequences' rows and pages hold is not defined, and the workspace has to be filled with zeros again. */

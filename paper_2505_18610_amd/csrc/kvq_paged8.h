@@ -8,7 +8,7 @@
 //
 // Page tables, lengths and row numbers are device arrays that a kernel holds against the sizes that the host knows, so that one captured
 // launch serves while the sequences grow: rows of a sequence beyond max_rows or beyond the tensors, tokens beyond the table and entries of
-// the table that name no page do not exist.
+// the table that name no page do not exist.  A row is the token that the sequence's length says, whether the table has it or not.
 #ifndef KVQ_PAGED8_H
 #define KVQ_PAGED8_H
 
@@ -35,7 +35,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Seq {
-    int32_t row0, rows, tokens;  // first row, rows, tokens up to and with those of the rows
+    int32_t row0, rows, end, tokens;  // first row, rows; tokens up to and with those of the rows, and how many of them the table has
 };
 __device__ inline Seq seq_of(const KvqP8& P, int s) {
     Seq q;
@@ -46,7 +46,8 @@ __device__ inline Seq seq_of(const KvqP8& P, int s) {
         end = min(P.row_begin[s + 1], P.n_rows);
     }
     q.rows = min(max(end - q.row0, 0), P.max_rows);
-    q.tokens = min(max(P.lengths[s], 0), P.table_pages << P.page_shift);
+    q.end = max(P.lengths[s], 0);
+    q.tokens = min(q.end, P.table_pages << P.page_shift);
     return q;
 }
 // The page that holds page `at` of a sequence, or -1.

@@ -36,8 +36,8 @@ struct Touched {
 };
 __device__ inline bool touched_page(const KvqP8& P, int per_seq, int id, Touched& T) {
     const auto pages = [&](const Seq& q) {
-        const int first = max(0, q.tokens - q.rows);
-        return q.rows && q.tokens ? ((q.tokens - 1) >> P.page_shift) - (first >> P.page_shift) + 1 : 0;
+        const int first = max(0, q.end - q.rows);
+        return first < min(q.tokens, first + q.rows) ? ((q.tokens - 1) >> P.page_shift) - (first >> P.page_shift) + 1 : 0;
     };
     int number;
     if (per_seq) {
@@ -55,7 +55,7 @@ __device__ inline bool touched_page(const KvqP8& P, int per_seq, int id, Touched
     }
     const Seq q = seq_of(P, T.s);
     if (number >= pages(q)) return false;
-    T.first = q.tokens - q.rows;
+    T.first = q.end - q.rows;
     T.row0 = q.row0;
     T.at = (max(0, T.first) >> P.page_shift) + number;
     T.page = page_of(P, T.s, T.at);

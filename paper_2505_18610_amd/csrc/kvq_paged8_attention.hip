@@ -56,6 +56,9 @@ struct AttnArgs {
     uint32_t flip;                 // sign bits to turn over in the queries (a negative scale)
 };
 
+// Tokens that row i of a sequence's rows sees: up to and with its own, of those that the table has.
+__device__ inline int sees(const Seq& q, int i) { return min(q.tokens, max(0, q.end - q.rows + i + 1)); }
+
 // A value that the compiler takes for a new one: what follows from it is worked out where it is used, not kept in registers through a loop.
 __device__ inline int opaque(int x) {
     asm volatile("" : "+v"(x));
@@ -212,7 +215,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
         return Cuts::Shape{max(1, (q.tokens + 31) >> 5), (int)blocks * P.n_kv, q.rows * A.gqa <= A.few_rows ? 1 : 0};
     };
     Cuts::Shape* const shapes = reinterpret_cast<Cuts::Shape*>(lds_o);
-    Seq seq = {0, 0, 0};
+    Seq seq = {0, 0, 0, 0};
     if (P.n_seqs > 64) {
         for (int at = threadIdx.x; at < P.n_seqs; at += 512) shapes[at] = shape(seq_of(P, at));
         __syncthreads();
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     if (!cuts.find(blockIdx.x, pc)) return;
     const int s = pc.seq, tiles = pc.tiles, pieces = pc.pieces, piece = pc.piece;
     if (P.n_seqs > 64) seq = seq_of(P, s);
-    else seq = Seq{__builtin_amdgcn_readlane(seq.row0, s), __builtin_amdgcn_readlane(seq.rows, s), __builtin_amdgcn_readlane(seq.tokens, s)};
+    else seq = Seq{__builtin_amdgcn_readlane(seq.row0, s), __builtin_amdgcn_readlane(seq.rows, s), __builtin_amdgcn_readlane(seq.end, s), __builtin_amdgcn_readlane(seq.tokens, s)};
     const int blocks = (uint32_t)(seq.rows * rows_per_token + RB - 1) / RB;
     if (pc.unit >= blocks * P.n_kv) return;  // (rows have changed since the units were counted)
     const int kv = (uint32_t)pc.unit / (uint32_t)blocks, block = pc.unit - kv * blocks;
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
     for (int r = 0; r < R; ++r) {
         row_i[r] = (uint32_t)(block * RB + 16 * r + n) / (uint32_t)rows_per_token;
         const bool real = row_i[r] < seq.rows;
-        limit[r] = real ? max(0, seq.tokens - seq.rows + row_i[r] + 1) : seq.tokens;
+        limit[r] = real ? sees(seq, row_i[r]) : seq.tokens;
         most = max(most, real ? limit[r] : 0);
         least = min(least, limit[r]);
     }
@@ -527,7 +530,7 @@ template <int RB>
 __device__ inline Line line_of(const Seq& q, int per_token, int few_rows) {
     Line x;
     x.rows = q.rows * per_token;
-    x.seen = max(0, q.tokens - q.rows) * (1. / 32);
+    x.seen = min(max(0, q.end - q.rows), q.tokens) * (1. / 32);
     x.growth = RB / 64. / per_token;
     x.blocks = x.rows > few_rows ? (x.rows + RB - 1) / RB : 0;
     x.length = Line::place(x.blocks, x.seen, x.growth);
@@ -681,7 +684,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         {
             const int lane = opaque(threadIdx.x) & 63, h = lane >> 5, n = lane & 31;
             const Row row = row_of(n);
-            limit = least = row.real ? max(0, seq.tokens - seq.rows + row.i + 1) : seq.tokens;
+            limit = least = row.real ? sees(seq, row.i) : seq.tokens;
             most = row.real ? limit : 0;
             const _Float16* const src = A.q + (seq.row0 + (row.real ? row.i : 0)) * A.q_rs + (int64_t)(row.real ? row.head : kv * gqa) * A.q_hs + 8 * h;
 #pragma unroll
@@ -702,7 +705,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         least = __builtin_amdgcn_readfirstlane(least);
         // the block's tiles: those that its last row sees
         const int last_row = min(flat, (block + 1) * RB) - 1;
-        const int tiles = (max(0, seq.tokens - seq.rows + last_row / gqa + 1) + 31) >> 5;
+        const int tiles = (sees(seq, last_row / gqa) + 31) >> 5;
         const auto tile_at = [&](int x) { return __builtin_amdgcn_readfirstlane((int)((double)(x - unit) * tiles / length)); };
         const int t0 = tile_at(pos), t1 = tile_at(unit_end), stages = (t1 - t0 + NT - 1) / NT;
 

@@ -67,14 +67,15 @@ class Plain:
         new = (rotate(k, cos_sin), v.float())
         for s in range(len(lengths)):
             r, n = begin[s + 1] - begin[s], lengths[s]
-            n = max(0, min(n, table.shape[1] * self.page))
+            n = max(0, n)
+            held = min(n, table.shape[1] * self.page)  # tokens beyond the table do not exist
             first = max(0, n - r)
-            for at in range(first // self.page, -(-n // self.page)) if r else ():
+            for at in range(first // self.page, -(-held // self.page)) if r else ():
                 page = int(table[s, at])
                 if not 0 <= page < self.pages:
                     continue
                 t0 = at * self.page
-                b, e = max(0, first - t0), min(self.page, n - t0)
+                b, e = max(0, first - t0), min(self.page, held - t0)
                 for kv in range(self.kv):
                     for kind in (0, 1):
                         x = new[kind][begin[s] + t0 + b - (n - r):begin[s] + t0 + e - (n - r), kv]
@@ -131,14 +132,15 @@ def attention(plain, table, lengths, begin, q, scale=0.0, lam=None, weight=None,
     out = torch.full((rows, heads, D), math.nan, dtype=torch.float64)
     tol, lse, ltol = out.clone(), torch.full((heads, rows), math.nan, dtype=torch.float64), torch.full((heads, rows), math.nan, dtype=torch.float64)
     for s in range(len(lengths)):
-        r, n = begin[s + 1] - begin[s], max(0, min(lengths[s], table.shape[1] * plain.page))
+        r, end = begin[s + 1] - begin[s], max(0, lengths[s])
+        n = min(end, table.shape[1] * plain.page)
         if not r:
             continue
         a, b = begin[s], begin[s + 1]
         i = torch.arange(r)
         for kv in range(plain.kv):
             k, v, there = plain.values(table[s], n, kv)
-            sees = (torch.arange(n)[None] <= n - r + i[:, None]) & there[None]
+            sees = (torch.arange(n)[None] <= end - r + i[:, None]) & there[None]
             for h in range(kv * g, kv * g + g):
                 o, e = torch.zeros(r, D, dtype=torch.float64), torch.zeros(r, D, dtype=torch.float64)
                 for m in range(maps):

@@ -60,3 +60,54 @@ def test_wide_batch(diff):
             call()
             assert bool((out == 777.0).all())
             begin.copy_(ints(begins(rows)))
+
+
+def test_append_beyond_the_table():
+    """A sequence that outgrows its table leaves what it holds: a step at the first token beyond, rows that begin in front of the table's end and end behind
+    it, rows that are all behind it, by as little and as much as there is."""
+    for page in (32, 128):
+        cap = 3 * page
+        have = [cap, cap, cap - 16, cap - 1, cap, 40]
+        c = Pair(2, page, 6, 3, seed=43).filled(have)
+        before = c.codes.clone(), c.words.clone()
+        for rows, lengths in (([1] * 6, [cap + 1, cap + 900, 1 << 30, (1 << 31) - 1, cap + 1, cap + 1]), ([5, 1, 33, 0, 2, 64], [cap + 5, cap + 6, cap + 40, cap + 9, cap + 2, cap + 64])):
+            c.append(rows, lengths, *c.new(rows, 50.0, 64))
+            c.same()
+            assert torch.equal(before[0], c.codes) and torch.equal(before[1], c.words)
+        rows, lengths = [30, 1, 30, 2, 3, 1], [cap + 14, cap + 1, cap + 14, cap + 1, cap + 1, 41]
+        k, v, cs = c.new(rows, 3.0, 32)
+        c.append(rows, lengths, k, v, cs)
+        c.same()
+        got = kq.KvqPaged8Batch(c.table.cuda(), ints([cap] * 6), ints([16 * s for s in range(7)]), 16)
+        keys, values = (torch.zeros(96, 2, D, device="cuda") for _ in range(2))
+        c.cache.kvq_paged8_read(got, keys, values)
+        # of 30 rows that end 14 tokens beyond, the first 16 are the table's last
+        want = v[31:47].float()
+        assert bool(((values[32:48].cpu() - want).abs() <= want.abs() * 2.0 ** -4 + want.abs().amax() * 2.0 ** -17).all())
+
+
+def test_read_beyond_the_table():
+    """Rows of tokens that the table does not have stay as they were; the others are their own tokens."""
+    cap = 3 * 64
+    c = Pair(2, 64, 4, 3, seed=44).filled([cap] * 4)
+    rows, lengths = [30, 1, 5, 300], [cap + 14, cap + 1, 1 << 30, cap + 290]
+    for dtype in (torch.float16, torch.float32):
+        k, v = (torch.full((sum(rows), 2, D), 777.0, dtype=dtype, device="cuda") for _ in range(2))
+        c.cache.kvq_paged8_read(c.batch(rows, lengths), k, v)
+        whole = [torch.empty(4 * cap, 2, D, dtype=dtype, device="cuda") for _ in range(2)]
+        c.cache.kvq_paged8_read(c.batch([cap] * 4, [cap] * 4), *whole)
+        for got, all_of in zip((k, v), whole):
+            assert torch.equal(got[:16], all_of[cap - 16:cap]) and bool((got[16:36] == 777.0).all())
+            first = cap + 290 - 300  # the fourth's rows are tokens cap - 10 and on
+            assert torch.equal(got[36:46], all_of[3 * cap + first:4 * cap]) and bool((got[46:] == 777.0).all())
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_queries_beyond_the_table(diff):
+    """They see all that the table has; the rows in front of them what they saw without those behind."""
+    cap = 10 * 32
+    c = Pair(4, 32, 5, 10, seed=45).filled([cap, cap, cap, cap, 200])
+    attend(c, 16, [1, 3, 8, 2, 1], [cap + 1, cap + 2, 1 << 30, (1 << 31) - 1, 200], diff=diff)
+    rows, lengths = [300, 290, 310, 90, 100], [cap + 150, cap + 290, 1 << 30, cap + 1, 200]
+    assert in_blocks(4, 4, rows, [cap, cap, cap, cap, 200], diff)
+    attend(c, 16, rows, lengths, diff=diff)
