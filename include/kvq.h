@@ -389,7 +389,7 @@ uint64_t kvq_paged8_workspace_bytes(const kvq_paged8_t* cache, const kvq_paged8_
 /* Attention of the rows over their sequences' cached tokens up to and with their own:
  *   out[r, h, :] = softmax_t(q[r, h, :] . K_hat[t, h / g, :] * softmax_scale) V_hat[t, h / g, :],  g = n_q_heads / n_kv_heads <= 16
  *   over t <= lengths[s] - rows(s) + i for the i-th row of sequence s; a row that sees nothing gives zeros.
- *   q_dev: fp16; out_dev: fp16 or fp32; softmax_scale 0 means 1 / sqrt(128).  lse_dev: fp32 [n_q_heads][n_rows] or NULL, the natural
+ *   q_dev: fp16; out_dev: fp16 (magnitudes beyond 65,504 become it) or fp32; softmax_scale 0 means 1 / sqrt(128).  lse_dev: fp32 [n_q_heads][n_rows] or NULL, the natural
  *   logarithms of the sums of exponentials (-inf where nothing is seen).  Sums and statistics are held in fp32, probabilities are rounded
  *   to fp16 for the product with V_hat.  Equal calls give equal bits. */
 kvq_status_t kvq_paged8_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,

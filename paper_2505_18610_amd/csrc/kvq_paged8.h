@@ -113,6 +113,9 @@ struct Census {
     }
 };
 
+// What an fp16 output takes of a value: a rounded code may lie beyond the largest one.  NaN stays.
+__device__ inline float half_range(float x) { return fabsf(x) > 65504.f ? copysignf(65504.f, x) : x; }
+
 // Whether the sequences have no more rows together than the tensors (row numbers that fall can have it otherwise).
 __device__ inline bool rows_fit(const KvqP8& P) {
     const int lane = threadIdx.x & 63, per = (P.n_seqs + 63) >> 6;

@@ -277,11 +277,7 @@ __device__ inline void store_values(void* to, int64_t at, const float (&x)[8]) {
     } else {
         half8 h;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            // a rounded code may lie beyond the largest value; NaN stays
-            const float y = fabsf(x[e]) > 65504.f ? copysignf(65504.f, x[e]) : x[e];
-            h[e] = (_Float16)y;
-        }
+        for (int e = 0; e < 8; ++e) h[e] = (_Float16)half_range(x[e]);
         __builtin_nontemporal_store(h, reinterpret_cast<half8*>(static_cast<_Float16*>(to) + at));
     }
 }

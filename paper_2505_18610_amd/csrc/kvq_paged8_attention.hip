@@ -504,6 +504,9 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
                 if (!real || (A.maps == 2 && (rest & 1))) continue;
                 const int64_t to = (seq.row0 + i) * A.o_rs + h * A.o_hs;
                 void* const dst = A.out_fp32 ? static_cast<void*>(static_cast<float*>(A.out) + to) : static_cast<void*>(static_cast<_Float16*>(A.out) + to);
+                if (!A.out_fp32)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = half_range(x[e]);
                 kvq_flash::store_out4(dst, A.out_fp32, 4 * chunk, x);
                 if (A.lse && chunk == 0)
                     A.lse[h * A.lse_hs + seq.row0 + i] = fine[r] == 0.f ? -INFINITY : (m[r] + __builtin_amdgcn_logf(fine[r])) * 0.69314718055994530942f;
@@ -1058,6 +1061,8 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                         to4[0] = lo;
                         to4[1] = hi;
                     } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) lo[i] = half_range(lo[i]), hi[i] = half_range(hi[i]);
                         const u32x4 w = {kvq_flash::pack2(lo[0], lo[1]), kvq_flash::pack2(lo[2], lo[3]), kvq_flash::pack2(hi[0], hi[1]), kvq_flash::pack2(hi[2], hi[3])};
                         *reinterpret_cast<u32x4*>(static_cast<_Float16*>(A.out) + to + channel) = w;
                     }

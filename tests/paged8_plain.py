@@ -178,6 +178,8 @@ def attention(plain, table, lengths, begin, q, scale=0.0, lam=None, weight=None,
                         e = ww * (e + o.abs() * off / torch.where(rho == 0, torch.ones_like(rho), rho)) * grown + ww * o.abs() * 2.0 ** -20
                         o = torch.where(rho == 0, torch.zeros_like(o), o / rho) * weight.double()[None]
                     o, e = o * out_scale, e * abs(out_scale)
+                if out_eps == 2.0 ** -11:  # outputs of 16 bits: magnitudes beyond the largest become it
+                    o = o.clamp(-65504, 65504)
                 out[a:b, h], tol[a:b, h] = o, e + out_eps * (o.abs() + e) + 2.0 ** -25
     return out, tol, lse, ltol
 

@@ -111,3 +111,28 @@ def test_queries_beyond_the_table(diff):
     rows, lengths = [300, 290, 310, 90, 100], [cap + 150, cap + 290, 1 << 30, cap + 1, 200]
     assert in_blocks(4, 4, rows, [cap, cap, cap, cap, 200], diff)
     attend(c, 16, rows, lengths, diff=diff)
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_outputs_of_the_largest_values(diff):
+    """Values above 63,488 round to a code of 65,536: outputs of 16 bits take the largest there is, of finite values none is infinite; NaN stays."""
+    for kv, gqa, rows, lengths in ((1, 4, [1, 2, 6, 1], [40, 2, 6, 300]), (4, 4, [600, 600], [600, 600])):
+        assert in_blocks(kv, gqa, rows, lengths, diff) == (kv == 4)
+        c = Pair(kv, 32, len(rows), max(lengths) // 32 + 1, seed=46)
+        k, v, _ = c.new(lengths)
+        v = torch.where(torch.arange(D)[None, None] % 3 == 0, -65504.0, 65504.0).expand_as(v).half().clone()
+        v[lengths[0] - 1, 0, 5] = float("nan")
+        c.append(lengths, lengths, k, v)
+        for out in (torch.float16, torch.float32):
+            attend(c, kv * gqa, rows, lengths, out=out, diff=diff, norm=False, out_scale=1.0)
+        n = sum(rows)
+        q, lam = torch.randn(n, kv * gqa, D, generator=c.g).half().cuda(), torch.full((kv * gqa,), -1.0, device="cuda")
+        batch, got = c.batch(rows, lengths), torch.empty(n, kv * gqa, D, device="cuda").half()
+        ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, kv * gqa, n, diff), dtype=torch.uint8, device="cuda")
+        if diff:  # (twice 65,536)
+            c.cache.kvq_paged8_diff_attention(batch, q, lam, got, workspace=ws)
+        else:
+            c.cache.kvq_paged8_attention(batch, q, got, workspace=ws)
+        nan = torch.isnan(got)
+        assert bool(nan[rows[0] - 1, :gqa, 5].all()) and int(nan.sum()) == gqa
+        assert torch.equal(got.abs()[~nan], torch.full_like(got, 65504.0)[~nan])
