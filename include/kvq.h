@@ -391,7 +391,7 @@ uint64_t kvq_paged8_workspace_bytes(const kvq_paged8_t* cache, const kvq_paged8_
  *   over t <= lengths[s] - rows(s) + i for the i-th row of sequence s; a row that sees nothing gives zeros.
  *   q_dev: fp16; out_dev: fp16 (magnitudes beyond 65,504 become it) or fp32; softmax_scale 0 means 1 / sqrt(128).  lse_dev: fp32 [n_q_heads][n_rows] or NULL, the natural
  *   logarithms of the sums of exponentials (-inf where nothing is seen).  Sums and statistics are held in fp32, probabilities are rounded
- *   to fp16 for the product with V_hat.  Equal calls give equal bits. */
+ *   to fp16 for the product with V_hat, whose values are held to 2^-38 of the sequence's and head's largest.  Equal calls give equal bits. */
 kvq_status_t kvq_paged8_attention(const kvq_paged8_t* cache, const kvq_paged8_batch_t* batch, const kvq_paged8_rows_t* q_dev,
                                   const kvq_paged8_rows_t* out_dev, int32_t n_q_heads, int32_t out_is_fp32, float softmax_scale,
                                   float* lse_dev, void* workspace_dev, uint64_t workspace_bytes, void* hip_stream);

@@ -74,8 +74,12 @@ __device__ inline half8 widen(uint32_t lo, uint32_t hi, float scale) {
 __device__ inline float score_factor(float scale_log2, int word) {
     return fminf(fmaxf(ldexpf(scale_log2, exponent_of(word)), 0x1p-126f), 0x1p126f);
 }
-// Values are taken times 1/2 and outputs times 2: a rounded code may stand for up to 2^16, beyond fp16.
-__device__ inline float value_scale(int word) { return ldexpf(0.5f, exponent_of(word)); }
+// Values of a page are taken times 2^(6 - behind) times their code, where `behind` is how far the page's exponent lies behind the largest, `top`, that the
+// wavefront or workgroup has come to (scale words' low bytes); accumulators stand for 2^(top - KVQ_P8_BIAS - 6) and follow when it grows.  448 2^6 is within
+// fp16, and what fp16 rounds away at its small end, 2^-25, is 2^-38 of that page's largest value (with values as they are, halved, those
+// below 2^-20 lost bits and 2^-24 all of them).
+__device__ inline float value_scale(int behind) { return __builtin_ldexpf(64.f, -behind); }
+__device__ inline float value_unit(int top) { return __builtin_ldexpf(1.f, top - KVQ_P8_BIAS - 6); }
 
 // What NaN codes among a lane's eight of one V operand, of tokens token, token + 1, ..., add to a row that sees those below limit; the codes
 // become zeros.
@@ -202,7 +206,7 @@ template <int R>
 __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(const AttnArgs A) {
     constexpr int RB = 16 * R, W = 8;
     __shared__ float4v lds_o[W][16][32];     // a wavefront's outputs of 16 rows, chunks of four channels turned by the row
-    __shared__ float4v lds_ml[W][16];        // reference, sum, sum of the unrounded
+    __shared__ float4v lds_ml[W][16];        // reference, sum, sum of the unrounded, what the outputs stand for
     __shared__ u32x4 lds_q[R][4][64];        // queries as operands: registers are for tiles on their way
     __shared__ int lds_last;
     const KvqP8& P = A.p;
@@ -300,7 +304,17 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 
     State<R> st;
     st.clear();
+    int top = 0;
     while (from < end) {
+        const int top_here = max(top, wave_max(page >= 0 ? (int)(words[1] & 0xffu) : 0));
+        if (top != 0 && top_here != top) {
+            const float by = __builtin_ldexpf(1.f, top - top_here);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= by;
+        }
+        top = top_here;
         const int todo = min(64, (int)((uint32_t)(end - from + W - 1) / W));
         for (int k = 0; k < todo; ++k) {
             const __amdgpu_buffer_rsrc_t next = tile_at(k + 1);
@@ -338,7 +352,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
                 const float factor = score_factor(A.scale_log2, kw);
 #pragma unroll
                 for (int r = 0; r < R; ++r) softmax_group<R, 1, false, true>(st, r, sc[r], factor, A.lse != nullptr, p[r]);
-                const float vs = value_scale(vw);
+                const float vs = value_scale(top - (vw & 0xff));
                 const bool nan = (vw & KVQ_P8_NAN) != 0;
 #pragma unroll
                 for (int nt = 0; nt < 8; ++nt) {
@@ -381,7 +395,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) lds_o[wave][n][(4 * nt + j + n) & 31] = st.o[r][nt];
             const float sum = quarters_sum(st.l[r]), fine_sum = quarters_sum(st.fine[r]);
-            if (lane < 16) lds_ml[wave][n] = float4v{st.m[r], sum, fine_sum, 0.f};
+            if (lane < 16) lds_ml[wave][n] = float4v{st.m[r], sum, fine_sum, value_unit(top)};
             __syncthreads();
             m[r] = -INFINITY;
 #pragma unroll
@@ -392,7 +406,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
             for (int w = 0; w < W; ++w) {
                 const float4v ml = lds_ml[w][row];
                 const float weight = __builtin_amdgcn_exp2f(ml[0] - reference_of(m[r]));
-                o[r] += lds_o[w][row][(chunk + row) & 31] * weight;
+                o[r] += lds_o[w][row][(chunk + row) & 31] * (weight * ml[3]);
                 l[r] += ml[1] * weight;
                 fine[r] += ml[2] * weight;
             }
@@ -480,7 +494,7 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int f = block * RB + 16 * r + row, i = f / rows_per_token, rest = f - i * rows_per_token;
-                float4v x = o[r] * (2.f * kvq_flash::inverse_of(l[r]));
+                float4v x = o[r] * kvq_flash::inverse_of(l[r]);
                 const int h = kv * A.gqa + (A.maps == 2 ? rest >> 1 : rest);
                 const bool real = i < seq.rows;
                 if (A.maps == 2) {
@@ -717,8 +731,14 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         for (int m = 0; m < MAPS; ++m) st[m].clear();
 
         // Pages and scale words of 64 tiles, one a lane: those that are loaded from, what the softmax needs of those that it has come to, and the 64
-        // tiles behind.  A scale's info: exponents of keys and values in the low bytes, kNan, kThere.
-        constexpr int kNan = 1 << 16, kThere = 1 << 17;
+        // tiles behind.  A scale's info: exponents of keys and values in the low bytes (values': how far behind the largest of these and
+        // earlier tiles, which is kTop's byte), kNan, kThere.
+        constexpr int kNan = 1 << 16, kThere = 1 << 17, kTop = 18;
+        const auto top_of = [](int info) { return __builtin_amdgcn_readfirstlane(info) >> kTop; };
+        const auto ranked = [&](int info, int top) {
+            top = max(top, wave_max(info & kThere ? (info >> 8) & 0xff : 0));
+            return (info & ~0xff00) + (((top - (info >> 8)) & 0xff) << 8) + (top << kTop);
+        };
         const auto page_at = [&](int t) { const int lane = opaque(threadIdx.x) & 63; return t + lane < t1 ? page_of(P, s, (t + lane) >> per_page) : -1; };
         const auto info_of = [&](int pg) {
             if (pg < 0) return 0;
@@ -726,7 +746,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             return (int)((w[0] & 0xffu) | (w[1] & 0xffu) << 8 | (w[1] & KVQ_P8_NAN ? kNan : 0) | kThere);
         };
         int load_batch = t0, soft_batch = t0;
-        int page = page_at(t0), page_next = page_at(t0 + 64), info = info_of(page), info_soft = info, info_next = 0;
+        int page = page_at(t0), page_next = page_at(t0 + 64), info = ranked(info_of(page), 0), info_soft = info, info_next = 0;
 
         struct Raw {
             u32x4 w[NT];
@@ -736,7 +756,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             const int t = t0 + stage * NT + (NT == 2 ? wave >> 2 : 0), lane = opaque(threadIdx.x) & 63;
             if (t0 + stage * NT - load_batch >= 64) {
                 page = page_next;
-                info = info_next;
+                info = ranked(info_next, top_of(info));
                 load_batch += 64;
                 page_next = page_at(load_batch + 64);
             }
@@ -768,7 +788,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                         for (int b = 0; b < 32; b += 8)
                             if (((w[d] >> b) & 0x7fu) == 0x7fu) w[d] &= ~(0xffu << b);
                 }
-                const float vs = value_scale(raw.info >> 8);
+                const float vs = value_scale((raw.info >> 8) & 0xff);
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     *reinterpret_cast<half8*>(to + KVQ_FLASH_TILE_BYTES + (2 * c + k) * 1024 + lane * 16) = widen(w[2 * k], w[2 * k + 1], vs);
@@ -860,6 +880,13 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         const auto softmax = [&](int stage, float16v (&sc)[MAPS][NT]) {
             const int tok = (t0 + stage * NT) * 32, h = (opaque(threadIdx.x) >> 5) & 1;
             if (t0 + stage * NT - soft_batch >= 64) {
+                if (top_of(info) != top_of(info_soft)) {
+                    const float by = __builtin_ldexpf(1.f, top_of(info_soft) - top_of(info));
+#pragma unroll
+                    for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+                        for (int cb = 0; cb < 4; ++cb) st[m].o[cb] *= by;
+                }
                 info_soft = info;
                 soft_batch += 64;
             }
@@ -949,6 +976,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
         // (no piece lies behind the line's end, also where lengths have changed since it was measured)
         const int w0 = unit / share, pieces = (min(unit + length, census.total) - 1) / share - w0 + 1;
         bool mine = true;
+        float unit_of_o = value_unit(top_of(info_soft));
         for (int width = 1, at = wg - w0, level = 0; mine && width < pieces; width *= 2, ++level) {
             const int other = join_other(at, width), begin = min(at, other), second = max(at, other);
             if (second >= pieces) continue;
@@ -973,7 +1001,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                         const float4v x = {o[4 * (v & 3)], o[4 * (v & 3) + 1], o[4 * (v & 3) + 2], o[4 * (v & 3) + 3]};
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, own_at + m * MAP + v * 1024, 0, 16);
                     }
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st[m].m, st[m].l, st[m].fine, 0.f}), to, own_at + m * MAP + 16384, 0, 16);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, float4v{st[m].m, st[m].l, st[m].fine, unit_of_o}), to, own_at + m * MAP + 16384, 0, 16);
                 }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
@@ -996,10 +1024,12 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
 #pragma unroll
                 for (int m = 0; m < MAPS; ++m) {
                     const float m_new = fmaxf(st[m].m, ml[m][0]), ref = reference_of(m_new);
-                    const float a = __builtin_amdgcn_exp2f(st[m].m - ref), b = __builtin_amdgcn_exp2f(ml[m][0] - ref);
+                    float a = __builtin_amdgcn_exp2f(st[m].m - ref), b = __builtin_amdgcn_exp2f(ml[m][0] - ref);
                     st[m].m = m_new;
                     st[m].l = __fadd_rn(__fmul_rn(st[m].l, a), __fmul_rn(ml[m][1], b));
                     st[m].fine = __fadd_rn(__fmul_rn(st[m].fine, a), __fmul_rn(ml[m][2], b));
+                    a *= unit_of_o;
+                    b *= ml[m][3];
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const int i = m * 16 + v;
@@ -1009,6 +1039,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
                         if (i + FLY < 16 * MAPS) x[i % FLY] = load(i + FLY);
                     }
                 }
+                unit_of_o = 1.f;
             }
             at = begin;
         }
@@ -1017,7 +1048,7 @@ __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs
             const Row row = row_of(n);
             float inv[MAPS], by;
 #pragma unroll
-            for (int m = 0; m < MAPS; ++m) inv[m] = 2.f * kvq_flash::inverse_of(halves_sum(st[m].l));
+            for (int m = 0; m < MAPS; ++m) inv[m] = unit_of_o * kvq_flash::inverse_of(halves_sum(st[m].l));
             by = inv[0];
             const float fine = MAPS == 1 ? halves_sum(st[0].fine) : 0.f;
             if (MAPS == 2) {

@@ -4,7 +4,7 @@ import torch
 
 import paper_2505_18610_amd as kq
 from paged8_lines import line
-from paged8_plain import D, attention, check
+from paged8_plain import D, Plain, attention, check
 from test_gpu_paged8 import Pair, attend, begins, in_blocks, ints
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +136,34 @@ def test_outputs_of_the_largest_values(diff):
         nan = torch.isnan(got)
         assert bool(nan[rows[0] - 1, :gqa, 5].all()) and int(nan.sum()) == gqa
         assert torch.equal(got.abs()[~nan], torch.full_like(got, 65504.0)[~nan])
+
+
+@pytest.mark.parametrize("diff", [False, True])
+@pytest.mark.parametrize("power", [-24, -21, -14, -4])
+def test_small_values(power, diff):
+    """Values down to the smallest of fp16 count for what they are: against the same values times a power of two, which takes them to the order of one,
+    where the oracle's bounds have no absolute part that matters."""
+    for kv, gqa, rows, lengths in ((2, 4, [1, 2, 6, 1], [40, 2, 700, 300]), (4, 4, [600, 600], [600, 600])):
+        assert in_blocks(kv, gqa, rows, lengths, diff) == (kv == 4)
+        c = Pair(kv, 32, len(rows), max(lengths) // 32 + 1, seed=47)
+        k, v, _ = c.new(lengths)
+        v = ((1 + v.float().abs()).clamp(max=4) * v.float().sign() * 2.0 ** power).half()
+        c.append(lengths, lengths, k, v)
+        large = Plain(c.plain.codes, c.plain.words)
+        large.words[..., 1] -= power
+        n, heads = sum(rows), kv * gqa
+        q, lam = torch.randn(n, heads, D, generator=c.g).half(), torch.rand(heads, generator=c.g)
+        weight = torch.randn(D, generator=c.g)
+        batch = c.batch(rows, lengths)
+        ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, heads, n, diff), dtype=torch.uint8, device="cuda")
+        got = torch.empty(n, heads, D, device="cuda")
+        if diff:
+            c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, workspace=ws)
+        else:
+            c.cache.kvq_paged8_attention(batch, q.cuda(), got, workspace=ws)
+        want, tol, _, _ = attention(large, c.table, lengths, begins(rows), q, lam=lam if diff else None, out_eps=2.0 ** -24)
+        check(got.double() * 2.0 ** -power, want, tol)
+        if diff:  # (a norm without eps does not see the size)
+            c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, norm_weight=weight.cuda(), norm_eps=0.0, workspace=ws)
+            want, tol, _, _ = attention(large, c.table, lengths, begins(rows), q, lam=lam, weight=weight, eps=0.0, out_eps=2.0 ** -24)
+            check(got, want, tol)
