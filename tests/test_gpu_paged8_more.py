@@ -167,3 +167,79 @@ def test_small_values(power, diff):
             c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, norm_weight=weight.cuda(), norm_eps=0.0, workspace=ws)
             want, tol, _, _ = attention(large, c.table, lengths, begins(rows), q, lam=lam, weight=weight, eps=0.0, out_eps=2.0 ** -24)
             check(got, want, tol)
+
+
+def graded(kv, pages, gains, seed, nan=()):
+    """Pages of 64 tokens, one sequence's, whose values are positive and of the size `gains` says page by page; keys of four sizes in turn."""
+    c = Pair(kv, 64, 1, pages, seed=seed)
+    k, v, _ = c.new([64 * pages])
+    of = torch.arange(64 * pages) // 64
+    k = (k.float() * torch.tensor([0.25, 1.0, 0.5, 2.0])[of % 4, None, None]).half()
+    v = (v.float().abs() * torch.tensor(gains)[of, None, None]).half()
+    for page, token, head, channel in nan:
+        v[64 * page + token, head, channel] = float("nan")
+    c.append([64 * pages], [64 * pages], k, v)
+    return c
+
+
+@pytest.mark.parametrize("diff", [False, True])
+def test_chunk_pieces_of_many_tiles(diff):
+    """A workgroup has more than 128 tiles of one block, so that it comes to a second and a third lot of 64 tables' entries and scale words: pages of many
+    scales, among them one behind the first lot that is larger than all before, NaN and a missing page behind it.  Rows here and there."""
+    kv, gqa, n, pages = 4, 16, 12000, 188
+    rows = 512
+    gains = [2.0 ** (p % 7 - 6) * (1.0 if p < 70 else 16.0 if p < 130 else 200.0) for p in range(pages)]
+    c = graded(kv, pages, gains, 48, nan=((140, 41, 1, 100), (184, 30, 2, 7)))
+    table = c.table.clone()
+    table[0, 120] = -1
+    share, _, longest = line(kv, gqa, [rows], [n], rows, pages * 64)
+    assert longest > 128 and in_blocks(kv, gqa, [rows], [n], diff)
+    g = torch.Generator().manual_seed(8)
+    q, lam = (0.5 * torch.randn(rows, kv * gqa, D, generator=g)).half(), torch.rand(kv * gqa, generator=g)
+    batch = c.batch([rows], [n], table)
+    got, lse = torch.empty(rows, kv * gqa, D, device="cuda"), torch.empty(kv * gqa, rows, device="cuda")
+    ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, kv * gqa, rows, diff), dtype=torch.uint8, device="cuda")
+    if diff:
+        c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, workspace=ws)
+    else:
+        c.cache.kvq_paged8_attention(batch, q.cuda(), got, lse=lse, workspace=ws)
+    some = [0, 17, 255, 306, 511]  # (token 11,806 is NaN, row 318)
+    want, tol, wl, tl = attention(c.plain, table.expand(5, -1), [n - rows + i + 1 for i in some], list(range(6)), q[some], lam=lam if diff else None, out_eps=2.0 ** -24)
+    check(got[some], want, tol)
+    assert bool(torch.isnan(got[:, 16:32, 100]).all())
+    assert bool(torch.isnan(got[318:, 32:48, 7]).all()) and not bool(torch.isnan(got[:318, 32:48, 7]).any())
+    if not diff:
+        check(lse[:, some], wl, tl)
+
+
+@pytest.mark.parametrize("gqa,rows,diff", [(8, 1, False), (16, 1, False), (16, 2, False), (8, 1, True), (16, 1, True)])
+def test_pieces_of_few_rows_of_many_tiles(gqa, rows, diff):
+    """A wavefront has more than 64 tiles, for the same reasons: 128 sequences of 65,536 tokens and a little less over 40 pages that they share."""
+    kv, n, pages = 2, 128, 40
+    gains = [2.0 ** (p % 5 - 4) * (1.0 if p < 20 else 16.0 if p < 30 else 200.0) for p in range(pages)]
+    c = graded(kv, pages, gains, 49, nan=((39, 3, 1, 9),))
+    g = torch.Generator().manual_seed(9)
+    which = torch.randint(0, 20, (n, 1024), generator=g)
+    which[:, 300:500] = torch.randint(0, 30, (n, 200), generator=g)
+    which[:, 800:] = torch.randint(0, 39, (n, 224), generator=g)
+    which[77, 900] = 39
+    table = c.table[0][which].contiguous()
+    table[5, 950] = -1
+    lengths = [65536 - 3 * s for s in range(n)]
+    units, tiles = n * kv, sum(-(-x // 32) for x in lengths) * kv
+    at_a_time = 512 if gqa * rows * (2 if diff else 1) <= 16 else 256
+    assert -(-tiles // at_a_time) > 512 and gqa * rows <= 64 and units <= 256
+    q, lam = (0.5 * torch.randn(n * rows, kv * gqa, D, generator=g)).half(), torch.rand(kv * gqa, generator=g)
+    batch = c.batch([rows] * n, lengths, table)
+    got = torch.empty(n * rows, kv * gqa, D, device="cuda")
+    ws = torch.zeros(kq.kvq_paged8_workspace_bytes(c.cache, batch, kv * gqa, n * rows, diff), dtype=torch.uint8, device="cuda")
+    if diff:
+        c.cache.kvq_paged8_diff_attention(batch, q.cuda(), lam.cuda(), got, workspace=ws)
+    else:
+        c.cache.kvq_paged8_attention(batch, q.cuda(), got, workspace=ws)
+    for s in (5, 77):
+        at = slice(s * rows, (s + 1) * rows)
+        want, tol, _, _ = attention(c.plain, table[s:s + 1], [lengths[s]], [0, rows], q[at], lam=lam if diff else None, out_eps=2.0 ** -24)
+        check(got[at], want, tol)
+    nan = torch.isnan(got)
+    assert bool(nan[77 * rows:78 * rows, gqa:, 9].all()) and int(nan.sum()) == rows * gqa
