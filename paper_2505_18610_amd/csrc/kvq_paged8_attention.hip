@@ -304,17 +304,8 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
 
     State<R> st;
     st.clear();
-    int top = 0;
+    int top = wave_max((int)(words[1] & 0xffu));
     while (from < end) {
-        const int top_here = max(top, wave_max(page >= 0 ? (int)(words[1] & 0xffu) : 0));
-        if (top != 0 && top_here != top) {
-            const float by = __builtin_ldexpf(1.f, top - top_here);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= by;
-        }
-        top = top_here;
         const int todo = min(64, (int)((uint32_t)(end - from + W - 1) / W));
         for (int k = 0; k < todo; ++k) {
             const __amdgpu_buffer_rsrc_t next = tile_at(k + 1);
@@ -377,6 +368,13 @@ __global__ __launch_bounds__(512, R == 1 ? 4 : 2) void kvq_paged8_ranges_kernel(
             describe();
             load_k(tile_at(0));
             load_v(tile_at(0));
+            const int top_here = max(top, wave_max((int)(words[1] & 0xffu)));
+            const float by = __builtin_ldexpf(1.f, top - top_here);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) st.o[r][nt] *= by;
+            top = top_here;
         }
     }
 
