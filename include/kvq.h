@@ -353,7 +353,7 @@ typedef struct {
     int64_t table_stride;
     int32_t n_seqs;                /* 0 .. 4096 */
     int32_t table_pages;
-    int32_t n_rows;                /* rows that the packed tensors of the call have */
+    int32_t n_rows;                /* rows that the packed tensors of the call have, at most 33,554,431 */
     int32_t max_rows;              /* no sequence has more (what it has more does not exist); 1 without row_begin_dev */
 } kvq_paged8_batch_t;
 
@@ -378,8 +378,8 @@ kvq_status_t kvq_paged8_read(const kvq_paged8_t* cache, const kvq_paged8_batch_t
                              const kvq_paged8_rows_t* v_out_dev, int32_t out_is_fp32, void* hip_stream);
 
 /* Bytes of workspace that attention of this batch needs; 0 on invalid arguments, and for batches beyond what one call takes, which are refused: with
- * T = table_pages * page_tokens / 32 and g = n_q_heads / n_kv_heads, n_seqs * n_kv_heads * T * ceil(b / 32) beyond 2^30, where b <= 128 is the least of 64
- * and max_rows * g, times 2 for two maps; or n_kv_heads * B * (T + 16 + max_rows / 64) beyond 2^30, where B is the lesser of
+ * T = table_pages * page_tokens / 32 and g = n_q_heads / n_kv_heads, n_seqs * n_kv_heads * ceil(b / 32) beyond 2^30 / T or 2^23 - 1,024, where b <= 128 is
+ * the lesser of 64 and max_rows * g, times 2 for two maps; or n_kv_heads * B * (T + 16 + max_rows / 64) beyond 2^30, where B is the lesser of
  * n_seqs * ceil(max_rows * g / 256) and n_seqs + n_rows * g / 256 (row_begin_dev must not fall then: where it does, rows of sequences
  * with more than 64 / g rows may be left as they were).  It depends on n_seqs, table_pages, max_rows, n_rows, the
  * page size and the heads only.  The workspace is filled with zeros once, before its first use; every call leaves what it counts with

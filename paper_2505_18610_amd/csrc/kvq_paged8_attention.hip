@@ -199,7 +199,7 @@ struct Cuts {
 // Memory bounds it: a unit's codes are read once, 16 wavefronts of a compute unit have 128 KB on their way (R = 1, at most 128 registers, which is why the
 // queries lie in LDS: 67.0 -> 54.8 us).  4 x 32,768 tokens x 40 heads 49.4 us = 5.4 TB/s, as much as a copy moves; two maps over eight sequences of up
 // to 16,384 tokens 42 us = 5.0; 48 sequences of 41 to 30,000 tokens 49 us = 4.8 (107 with equal shares of all tiles over the units, as short
-// units then waited for one another in one workgroup).  A short call is a chain of trips: 1,001 tokens x 8 heads 8.4 us.
+// units then waited for one another in one workgroup).  A short call is a chain of trips: 1,001 tokens x 8 heads 8.7 us.
 // The hand-over: partial results go out with device-scope stores (sc1), a wait and a barrier stand before the arrival counter, the last to arrive reads
 // them with device-scope loads and leaves the counter at zero for the next call.
 template <int R>
@@ -632,9 +632,9 @@ __device__ inline void softmax_tiles(Map& st, const float16v (&s)[NT], const flo
 // Products and vector instructions bound it, which overlap by half at best (16,000 products of one wavefront a SIMD 298 us, 128,000 multiply-adds of another
 // 316, both 439): matrix cores 40 % busy, vector instructions, products among them, 44 %.  So what counts is few instructions: codes are widened once a
 // workgroup of 256 rows, products are of 32 x 32 (half the instructions and operand reads of 16 x 16), a lane has one row's statistics, the sum is a dot
-// product of the rounded pairs.  Two chunks of 1,024 behind 16,000 tokens x 40 heads 704 us = 923 TFLOP/s where a library product of 8,192^3 has 1,160 (770
-// with four wavefronts of 32 rows each and products of 16 x 16, two workgroups a compute unit), a prompt of 8,192 x 28 heads with two maps 850 us =
-// 849 TFLOP/s (1,110).
+// product of the rounded pairs.  Two chunks of 1,024 behind 16,000 tokens x 40 heads 700 us = 929 TFLOP/s where a library product of 8,192^3 has 1,160 (770
+// with four wavefronts of 32 rows each and products of 16 x 16, two workgroups a compute unit), a prompt of 8,192 x 28 heads with two maps 837 us =
+// 863 TFLOP/s (1,110).
 template <int MAPS>
 __global__ __launch_bounds__(512, 2) void kvq_paged8_chunk_kernel(const AttnArgs A) {
     constexpr int RB = 256, NT = MAPS == 1 ? 2 : 1, KB = 8 / MAPS, TILE = 2 * KVQ_FLASH_TILE_BYTES, STAGE = NT * TILE, AHEAD = 4;
